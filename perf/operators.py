@@ -216,7 +216,7 @@ def prepare(case, seed):
                 s["codes"] = torch.empty(n, 16 * _groups(k), dtype=torch.uint8, device="cuda")
                 s["scales"] = torch.empty(n, _scale_ld(k), dtype=torch.uint8, device="cuda")
                 s["out"] = torch.empty(n, k, dtype=dt, device="cuda")
-                s["q4"] = dlm.make_q4(s["codes"], s["scales"], n, k)
+                s["mx"] = dlm.make_mx(s["codes"], s["scales"], n, k)
             return s
         s["codes"], s["scales"] = _encode(w.float())
         m = case["rows"]
@@ -231,9 +231,9 @@ def prepare(case, seed):
             from paper_2606_29094_amd import dlm
             s["y"] = torch.empty(out, dtype=dt if case["epilogue"] == "swiglu" else torch.float32,
                                  device="cuda")
-            s["q4"] = dlm.make_q4(s["codes"], s["scales"], n, k)
-            s["epilogue"] = dlm.Q4_EPILOGUES[case["epilogue"]]
-            s["ws"] = torch.empty(max(1, dlm.q4_linear_workspace(dt, m, s["q4"], s["epilogue"])),
+            s["mx"] = dlm.make_mx(s["codes"], s["scales"], n, k)
+            s["epilogue"] = dlm.MX_EPILOGUES[case["epilogue"]]
+            s["ws"] = torch.empty(max(1, dlm.mx_linear_workspace(dt, m, s["mx"], s["epilogue"])),
                                   dtype=torch.uint8, device="cuda")
         return s
     h, reqs = HEADS[case["heads"]], _requests(case)
@@ -278,9 +278,9 @@ def prepare(case, seed):
         s["model"] = engine.DeviceModel(shape, {"embed": z(v, d), "lm_head": z(v, d),
                                                 "final_norm": z(d, dtype=torch.float32),
                                                 "layers": [layer]}, 1.0)
-        _, need = dlm.kv_cache_alloc_q4(s["model"].handle, slots, s_max)
+        _, need = dlm.kv_cache_alloc_mx(s["model"].handle, slots, s_max)
         s["buf"] = torch.zeros(need, dtype=torch.uint8, device="cuda")
-        s["cache"], _ = dlm.kv_cache_alloc_q4(s["model"].handle, slots, s_max, s["buf"], need)
+        s["cache"], _ = dlm.kv_cache_alloc_mx(s["model"].handle, slots, s_max, s["buf"], need)
         s["kv_rows"] = dlm.make_kv_rows([(slot[i], l, p, n) for i, (l, p, n) in enumerate(reqs)])
         if case["kind"] == "append":
             s["out"] = {"q": torch.empty(rows, hq * dh, dtype=dt, device="cuda"),
@@ -294,7 +294,7 @@ def prepare(case, seed):
                 s["buf"][at:at + x.numel()].copy_(x)
                 at += -(-x.numel() // 256) * 256
             s["out"] = torch.empty(rows, hq * dh, dtype=dt, device="cuda")
-            s["ws"] = torch.empty(max(1, dlm.q4_kv_attention_workspace(s["cache"], s["kv_rows"])),
+            s["ws"] = torch.empty(max(1, dlm.mx_kv_attention_workspace(s["cache"], s["kv_rows"])),
                                   dtype=torch.uint8, device="cuda")
     return s
 
@@ -309,8 +309,8 @@ def run(s):
 def _run_pack(s, case):
     if own:
         from paper_2606_29094_amd import dlm
-        dlm.q4_pack(s["w"], s["q4"])
-        dlm.q4_unpack(s["q4"], s["out"])
+        dlm.mx_pack(s["w"], s["mx"])
+        dlm.mx_unpack(s["mx"], s["out"])
         return s["out"]
     return _values(*_encode(s["w"].float()), case["k"]).to(s["w"].dtype)
 
@@ -320,7 +320,7 @@ def _run_linear(s, case):
         from paper_2606_29094_amd import dlm
         if case["epilogue"] == "add":
             s["y"].copy_(s["h"])
-        dlm.q4_linear(s["x"], s["q4"], s["y"], s["epilogue"], s["ws"])
+        dlm.mx_linear(s["x"], s["mx"], s["y"], s["epilogue"], s["ws"])
         return s["y"]
     y = s["x"].float() @ _values(s["codes"], s["scales"], case["k"]).T
     if case["epilogue"] == "add":
@@ -342,8 +342,8 @@ def _run_append(s, case):
     if own:
         from paper_2606_29094_amd import dlm
         o = s["out"]
-        dlm.q4_kv_append(s["cache"], 0, s["kv_rows"], s["qkv"], s["rot"], o["q"])
-        dlm.q4_kv_read(s["cache"], 0, s["kv_rows"], o["k"], o["v"])
+        dlm.mx_kv_append(s["cache"], 0, s["kv_rows"], s["qkv"], s["rot"], o["q"])
+        dlm.mx_kv_read(s["cache"], 0, s["kv_rows"], o["k"], o["v"])
         return o
     h = HEADS[case["heads"]]
     hq, hkv, dh, dt = h["hq"], h["hkv"], h["dh"], DTYPE[h["dtype"]]
@@ -358,7 +358,7 @@ def _run_append(s, case):
 def _run_attn(s, case):
     if own:
         from paper_2606_29094_amd import dlm
-        dlm.q4_kv_attention(s["cache"], 0, s["kv_rows"], s["q"], s["out"], s["ws"])
+        dlm.mx_kv_attention(s["cache"], 0, s["kv_rows"], s["q"], s["out"], s["ws"])
         return s["out"]
     return _attention(s, case, torch.float32).to(s["q"].dtype)
 
