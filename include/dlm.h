@@ -300,6 +300,134 @@ dlm_status dlm_head_confidence(dlm_model* m, const void* u_rows, int32_t m_rows,
                                float* conf, int32_t* tok, void* workspace,
                                size_t ws_bytes, void* stream);
 
+/* ---- 4-bit operands: weights and key/value cache in 4 bits ----
+ *
+ * Format. The values of a row are taken in groups of DLM_MX_GROUP consecutive
+ * ones. A group has one scale byte e (the scale is 2^(e - 127); e = 255 makes
+ * every value of the group NaN) and each value a 4-bit code: the sign (bit 3)
+ * and the magnitude 0, 0.5, 1, 1.5, 2, 3, 4, 6 (bits 0-2) in units of the
+ * scale. Element 2i of a row is the low half of its byte i, element 2i + 1 the
+ * high half. (These are the e2m1 elements and e8m0 scales of the OCP
+ * microscaling formats.) Every value is exact in bf16 and fp32 (scales above
+ * 2^125 can stand for values beyond both types' range, which become infinite);
+ * the products below multiply them unrounded and accumulate in fp32.
+ * Packing takes, per group, the power of two that puts the largest magnitude
+ * into (3.5, 7] scales and rounds each value to the nearest representable one
+ * (ties to the even code, at most 6); scale bytes written are 2 .. 252, and 255
+ * with zero codes where the group holds an infinity or a NaN. */
+enum { DLM_MX_GROUP = 32 };
+
+/* A packed matrix [n, k] in device memory; with G = ceil(k / 32):
+ *   codes  [n, 16 G] bytes (codes behind k: zero where the library packs, not
+ *          used otherwise), scales [n, S] bytes, S = G rounded up to a multiple of
+ *          16 (bytes behind G are not used). Both 16-byte aligned. */
+typedef struct dlm_mx {
+  void* codes;
+  uint8_t* scales;
+  int32_t n, k;
+} dlm_mx;
+
+/* Bytes of the two buffers of a packed [n, k] matrix. */
+dlm_status dlm_mx_bytes(int32_t n, int32_t k, size_t* codes_bytes, size_t* scales_bytes);
+
+/* Pack w [n, k] (dtype: dlm_dtype; rows ldw elements apart, any alignment) into
+ * out's buffers. n and k are out's. */
+dlm_status dlm_mx_pack(int32_t dtype, const void* w, int64_t ldw, const dlm_mx* out, void* stream);
+
+/* The values of a packed matrix: out [n, k] in dtype, rows ldo elements apart. */
+dlm_status dlm_mx_unpack(const dlm_mx* w, int32_t dtype, void* out, int64_t ldo, void* stream);
+
+/* Product with a packed matrix: p[m][n] = sum_k x[m][k] w[n][k], x [m_rows, k] in
+ * dtype (rows ldx elements apart, any alignment), accumulated in fp32.
+ * m_rows may be 0 (nothing is enqueued).
+ * Epilogues:
+ *   DLM_MX_STORE   y [m_rows, n] fp32 = p
+ *   DLM_MX_ADD     y [m_rows, n] fp32 += p
+ *   DLM_MX_SWIGLU  y [m_rows, n / 2] in dtype = silu(p[:, f]) * p[:, n / 2 + f]
+ *                  (rows [0, n / 2) of w are the gate weights; n even)
+ * y's rows are ldy elements apart; y must not overlap x. The workspace (256-byte
+ * aligned, at least dlm_mx_linear_workspace bytes for the same dtype, m_rows, w
+ * and epilogue; may be NULL where that is 0) is scratch, overwritten by the call.
+ * The result of a row does not change from call to call. */
+typedef enum { DLM_MX_STORE = 0, DLM_MX_ADD = 1, DLM_MX_SWIGLU = 2 } dlm_mx_epilogue;
+dlm_status dlm_mx_linear_workspace(int32_t dtype, int32_t m_rows, const dlm_mx* w, int32_t epilogue,
+                                   size_t* out_bytes);
+dlm_status dlm_mx_linear(int32_t dtype, const void* x, int64_t ldx, int32_t m_rows, const dlm_mx* w,
+                         int32_t epilogue, void* y, int64_t ldy, void* workspace, size_t ws_bytes,
+                         void* stream);
+
+/* A model whose layer projections are packed (shapes as in dlm_layer_weights);
+ * embedding, LM head and norms as in dlm_weights. Every entry point takes such
+ * a model: its steps multiply by the packed values and are otherwise the
+ * steps of a model that holds those values in its own dtype. */
+typedef struct dlm_layer_mx {
+  const float* attn_norm;
+  dlm_mx w_qkv, w_o;
+  const float* ffn_norm;
+  dlm_mx w_gate_up, w_down;
+} dlm_layer_mx;
+typedef struct dlm_weights_mx {
+  const void* embed;
+  const void* lm_head;
+  const float* final_norm;
+  const dlm_layer_mx* layers; /* host array of n_layers entries, copied by load     */
+} dlm_weights_mx;
+dlm_status dlm_load_weights_mx(const dlm_config* cfg, const dlm_weights_mx* w, dlm_model** out);
+
+/* dlm_kv_cache_alloc for a cache in 4 bits (17/64 of a bf16 cache's bytes): the
+ * steps of such a cache pack the rotated keys and the values of the recomputed
+ * rows, head vector by head vector, and attend over the packed values; any model
+ * may have one. Layout: per layer the codes of the keys
+ * [slot][kv_head][pos][head_dim / 2], the codes of the values, the scales of the
+ * keys [slot][kv_head][pos][head_dim / 32] and the scales of the values, each
+ * part rounded up to 256 bytes, slots rounded up to 64 positions. */
+dlm_status dlm_kv_cache_alloc_mx(const dlm_model* m, int32_t n_slots, int32_t max_seq_len,
+                                 void* dev_buf, size_t buf_bytes, size_t* required_bytes,
+                                 dlm_cache** out);
+
+/* One layer's cache operators alone, on a 4-bit cache (DLM_EUNSUPPORTED for others).
+ * rows: host array [n_req] (1 .. DLM_MAX_REQ) of requests; N is the sum of n_rows,
+ * and the rows of the tensors are packed in request order, positions ascending. Calls
+ * do not look at or change which steps a slot is current for: a caller that
+ * appends to a slot with these invalidates it for dlm_denoise_step by
+ * dlm_cache_invalidate. Device buffers are 16-byte aligned and contiguous. */
+typedef struct dlm_kv_rows {
+  int32_t slot;
+  int32_t seq_len;        /* keys attended: positions [0, seq_len), 0 .. the slot's size  */
+  int32_t pos0;           /* append, read: position of the first row                      */
+  int32_t n_rows;         /* rows, 0 or more; append, read: pos0 + n_rows <= seq_len       */
+} dlm_kv_rows;
+
+/* Append: qkv fp32 [splits, N, (n_q_heads + 2 n_kv_heads) head_dim] (K-split slices,
+ * added in order; one slice is the plain product), rot fp32 [N, head_dim / 2, 2]
+ * (cosine, sine). Element i and i + head_dim / 2 of each query and key head turn to
+ * (a cos - b sin, b cos + a sin), every product and sum rounded to fp32 by itself;
+ * the queries go to q_out [N, n_q_heads head_dim] in the model dtype, the keys and
+ * values are packed from fp32 into the slots. Every other position of the cache
+ * stays as it was. A slot may be listed once (DLM_EINVAL). */
+dlm_status dlm_mx_kv_append(dlm_cache* c, int32_t layer, int32_t n_req, const dlm_kv_rows* rows,
+                            const float* qkv, int32_t splits, const float* rot, void* q_out,
+                            void* stream);
+
+/* The packed keys and values of the rows' positions, k_out and v_out
+ * [N, n_kv_heads head_dim] in the model dtype. */
+dlm_status dlm_mx_kv_read(const dlm_cache* c, int32_t layer, int32_t n_req, const dlm_kv_rows* rows,
+                          void* k_out, void* v_out, void* stream);
+
+/* Attention: out[i] = softmax(q_i K^T / sqrt(head_dim)) V over the request's
+ * positions [0, seq_len), query head h over key/value head h / (n_q_heads /
+ * n_kv_heads); q and out [N, n_q_heads head_dim] in the model dtype (out may not
+ * overlap q). What the cache holds from seq_len on has no effect; rows of a
+ * request with seq_len 0 become zeros. fp32 softmax; the weights enter the second
+ * product as bf16 in bf16 models (at most 2^-9 off each) and as three bf16 terms
+ * (24 bits) in fp32 ones. pos0 is not used, and a slot may be listed more than
+ * once. Workspace: as in dlm_mx_linear, for the same requests. */
+dlm_status dlm_mx_kv_attention_workspace(const dlm_cache* c, int32_t n_req, const dlm_kv_rows* rows,
+                                         size_t* out_bytes);
+dlm_status dlm_mx_kv_attention(const dlm_cache* c, int32_t layer, int32_t n_req,
+                               const dlm_kv_rows* rows, const void* q, void* out, void* workspace,
+                               size_t ws_bytes, void* stream);
+
 /* Test hooks for the bf16 GEMM kernel (the contraction of every projection of
  * the step: QKV, output, gate/up and down). dlm_debug_gemm_info: the output
  * tile (bm x bn) of tile configuration cfg and, in *subs, the sub-tile splits

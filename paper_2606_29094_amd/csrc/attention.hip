@@ -920,3 +920,6 @@ hipError_t attention<float>(const StepPlan& p, const float* q, const float* kc, 
 }
 
 }  // namespace dlm
+
+// attention over a cache in 4 bits
+#include "mx_attention.h"

@@ -620,5 +620,9 @@ hipError_t gemm_lm_head(const GemmPlan& p, const T* U, int ldu, const T* W, int 
                                       float, float*, float*, int*, int, const int*, hipStream_t);
 INST(bf16)
 INST(float)
+#undef INST
 
 }  // namespace dlm
+
+// products with 4-bit matrices
+#include "mx_gemm.h"

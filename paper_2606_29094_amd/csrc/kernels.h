@@ -186,4 +186,60 @@ hipError_t attention(const StepPlan& p, const T* q, const T* kcache, const T* vc
 hipError_t attention_merge(const StepPlan& p, int hq, int dh, int splits, const float* scratch,
                            bf16* out, hipStream_t st);
 
+// ---- 4-bit operands (mx_gemm.h, mx_rowwise.h, mx_attention.h; the format is in mx_common.h) ----
+// A packed [n, k] matrix: groups = ceil(k / 32), codes [n, 16 groups] bytes, scales
+// [n, scale_ld], scale_ld = groups rounded up to 16. Both 16-byte aligned.
+struct MxView { uint8_t* codes; uint8_t* scales; int n, groups, scale_ld; };
+template <typename T>
+hipError_t mx_pack(const T* w, long ldw, int k, const MxView& o, hipStream_t st);
+template <typename T>
+hipError_t mx_unpack(const MxView& w, int k, T* out, long ldo, hipStream_t st);
+// y = x w^T: store or add fp32 [rows, n], or silu(gate) * up in T ([rows, n / 2], rows
+// [0, n / 2) of w the gate). scratch: mx_linear_scratch bytes, 16-byte aligned; aligned:
+// x rows start at multiples of 16 bytes and k is a multiple of 8.
+size_t mx_linear_scratch(int elem, int rows, int k, bool aligned);
+template <typename T>
+hipError_t mx_linear(const T* x, long ldx, int rows, const MxView& w, int k, bool swiglu, bool add,
+                     void* y, long ldy, void* scratch, hipStream_t st);
+// A product's way: straight from the codes, or (gemm) over the matrix unpacked to the
+// scratch and the GEMM kernels of its type.
+struct MxPlan { bool gemm = false; GemmPlan g{}; size_t scratch = 0; };
+MxPlan mx_plan(int elem, int rows, int n, int k, bool swiglu, bool aligned, int num_cu);
+// epilogue: dlm_mx_epilogue
+template <typename T>
+hipError_t mx_matmul(const MxPlan& plan, const T* x, long ldx, int rows, const MxView& w, int k,
+                     int epilogue, void* y, long ldy, void* scratch, hipStream_t st);
+// kernel arguments of a product
+struct MxLinear {
+  const bf16* x;           // [m, ldx], NP planes `plane` elements apart
+  long ldx, plane;
+  MxView w;
+  int m, k;                // k: elements of x a row holds (a multiple of 8)
+  void* y;
+  long ldy;
+  bool swiglu, add;
+};
+
+// One layer of a 4-bit key/value cache: codes [slot][kv_head][pos][dh / 2] and scales
+// [slot][kv_head][pos][dh / 32] of the keys and of the values, s_max positions a slot.
+struct MxKv { uint8_t *kc, *vc, *ks, *vs; int s_max; };
+// queries rotated to T, keys (rotated) and values packed at (slot, head, pos) of each row
+template <typename T>
+hipError_t mx_kv_append(const StepPlan& p, const float* qkv, int splits, long split_stride,
+                        const float2* cs, int hq, int hkv, int dh, T* q_out, const MxKv& kv,
+                        hipStream_t st);
+// the stored keys and values of each row, [rows, hkv dh]
+template <typename T>
+hipError_t mx_kv_read(const StepPlan& p, int hkv, int dh, const MxKv& kv, T* k, T* v,
+                      hipStream_t st);
+// Attention of every row over [0, seq_len) of its request's slot (zeros where that is
+// empty). splits > 1: the keys of a request are split over blocks, their partials go to
+// scratch (mx_attention_scratch bytes) and a second kernel joins them.
+int mx_attention_splits(const StepPlan& p, int hq, int hkv, int dh, size_t elem,
+                        size_t scratch_bytes, int num_cu);
+size_t mx_attention_scratch(int rows, int hq, int dh, int splits);
+template <typename T>
+hipError_t mx_attention(const StepPlan& p, const T* q, const MxKv& kv, int hq, int hkv, int dh,
+                        T* out, int splits, float* scratch, hipStream_t st);
+
 }  // namespace dlm

@@ -1,0 +1,63 @@
+// 4-bit operands: groups of 32 consecutive values of a row, one scale byte e for
+// each group (the scale 2^(e - 127); 255: every value of the group is NaN) and a
+// 4-bit code for each value: a sign and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6. Element
+// 2i of a row is the low half of its byte i. A code times its scale is exact in
+// bf16 and in fp32 (at most two significant bits), and gfx950 converts two codes
+// with their scale in one instruction (v_cvt_scalef32_pk_bf16_fp4, which reads the
+// scale's exponent field and gives NaN for 255), so the products below multiply
+// the values themselves: nothing is rounded between the stored codes and the
+// matrix cores.
+#pragma once
+
+#include "common.h"
+
+namespace dlm {
+
+constexpr int kMxGroup = 32;
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+// the scale operand of the conversions for a scale byte
+__device__ __forceinline__ float mx_scale(uint32_t e) { return __uint_as_float(e << 23); }
+
+// eight codes (one dword, in element order) -> bf16
+__device__ __forceinline__ bf16x8 mx_bf16x8(uint32_t w, float s) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 0);
+  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 1);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 2);
+  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// Scale byte of a group from the largest magnitude's bits (any value's bits without
+// the sign, compared as integers: NaN and infinity come out above every number).
+// e is the exponent that puts the largest magnitude into (3.5, 7] scales, so it
+// rounds to 4 or 6 and no value is off by more than one step. The
+// ends are clamped so that every code times the scale is a normal number: below
+// 2^-126 nothing is kept, and the top scale stays at 2^125.
+__device__ __forceinline__ uint32_t mx_scale_byte(uint32_t amax) {
+  if (amax >= 0x7f800000u) return 255u;
+  const int e = (int)(amax >> 23) - 2 + ((amax & 0x7fffffu) > 0x600000u ? 1 : 0);
+  return (uint32_t)min(max(e, 2), 252);
+}
+
+// four values -> 16 bits of codes, round to nearest (ties to the even code)
+__device__ __forceinline__ uint32_t mx_codes4(float a, float b, float c, float d, float s) {
+  uint32_t r = 0;
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, a, b, s, 0);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, c, d, s, 1);
+  return r & 0xffffu;
+}
+
+// fp32 x as the sum of three bf16 terms, which together hold its 24 bits: products
+// of 4-bit values with fp32 ones run on the bf16 matrix cores, exactly to each term.
+// What no bf16 holds (beyond 3.39e38, infinities, NaN) goes into the first term alone.
+__device__ __forceinline__ void split3(float x, bf16& hi, bf16& mid, bf16& lo) {
+  hi = (bf16)x;
+  float r = x - (float)hi;
+  r = __builtin_isfinite(r) ? r : 0.f;
+  mid = (bf16)r;
+  lo = (bf16)(r - (float)mid);
+}
+
+}  // namespace dlm

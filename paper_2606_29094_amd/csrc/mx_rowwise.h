@@ -1,0 +1,248 @@
+// 4-bit matrices and caches (mx_common.h), row by row: packing, unpacking, appending
+// rotated keys and values, reading them back. Part of rowwise.hip.
+#pragma once
+
+#include "kernels.h"
+#include "mx_common.h"
+
+namespace dlm {
+
+namespace {
+
+// ------------------------------------------------------------ pack, unpack --
+// One thread per group: 32 values, 16 bytes of codes, a scale byte. Streaming;
+// bound by memory. Threads of the padding groups of a row clear its scale bytes.
+template <typename T>
+__device__ __forceinline__ void load_group(const T* p, int n, bool vec, float (&x)[kMxGroup]) {
+  if (vec && n >= kMxGroup) {
+    constexpr int V = 16 / sizeof(T);
+    typedef T vt __attribute__((ext_vector_type(V)));
+#pragma unroll
+    for (int i = 0; i < kMxGroup / V; ++i) {
+      const vt v = reinterpret_cast<const vt*>(p)[i];
+#pragma unroll
+      for (int j = 0; j < V; ++j) x[i * V + j] = to_f32((T)v[j]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < kMxGroup; ++i) x[i] = i < n ? to_f32(p[i]) : 0.f;
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void mx_pack_kernel(const T* __restrict__ w, long ldw, int k,
+                                                      int vec, MxView o, long total) {
+  const long at = (long)blockIdx.x * 256 + threadIdx.x;
+  if (at >= total) return;
+  const long row = at / o.scale_ld;
+  const int g = (int)(at - row * o.scale_ld);
+  if (g >= o.groups) {
+    o.scales[at] = 0;
+    return;
+  }
+  float x[kMxGroup];
+  load_group(w + row * ldw + g * kMxGroup, k - g * kMxGroup, vec != 0, x);
+  uint32_t amax = 0;
+#pragma unroll
+  for (int i = 0; i < kMxGroup; ++i) amax = max(amax, __float_as_uint(x[i]) & 0x7fffffffu);
+  const uint32_t e = mx_scale_byte(amax);
+  const float s = mx_scale(e);
+  u32x4 c;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    c[i] = e == 255u ? 0u
+                     : mx_codes4(x[8 * i], x[8 * i + 1], x[8 * i + 2], x[8 * i + 3], s) |
+                           mx_codes4(x[8 * i + 4], x[8 * i + 5], x[8 * i + 6], x[8 * i + 7], s) << 16;
+  reinterpret_cast<u32x4*>(o.codes)[row * o.groups + g] = c;
+  o.scales[at] = (uint8_t)e;
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void mx_unpack_kernel(MxView w, int k, int vec,
+                                                        T* __restrict__ out, long ldo, long total) {
+  const long at = (long)blockIdx.x * 256 + threadIdx.x;
+  if (at >= total) return;
+  const long row = at / w.groups;
+  const int g = (int)(at - row * w.groups);
+  const u32x4 c = reinterpret_cast<const u32x4*>(w.codes)[at];
+  const float s = mx_scale(w.scales[row * w.scale_ld + g]);
+  const int n = k - g * kMxGroup;
+  T* o = out + row * ldo + g * kMxGroup;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const bf16x8 v = mx_bf16x8(c[i], s);
+    if (vec && n >= kMxGroup) {
+      if constexpr (sizeof(T) == 2) {
+        reinterpret_cast<bf16x8*>(o)[i] = v;
+      } else {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          reinterpret_cast<f32x4*>(o)[2 * i + h] = f32x4{(float)v[4 * h], (float)v[4 * h + 1],
+                                                         (float)v[4 * h + 2], (float)v[4 * h + 3]};
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (8 * i + j < n) o[8 * i + j] = (T)(float)v[j];
+    }
+  }
+}
+
+// ------------------------------------------------------------------ append --
+// One block: 256 / QUADS heads of one row, QUADS = dh / 8 lanes a head; a lane takes
+// four consecutive elements of the head's first half and the same four of the
+// second, which are its rotary partners. Eight lanes hold a group of 32 of each
+// half and find its largest magnitude with three lane exchanges. Bound by memory:
+// it reads the product's fp32 slices once.
+//
+// Every product of the rotation is rounded by itself (no fused multiply-add): the
+// stored codes then follow from the inputs by plain fp32 operations, and a value on
+// the border of two codes falls to the same side wherever it is computed.
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void mx_append_kernel(StepPlan p, const float* __restrict__ qkv,
+                                                        int splits, long split_stride,
+                                                        const float2* __restrict__ cs, int hq,
+                                                        int hkv, T* __restrict__ q_out, MxKv kv) {
+#pragma clang fp contract(off)
+  constexpr int HALF = DH / 2, QUADS = HALF / 4, GROUPS = DH / kMxGroup;
+  const int row = blockIdx.x;
+  const int r = plan_req_of_row(p, row);
+  const int y = blockIdx.y * (256 / QUADS) + threadIdx.x / QUADS;   // head: q, then k, then v
+  const int i = threadIdx.x % QUADS * 4;
+  const int heads = hq + 2 * hkv;
+  if (y >= heads) return;   // (whole groups of QUADS lanes: the exchanges stay among live lanes)
+  const float* src = qkv + ((long)row * heads + y) * DH + i;
+  f32x4 a = *reinterpret_cast<const f32x4*>(src);
+  f32x4 b = *reinterpret_cast<const f32x4*>(src + HALF);
+  for (int s = 1; s < splits; ++s) {
+    a += *reinterpret_cast<const f32x4*>(src + s * split_stride);
+    b += *reinterpret_cast<const f32x4*>(src + s * split_stride + HALF);
+  }
+  if (y < hq + hkv) {
+    const f32x4 c0 = *reinterpret_cast<const f32x4*>(cs + (long)row * HALF + i);
+    const f32x4 c1 = *reinterpret_cast<const f32x4*>(cs + (long)row * HALF + i + 2);
+    const f32x4 c = {c0[0], c0[2], c1[0], c1[2]}, d = {c0[1], c0[3], c1[1], c1[3]};
+    const f32x4 ac = a * c, bd = b * d, bc = b * c, ad = a * d;
+    a = ac - bd;
+    b = bc + ad;
+  }
+  if (y < hq) {
+    T* o = q_out + ((long)row * hq + y) * DH + i;
+    typedef T T4 __attribute__((ext_vector_type(4)));
+    *reinterpret_cast<T4*>(o) = T4{from_f32<T>(a[0]), from_f32<T>(a[1]), from_f32<T>(a[2]), from_f32<T>(a[3])};
+    *reinterpret_cast<T4*>(o + HALF) =
+        T4{from_f32<T>(b[0]), from_f32<T>(b[1]), from_f32<T>(b[2]), from_f32<T>(b[3])};
+    return;
+  }
+  const bool is_v = y >= hq + hkv;
+  const ReqPlan& q = p.r[r];
+  const long at = ((long)q.slot * hkv + (y - hq - (is_v ? hkv : 0))) * kv.s_max + q.pos0 + (row - q.row0);
+  uint8_t* codes = (is_v ? kv.vc : kv.kc) + at * (DH / 2);
+  uint8_t* scales = (is_v ? kv.vs : kv.ks) + at * GROUPS;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const f32x4 x = h ? b : a;
+    uint32_t amax = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) amax = max(amax, __float_as_uint(x[j]) & 0x7fffffffu);
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) amax = max(amax, (uint32_t)__shfl_xor((int)amax, o, kWave));
+    const uint32_t e = mx_scale_byte(amax);
+    const uint32_t w = e == 255u ? 0u : mx_codes4(x[0], x[1], x[2], x[3], mx_scale(e));
+    const int d = i + h * HALF;
+    *reinterpret_cast<uint16_t*>(codes + d / 2) = (uint16_t)w;
+    if (d % kMxGroup == 0) scales[d / kMxGroup] = (uint8_t)e;
+  }
+}
+
+// The stored values: one thread per group.
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void mx_read_kernel(StepPlan p, int hkv, MxKv kv,
+                                                      T* __restrict__ k, T* __restrict__ v) {
+  constexpr int GROUPS = DH / kMxGroup;
+  const int row = blockIdx.x;
+  const int r = plan_req_of_row(p, row);
+  const ReqPlan& q = p.r[r];
+  for (int i = threadIdx.x; i < 2 * hkv * GROUPS; i += 256) {
+    const bool is_v = i >= hkv * GROUPS;
+    const int j = i - (is_v ? hkv * GROUPS : 0), head = j / GROUPS, g = j % GROUPS;
+    const long at = ((long)q.slot * hkv + head) * kv.s_max + q.pos0 + (row - q.row0);
+    const u32x4 c = reinterpret_cast<const u32x4*>(is_v ? kv.vc : kv.kc)[at * GROUPS + g];
+    const float s = mx_scale((is_v ? kv.vs : kv.ks)[at * GROUPS + g]);
+    T* o = (is_v ? v : k) + (long)row * hkv * DH + head * DH + g * kMxGroup;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const bf16x8 x = mx_bf16x8(c[w], s);
+      if constexpr (sizeof(T) == 2) {
+        reinterpret_cast<bf16x8*>(o)[w] = x;
+      } else {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          reinterpret_cast<f32x4*>(o)[2 * w + h] =
+              f32x4{(float)x[4 * h], (float)x[4 * h + 1], (float)x[4 * h + 2], (float)x[4 * h + 3]};
+      }
+    }
+  }
+}
+
+}  // namespace
+
+template <typename T>
+hipError_t mx_pack(const T* w, long ldw, int k, const MxView& o, hipStream_t st) {
+  const long total = (long)o.n * o.scale_ld;
+  const int vec = reinterpret_cast<uintptr_t>(w) % 16 == 0 && ldw * sizeof(T) % 16 == 0;
+  DLM_LAUNCH(mx_pack_kernel<T>, dim3((unsigned)((total + 255) / 256)), dim3(256), 0, st, w, ldw, k,
+             vec, o, total);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t mx_unpack(const MxView& w, int k, T* out, long ldo, hipStream_t st) {
+  const long total = (long)w.n * w.groups;
+  const int vec = reinterpret_cast<uintptr_t>(out) % 16 == 0 && ldo * sizeof(T) % 16 == 0;
+  DLM_LAUNCH(mx_unpack_kernel<T>, dim3((unsigned)((total + 255) / 256)), dim3(256), 0, st, w, k, vec,
+             out, ldo, total);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t mx_kv_append(const StepPlan& p, const float* qkv, int splits, long split_stride,
+                        const float2* cs, int hq, int hkv, int dh, T* q_out, const MxKv& kv,
+                        hipStream_t st) {
+  if (p.n_rows == 0) return hipSuccess;
+  const dim3 grid(p.n_rows, ceil_div((hq + 2 * hkv) * (dh / 8), 256));
+  if (dh == 128)
+    DLM_LAUNCH((mx_append_kernel<T, 128>), grid, dim3(256), 0, st, p, qkv, splits, split_stride, cs, hq,
+               hkv, q_out, kv);
+  else if (dh == 64)
+    DLM_LAUNCH((mx_append_kernel<T, 64>), grid, dim3(256), 0, st, p, qkv, splits, split_stride, cs, hq,
+               hkv, q_out, kv);
+  else
+    return hipErrorInvalidValue;
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t mx_kv_read(const StepPlan& p, int hkv, int dh, const MxKv& kv, T* k, T* v,
+                      hipStream_t st) {
+  if (p.n_rows == 0) return hipSuccess;
+  if (dh == 128)
+    DLM_LAUNCH((mx_read_kernel<T, 128>), dim3(p.n_rows), dim3(256), 0, st, p, hkv, kv, k, v);
+  else if (dh == 64)
+    DLM_LAUNCH((mx_read_kernel<T, 64>), dim3(p.n_rows), dim3(256), 0, st, p, hkv, kv, k, v);
+  else
+    return hipErrorInvalidValue;
+  return hipGetLastError();
+}
+
+#define INST(T)                                                                                 \
+  template hipError_t mx_pack<T>(const T*, long, int, const MxView&, hipStream_t);              \
+  template hipError_t mx_unpack<T>(const MxView&, int, T*, long, hipStream_t);                  \
+  template hipError_t mx_kv_append<T>(const StepPlan&, const float*, int, long, const float2*,  \
+                                      int, int, int, T*, const MxKv&, hipStream_t);             \
+  template hipError_t mx_kv_read<T>(const StepPlan&, int, int, const MxKv&, T*, T*, hipStream_t);
+INST(bf16)
+INST(float)
+#undef INST
+
+}  // namespace dlm

@@ -738,5 +738,9 @@ hipError_t unmask_select(const StepPlan& p, const float* conf, const int* tok,
                                           hipStream_t);
 INST(bf16)
 INST(float)
+#undef INST
 
 }  // namespace dlm
+
+// 4-bit matrices and caches
+#include "mx_rowwise.h"

@@ -9,6 +9,7 @@
 #include <cstdint>
 #include <cstdarg>
 #include <cstdio>
+#include <cstring>
 #include <mutex>
 #include <string>
 #include <utility>
@@ -17,6 +18,7 @@
 #include "../../include/dlm.h"
 #include "common.h"
 #include "kernels.h"
+#include "mx_common.h"
 
 using namespace dlm;
 
@@ -155,6 +157,7 @@ struct dlm_model {
   const void* lm_head;
   const float* final_norm;
   std::vector<dlm_layer_weights> layers;
+  std::vector<dlm_layer_mx> mx;   // packed projections (dlm_load_weights_mx), or empty
   int num_cu;
   size_t es;   // element size
 };
@@ -172,8 +175,14 @@ struct dlm_cache {
   char* base;
   size_t region;      // bytes of one layer's K (or V) region
   std::vector<SlotState> slots;
+  bool mx = false;            // 4-bit slots: region is then the bytes of one layer's codes
+  size_t scale_region = 0;    // and this the bytes of one layer's scales (keys or values)
   void* k_layer(int l) const { return base + (size_t)(2 * l) * region; }
   void* v_layer(int l) const { return base + (size_t)(2 * l + 1) * region; }
+  MxKv mx_layer(int l) const {
+    uint8_t* b = reinterpret_cast<uint8_t*>(base) + (size_t)(2 * l) * (region + scale_region);
+    return {b, b + region, b + 2 * region, b + 2 * region + scale_region, s_max};
+  }
 };
 
 namespace {
@@ -181,10 +190,16 @@ namespace {
 // Workspace layout of a step with n recomputed rows and n_req requests.
 struct Layout {
   size_t h, a, qkv, cs, q, ao, part, act, lm_rows, lm_count, req_off, req_cnt, u, pm, ps, pi,
-      conf, tok, total;
+      conf, tok, mx, total;
   GemmPlan g_qkv, g_o, g_gu, g_down, g_lm, g_logits;
+  MxPlan q_qkv, q_o, q_gu, q_down;   // of a model with packed projections
   int s_qkv, s_o, s_down, tiles, m_max;
 };
+
+MxView mx_view(const dlm_mx& w) {
+  const int groups = ceil_div(w.k, kMxGroup);
+  return {reinterpret_cast<uint8_t*>(w.codes), w.scales, w.n, groups, ceil_div(groups, 16) * 16};
+}
 
 GemmPlan projection_plan(int es, int rows, int N, int K, int num_cu) {
   return gemm_plan(es, rows, N, K, true, num_cu);
@@ -211,6 +226,13 @@ Layout layout(const dlm_model* m, int n, int n_req) {
   L.s_qkv = L.g_qkv.splits;
   L.s_o = L.g_o.splits;
   L.s_down = L.g_down.splits;
+  if (!m->mx.empty()) {
+    L.q_qkv = mx_plan(es_i, n, qkv_dim, c.d_model, false, true, m->num_cu);
+    L.q_o = mx_plan(es_i, n, c.d_model, qd, false, true, m->num_cu);
+    L.q_gu = mx_plan(es_i, n, 2 * c.d_ffn, c.d_model, true, true, m->num_cu);
+    L.q_down = mx_plan(es_i, n, c.d_model, c.d_ffn, false, true, m->num_cu);
+    L.s_qkv = L.s_o = L.s_down = 1;
+  }
   L.tiles = lm_head_tiles(L.g_lm, c.vocab);
   const size_t es = m->es;
   size_t off = 0;
@@ -237,6 +259,7 @@ Layout layout(const dlm_model* m, int n, int n_req) {
   L.pi = take((size_t)L.tiles * std::max(L.m_max, 1) * 4);
   L.conf = take((size_t)std::max(L.m_max, 1) * 4);
   L.tok = take((size_t)std::max(L.m_max, 1) * 4);
+  L.mx = take(std::max({L.q_qkv.scratch, L.q_o.scratch, L.q_gu.scratch, L.q_down.scratch}));
   L.total = off;
   return L;
 }
@@ -387,6 +410,10 @@ dlm_status run_forward(dlm_model* m, dlm_cache* c, const dlm_batch* b, const Ste
   T* act = reinterpret_cast<T*>(ws + L.act);
   // part and act (consecutive) hold nothing while attention runs: its key splits' partials go there
   const AttnPlan ap = attention_plan(p, hq, hkv, dh, sizeof(T), L.lm_rows - L.part, m->num_cu);
+  const int mx_splits =
+      c->mx ? mx_attention_splits(p, hq, hkv, dh, sizeof(T), L.lm_rows - L.part, m->num_cu) : 1;
+  const bool w4 = !m->mx.empty();
+  void* const mxs = ws + L.mx;
 
   LAUNCH(m, st, "embed_norm", embed_norm_rows<T>(p, reinterpret_cast<const T*>(m->embed), d, cf.vocab,
                          cf.mask_id, b->tokens, b->mask, m->layers[0].attn_norm, cf.rms_eps, dh,
@@ -394,27 +421,45 @@ dlm_status run_forward(dlm_model* m, dlm_cache* c, const dlm_batch* b, const Ste
   const size_t es = sizeof(T);
   for (int l = 0; l < cf.n_layers; ++l) {
     const dlm_layer_weights& w = m->layers[l];
-    T* kc = reinterpret_cast<T*>(c->k_layer(l));
-    T* vc = reinterpret_cast<T*>(c->v_layer(l));
+    const dlm_layer_mx* w4l = w4 ? &m->mx[l] : nullptr;
+    const MxKv kv4 = c->mx ? c->mx_layer(l) : MxKv{};
+    T* kc = c->mx ? nullptr : reinterpret_cast<T*>(c->k_layer(l));
+    T* vc = c->mx ? nullptr : reinterpret_cast<T*>(c->v_layer(l));
     const dlm_trace* t = tr && tr->layer == l ? tr : nullptr;
     if (t) {
       TRACE_COPY(t->h_in, h, (size_t)n * d * 4);
       TRACE_COPY(t->a_attn, a, (size_t)n * d * es);
     }
-    LAUNCH(m, st, "gemm_qkv", gemm_store_f32<T>(L.g_qkv, a, d, reinterpret_cast<const T*>(w.w_qkv), d, n,
+    if (w4)
+      LAUNCH(m, st, "gemm_qkv", mx_matmul<T>(L.q_qkv, a, d, n, mx_view(w4l->w_qkv), d, DLM_MX_STORE, qkv,
+                                             qkv_dim, mxs, st));
+    else
+      LAUNCH(m, st, "gemm_qkv", gemm_store_f32<T>(L.g_qkv, a, d, reinterpret_cast<const T*>(w.w_qkv), d, n,
                                                       qkv_dim, d, qkv, qkv_dim, st));
     if (t) TRACE_COPY(t->qkv, qkv, (size_t)L.s_qkv * n * qkv_dim * 4);
-    LAUNCH(m, st, "rope_kv_write", qkv_rope_scatter<T>(p, qkv, L.s_qkv, (long)n * qkv_dim, cs, hq, hkv, dh, q, kc, vc,
+    if (c->mx)
+      LAUNCH(m, st, "rope_kv_write", mx_kv_append<T>(p, qkv, L.s_qkv, (long)n * qkv_dim, cs, hq, hkv, dh,
+                                                     q, kv4, st));
+    else
+      LAUNCH(m, st, "rope_kv_write", qkv_rope_scatter<T>(p, qkv, L.s_qkv, (long)n * qkv_dim, cs, hq, hkv, dh, q, kc, vc,
                                  c->s_max, st));
     if (t) TRACE_COPY(t->q, q, (size_t)n * qd * es);
-    LAUNCH(m, st, "attention", attention<T>(p, q, kc, vc, c->s_max, hq, hkv, dh, ao, ap, part, st));
-    if constexpr (sizeof(T) == 2)
-      if (ap.splits > 1)
-        LAUNCH(m, st, "attention_merge", attention_merge(p, hq, dh, ap.splits, part, ao, st));
+    if (c->mx) {
+      LAUNCH(m, st, "attention", mx_attention<T>(p, q, kv4, hq, hkv, dh, ao, mx_splits, part, st));
+    } else {
+      LAUNCH(m, st, "attention", attention<T>(p, q, kc, vc, c->s_max, hq, hkv, dh, ao, ap, part, st));
+      if constexpr (sizeof(T) == 2)
+        if (ap.splits > 1)
+          LAUNCH(m, st, "attention_merge", attention_merge(p, hq, dh, ap.splits, part, ao, st));
+    }
     if (t) TRACE_COPY(t->attn_out, ao, (size_t)n * qd * es);
     // O projection; its residual update is fused into the FFN norm when K is split
     if (L.s_o == 1) {
-      LAUNCH(m, st, "gemm_o", gemm_add_f32<T>(L.g_o, ao, qd, reinterpret_cast<const T*>(w.w_o), qd, n, d,
+      if (w4)
+        LAUNCH(m, st, "gemm_o", mx_matmul<T>(L.q_o, ao, qd, n, mx_view(w4l->w_o), qd, DLM_MX_ADD, h, d,
+                                             mxs, st));
+      else
+        LAUNCH(m, st, "gemm_o", gemm_add_f32<T>(L.g_o, ao, qd, reinterpret_cast<const T*>(w.w_o), qd, n, d,
                                                   qd, h, d, st));
       LAUNCH(m, st, "rmsnorm", rmsnorm_rows<T>(h, w.ffn_norm, n, d, cf.rms_eps, a, st));
     } else {
@@ -427,14 +472,22 @@ dlm_status run_forward(dlm_model* m, dlm_cache* c, const dlm_batch* b, const Ste
       TRACE_COPY(t->h_mid, h, (size_t)n * d * 4);
       TRACE_COPY(t->a_ffn, a, (size_t)n * d * es);
     }
-    LAUNCH(m, st, "gemm_gate_up_swiglu", gemm_swiglu<T>(L.g_gu, a, d, reinterpret_cast<const T*>(w.w_gate_up), d, n, cf.d_ffn, d, act,
+    if (w4)
+      LAUNCH(m, st, "gemm_gate_up_swiglu", mx_matmul<T>(L.q_gu, a, d, n, mx_view(w4l->w_gate_up), d,
+                                                        DLM_MX_SWIGLU, act, cf.d_ffn, mxs, st));
+    else
+      LAUNCH(m, st, "gemm_gate_up_swiglu", gemm_swiglu<T>(L.g_gu, a, d, reinterpret_cast<const T*>(w.w_gate_up), d, n, cf.d_ffn, d, act,
                             cf.d_ffn, st));
     if (t) TRACE_COPY(t->act, act, (size_t)n * cf.d_ffn * es);
     // down projection; its residual update is fused into the next layer's norm
     const float* next_norm = l + 1 < cf.n_layers ? m->layers[l + 1].attn_norm : nullptr;
     T* next_a = l + 1 < cf.n_layers ? a : nullptr;
     if (L.s_down == 1) {
-      LAUNCH(m, st, "gemm_down", gemm_add_f32<T>(L.g_down, act, cf.d_ffn, reinterpret_cast<const T*>(w.w_down), cf.d_ffn, n, d,
+      if (w4)
+        LAUNCH(m, st, "gemm_down", mx_matmul<T>(L.q_down, act, cf.d_ffn, n, mx_view(w4l->w_down), cf.d_ffn,
+                                                DLM_MX_ADD, h, d, mxs, st));
+      else
+        LAUNCH(m, st, "gemm_down", gemm_add_f32<T>(L.g_down, act, cf.d_ffn, reinterpret_cast<const T*>(w.w_down), cf.d_ffn, n, d,
                                cf.d_ffn, h, d, st));
       if (next_a) LAUNCH(m, st, "rmsnorm", rmsnorm_rows<T>(h, next_norm, n, d, cf.rms_eps, a, st));
     } else {
@@ -507,6 +560,77 @@ dlm_status dispatch(dlm_model* m, dlm_cache* c, const dlm_batch* b, const StepPl
   return run_step<float>(m, c, b, p, L, w, tail, out, logits, tr, st);
 }
 
+int device_cus() {
+  int dev = 0, cu = 0;
+  const bool ok = hipGetDevice(&dev) == hipSuccess &&
+                  hipDeviceGetAttribute(&cu, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess &&
+                  cu > 0;
+  (void)hipGetLastError();
+  return ok ? cu : 256;
+}
+
+// ---- 4-bit operands ----
+bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+// A packed matrix of the given shape (n, k < 0: any), with buffers the kernels can read.
+dlm_status check_mx(const dlm_mx* w, int n, int k, const char* what) {
+  if (!w || !w->codes || !w->scales) return fail(DLM_EINVAL, "%s: packed matrix pointer is NULL", what);
+  if (w->n < 1 || w->k < 1) return fail(DLM_EINVAL, "%s: packed matrix of %d x %d", what, w->n, w->k);
+  if ((n >= 0 && w->n != n) || (k >= 0 && w->k != k))
+    return fail(DLM_EINVAL, "%s: packed matrix is %d x %d, expected %d x %d", what, w->n, w->k, n, k);
+  // (the kernels count k in int, whole groups with a chunk to spare)
+  if (w->n > INT32_MAX - 1024 || w->k > INT32_MAX - 1024)
+    return fail(DLM_EUNSUPPORTED, "%s: packed matrix of %d x %d", what, w->n, w->k);
+  if (!aligned16(w->codes) || !aligned16(w->scales))
+    return fail(DLM_EINVAL, "%s: packed matrix is not 16-byte aligned", what);
+  return DLM_OK;
+}
+
+dlm_status check_dtype(int32_t dtype) {
+  if (dtype != DLM_F32 && dtype != DLM_BF16)
+    return fail(DLM_EINVAL, "dtype %d is not DLM_F32 or DLM_BF16", dtype);
+  return DLM_OK;
+}
+
+// Row plan of an operator call on a 4-bit cache: `rows` lists the requests. writes: the
+// rows' own positions are written, so each must exist and no slot may come twice.
+dlm_status make_kv_plan(const dlm_cache* c, int32_t layer, int32_t n_req, const dlm_kv_rows* rows,
+                        bool positions, bool writes, StepPlan* p) {
+  if (!c) return fail(DLM_EINVAL, "cache is NULL");
+  if (!c->mx) return fail(DLM_EUNSUPPORTED, "the cache is not a 4-bit one (dlm_kv_cache_alloc_mx)");
+  if (layer < 0 || layer >= c->model->cfg.n_layers)
+    return fail(DLM_EINVAL, "layer %d outside [0, %d)", layer, c->model->cfg.n_layers);
+  if (n_req < 1 || n_req > kMaxReq) return fail(DLM_EINVAL, "n_req %d outside [1, %d]", n_req, kMaxReq);
+  if (!rows) return fail(DLM_EINVAL, "rows is NULL");
+  memset(p, 0, sizeof *p);
+  p->n_req = n_req;
+  long total = 0;
+  for (int r = 0; r < n_req; ++r) {
+    const dlm_kv_rows& q = rows[r];
+    if (q.slot < 0 || q.slot >= c->n_slots)
+      return fail(DLM_EINVAL, "request %d: slot %d outside [0, %d)", r, q.slot, c->n_slots);
+    if (q.seq_len < 0 || q.seq_len > c->s_max)
+      return fail(DLM_ESIZE, "request %d: seq_len %d outside [0, %d]", r, q.seq_len, c->s_max);
+    if (q.n_rows < 0) return fail(DLM_EINVAL, "request %d: n_rows %d < 0", r, q.n_rows);
+    if (positions && (q.pos0 < 0 || (long)q.pos0 + q.n_rows > q.seq_len))
+      return fail(DLM_EINVAL, "request %d: positions [%d, %ld) outside [0, %d)", r, q.pos0,
+                  (long)q.pos0 + q.n_rows, q.seq_len);
+    for (int s = 0; writes && s < r; ++s)
+      if (rows[s].slot == q.slot) return fail(DLM_EINVAL, "request %d: slot %d used twice", r, q.slot);
+    ReqPlan& rp = p->r[r];
+    rp.row0 = (int)total;
+    rp.nrows = q.n_rows;
+    rp.pos0 = positions ? q.pos0 : 0;
+    rp.seq_len = q.seq_len;
+    rp.slot = q.slot;
+    total += q.n_rows;
+    if (total > DLM_MAX_REQ * DLM_MAX_SEQ)
+      return fail(DLM_ESIZE, "more than %d rows", DLM_MAX_REQ * DLM_MAX_SEQ);
+  }
+  p->n_rows = (int)total;
+  return DLM_OK;
+}
+
 dlm_status check_handles(dlm_model* m, dlm_cache* c) {
   if (!m) return fail(DLM_EINVAL, "model is NULL");
   if (!c) return fail(DLM_EINVAL, "cache is NULL");
@@ -540,13 +664,44 @@ dlm_status dlm_load_weights(const dlm_config* cfg, const dlm_weights* w, dlm_mod
   m->final_norm = w->final_norm;
   m->layers.assign(w->layers, w->layers + cfg->n_layers);
   m->es = cfg->dtype == DLM_BF16 ? 2 : 4;
-  int dev = 0, cu = 0;
-  if (hipGetDevice(&dev) == hipSuccess &&
-      hipDeviceGetAttribute(&cu, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess && cu > 0)
-    m->num_cu = cu;
-  else
-    m->num_cu = 256;
-  (void)hipGetLastError();
+  m->num_cu = device_cus();
+  *out = m;
+  return DLM_OK;
+}
+
+dlm_status dlm_load_weights_mx(const dlm_config* cfg, const dlm_weights_mx* w, dlm_model** out) {
+  g_err.clear();
+  if (!out) return fail(DLM_EINVAL, "out is NULL");
+  *out = nullptr;
+  dlm_status s = check_config(cfg);
+  if (s != DLM_OK) return s;
+  if (!w || !w->embed || !w->lm_head || !w->final_norm || !w->layers)
+    return fail(DLM_EINVAL, "weights pointer is NULL");
+  const int qd = cfg->n_q_heads * cfg->head_dim, qkv_dim = qd + 2 * cfg->n_kv_heads * cfg->head_dim;
+  for (int l = 0; l < cfg->n_layers; ++l) {
+    const dlm_layer_mx& lw = w->layers[l];
+    char what[48];
+    if (!lw.attn_norm || !lw.ffn_norm) return fail(DLM_EINVAL, "layer %d: weight pointer is NULL", l);
+    const struct { const dlm_mx* w; int n, k; const char* name; } parts[4] = {
+        {&lw.w_qkv, qkv_dim, cfg->d_model, "w_qkv"},
+        {&lw.w_o, cfg->d_model, qd, "w_o"},
+        {&lw.w_gate_up, 2 * cfg->d_ffn, cfg->d_model, "w_gate_up"},
+        {&lw.w_down, cfg->d_model, cfg->d_ffn, "w_down"}};
+    for (const auto& q : parts) {
+      snprintf(what, sizeof what, "layer %d: %s", l, q.name);
+      if ((s = check_mx(q.w, q.n, q.k, what)) != DLM_OK) return s;
+    }
+  }
+  dlm_model* m = new dlm_model();
+  m->cfg = *cfg;
+  m->embed = w->embed;
+  m->lm_head = w->lm_head;
+  m->final_norm = w->final_norm;
+  m->mx.assign(w->layers, w->layers + cfg->n_layers);
+  for (const dlm_layer_mx& lw : m->mx)
+    m->layers.push_back({lw.attn_norm, nullptr, nullptr, lw.ffn_norm, nullptr, nullptr});
+  m->es = cfg->dtype == DLM_BF16 ? 2 : 4;
+  m->num_cu = device_cus();
   *out = m;
   return DLM_OK;
 }
@@ -622,9 +777,9 @@ dlm_status dlm_workspace_bytes(const dlm_model* m, int32_t max_rows, int32_t max
   return DLM_OK;
 }
 
-dlm_status dlm_kv_cache_alloc(const dlm_model* m, int32_t n_slots, int32_t max_seq_len,
-                              void* dev_buf, size_t buf_bytes, size_t* required_bytes,
-                              dlm_cache** out) {
+static dlm_status kv_cache_alloc(const dlm_model* m, bool mx, int32_t n_slots, int32_t max_seq_len,
+                                 void* dev_buf, size_t buf_bytes, size_t* required_bytes,
+                                 dlm_cache** out) {
   g_err.clear();
   if (!m) return fail(DLM_EINVAL, "model is NULL");
   if (n_slots < 1) return fail(DLM_EINVAL, "n_slots %d < 1", n_slots);
@@ -632,8 +787,10 @@ dlm_status dlm_kv_cache_alloc(const dlm_model* m, int32_t n_slots, int32_t max_s
     return fail(DLM_ESIZE, "max_seq_len %d outside [1, %d]", max_seq_len, DLM_MAX_SEQ);
   const dlm_config& c = m->cfg;
   const int s_max = (int)align_up(max_seq_len, 64);
-  const size_t region = (size_t)n_slots * c.n_kv_heads * s_max * c.head_dim * m->es;
-  const size_t need = region * 2 * c.n_layers;
+  const size_t vecs = (size_t)n_slots * c.n_kv_heads * s_max;
+  const size_t region = mx ? vecs * (c.head_dim / 2) : vecs * c.head_dim * m->es;
+  const size_t scale_region = mx ? align_up(vecs * (c.head_dim / kMxGroup), 256) : 0;
+  const size_t need = (region + scale_region) * 2 * c.n_layers;
   if (required_bytes) *required_bytes = need;
   if (!dev_buf) {
     if (out) *out = nullptr;
@@ -650,9 +807,23 @@ dlm_status dlm_kv_cache_alloc(const dlm_model* m, int32_t n_slots, int32_t max_s
   k->s_max = s_max;
   k->base = reinterpret_cast<char*>(dev_buf);
   k->region = region;
+  k->mx = mx;
+  k->scale_region = scale_region;
   k->slots.assign(n_slots, SlotState{});
   *out = k;
   return DLM_OK;
+}
+
+dlm_status dlm_kv_cache_alloc(const dlm_model* m, int32_t n_slots, int32_t max_seq_len,
+                              void* dev_buf, size_t buf_bytes, size_t* required_bytes,
+                              dlm_cache** out) {
+  return kv_cache_alloc(m, false, n_slots, max_seq_len, dev_buf, buf_bytes, required_bytes, out);
+}
+
+dlm_status dlm_kv_cache_alloc_mx(const dlm_model* m, int32_t n_slots, int32_t max_seq_len,
+                                 void* dev_buf, size_t buf_bytes, size_t* required_bytes,
+                                 dlm_cache** out) {
+  return kv_cache_alloc(m, true, n_slots, max_seq_len, dev_buf, buf_bytes, required_bytes, out);
 }
 
 void dlm_cache_destroy(dlm_cache* c) { delete c; }
@@ -897,6 +1068,198 @@ dlm_status dlm_debug_gemm(int32_t cfg, int32_t epilogue, int32_t sub, int32_t n_
   if (e == hipErrorInvalidValue)
     return fail(DLM_EINVAL, "GEMM configuration %d rejects this launch", cfg);
   if (e != hipSuccess) return fail(DLM_EHIP, "GEMM launch: %s", hipGetErrorString(e));
+  return DLM_OK;
+}
+
+// ---- operators on 4-bit operands ----
+
+dlm_status dlm_mx_bytes(int32_t n, int32_t k, size_t* codes_bytes, size_t* scales_bytes) {
+  g_err.clear();
+  if (n < 1 || k < 1) return fail(DLM_EINVAL, "packed matrix of %d x %d", n, k);
+  const size_t groups = ((size_t)k + kMxGroup - 1) / kMxGroup;
+  if (codes_bytes) *codes_bytes = (size_t)n * groups * 16;
+  if (scales_bytes) *scales_bytes = (size_t)n * align_up(groups, 16);
+  return DLM_OK;
+}
+
+dlm_status dlm_mx_pack(int32_t dtype, const void* w, int64_t ldw, const dlm_mx* out, void* stream) {
+  g_err.clear();
+  dlm_status s = check_dtype(dtype);
+  if (s != DLM_OK || (s = check_mx(out, -1, -1, "out")) != DLM_OK) return s;
+  if (!w) return fail(DLM_EINVAL, "w is NULL");
+  if (ldw < out->k) return fail(DLM_EINVAL, "row stride %lld < %d", (long long)ldw, out->k);
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  if (dtype == DLM_BF16)
+    HIPCHECK(mx_pack<bf16>(reinterpret_cast<const bf16*>(w), ldw, out->k, mx_view(*out), st));
+  else
+    HIPCHECK(mx_pack<float>(reinterpret_cast<const float*>(w), ldw, out->k, mx_view(*out), st));
+  return DLM_OK;
+}
+
+dlm_status dlm_mx_unpack(const dlm_mx* w, int32_t dtype, void* out, int64_t ldo, void* stream) {
+  g_err.clear();
+  dlm_status s = check_dtype(dtype);
+  if (s != DLM_OK || (s = check_mx(w, -1, -1, "w")) != DLM_OK) return s;
+  if (!out) return fail(DLM_EINVAL, "out is NULL");
+  if (ldo < w->k) return fail(DLM_EINVAL, "row stride %lld < %d", (long long)ldo, w->k);
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  if (dtype == DLM_BF16)
+    HIPCHECK(mx_unpack<bf16>(mx_view(*w), w->k, reinterpret_cast<bf16*>(out), ldo, st));
+  else
+    HIPCHECK(mx_unpack<float>(mx_view(*w), w->k, reinterpret_cast<float*>(out), ldo, st));
+  return DLM_OK;
+}
+
+static dlm_status check_linear(int32_t dtype, int32_t m_rows, const dlm_mx* w, int32_t epilogue) {
+  dlm_status s = check_dtype(dtype);
+  if (s != DLM_OK || (s = check_mx(w, -1, -1, "w")) != DLM_OK) return s;
+  if (m_rows < 0 || m_rows > DLM_MAX_REQ * DLM_MAX_SEQ)
+    return fail(DLM_EINVAL, "m_rows %d outside [0, %d]", m_rows, DLM_MAX_REQ * DLM_MAX_SEQ);
+  if (epilogue < DLM_MX_STORE || epilogue > DLM_MX_SWIGLU) return fail(DLM_EINVAL, "epilogue %d", epilogue);
+  if (epilogue == DLM_MX_SWIGLU && w->n % 2 != 0)
+    return fail(DLM_EINVAL, "odd number of rows %d for the SwiGLU epilogue", w->n);
+  return DLM_OK;
+}
+
+dlm_status dlm_mx_linear_workspace(int32_t dtype, int32_t m_rows, const dlm_mx* w, int32_t epilogue,
+                                   size_t* out_bytes) {
+  g_err.clear();
+  dlm_status s = check_linear(dtype, m_rows, w, epilogue);
+  if (s != DLM_OK) return s;
+  if (!out_bytes) return fail(DLM_EINVAL, "out_bytes is NULL");
+  // whatever the address and the row stride of x turn out to be
+  size_t need = 0;
+  for (int al = 0; al < 2; ++al)
+    need = std::max(need, mx_plan(dtype == DLM_BF16 ? 2 : 4, m_rows, w->n, w->k,
+                                  epilogue == DLM_MX_SWIGLU, al != 0, device_cus()).scratch);
+  *out_bytes = need;
+  return DLM_OK;
+}
+
+dlm_status dlm_mx_linear(int32_t dtype, const void* x, int64_t ldx, int32_t m_rows, const dlm_mx* w,
+                         int32_t epilogue, void* y, int64_t ldy, void* workspace, size_t ws_bytes,
+                         void* stream) {
+  g_err.clear();
+  dlm_status s = check_linear(dtype, m_rows, w, epilogue);
+  if (s != DLM_OK) return s;
+  if (m_rows == 0) return DLM_OK;
+  if (!x || !y) return fail(DLM_EINVAL, "NULL buffer");
+  const bool swiglu = epilogue == DLM_MX_SWIGLU;
+  if (ldx < w->k || ldy < (swiglu ? w->n / 2 : w->n))
+    return fail(DLM_EINVAL, "row strides %lld, %lld too small for %d inputs and %d outputs",
+                (long long)ldx, (long long)ldy, w->k, swiglu ? w->n / 2 : w->n);
+  const int es = dtype == DLM_BF16 ? 2 : 4;
+  const bool al = aligned16(x) && ldx * es % 16 == 0 && w->k * (long)es % 16 == 0 && aligned16(y) &&
+                  ldy % 8 == 0 && ldx < INT32_MAX && ldy < INT32_MAX;
+  const MxPlan plan = mx_plan(es, m_rows, w->n, w->k, swiglu, al, device_cus());
+  if (plan.scratch) {
+    if (!workspace) return fail(DLM_EINVAL, "workspace is NULL");
+    if (reinterpret_cast<uintptr_t>(workspace) % 256 != 0)
+      return fail(DLM_EINVAL, "workspace is not 256-byte aligned");
+    if (ws_bytes < plan.scratch)
+      return fail(DLM_ESIZE, "workspace of %zu bytes; needs %zu", ws_bytes, plan.scratch);
+  }
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  if (dtype == DLM_BF16)
+    HIPCHECK(mx_matmul<bf16>(plan, reinterpret_cast<const bf16*>(x), ldx, m_rows, mx_view(*w), w->k,
+                             epilogue, y, ldy, workspace, st));
+  else
+    HIPCHECK(mx_matmul<float>(plan, reinterpret_cast<const float*>(x), ldx, m_rows, mx_view(*w), w->k,
+                              epilogue, y, ldy, workspace, st));
+  return DLM_OK;
+}
+
+dlm_status dlm_mx_kv_append(dlm_cache* c, int32_t layer, int32_t n_req, const dlm_kv_rows* rows,
+                            const float* qkv, int32_t splits, const float* rot, void* q_out,
+                            void* stream) {
+  g_err.clear();
+  StepPlan p;
+  dlm_status s = make_kv_plan(c, layer, n_req, rows, true, true, &p);
+  if (s != DLM_OK) return s;
+  if (splits < 1) return fail(DLM_EINVAL, "splits %d < 1", splits);
+  if (p.n_rows == 0) return DLM_OK;
+  if (!qkv || !rot || !q_out) return fail(DLM_EINVAL, "NULL buffer");
+  if (!aligned16(qkv) || !aligned16(rot) || !aligned16(q_out))
+    return fail(DLM_EINVAL, "a buffer is not 16-byte aligned");
+  const dlm_config& cf = c->model->cfg;
+  const long stride = (long)p.n_rows * (cf.n_q_heads + 2 * cf.n_kv_heads) * cf.head_dim;
+  const float2* cs = reinterpret_cast<const float2*>(rot);
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  if (cf.dtype == DLM_BF16)
+    HIPCHECK(mx_kv_append<bf16>(p, qkv, splits, stride, cs, cf.n_q_heads, cf.n_kv_heads, cf.head_dim,
+                                reinterpret_cast<bf16*>(q_out), c->mx_layer(layer), st));
+  else
+    HIPCHECK(mx_kv_append<float>(p, qkv, splits, stride, cs, cf.n_q_heads, cf.n_kv_heads, cf.head_dim,
+                                 reinterpret_cast<float*>(q_out), c->mx_layer(layer), st));
+  return DLM_OK;
+}
+
+dlm_status dlm_mx_kv_read(const dlm_cache* c, int32_t layer, int32_t n_req, const dlm_kv_rows* rows,
+                          void* k_out, void* v_out, void* stream) {
+  g_err.clear();
+  StepPlan p;
+  dlm_status s = make_kv_plan(c, layer, n_req, rows, true, false, &p);
+  if (s != DLM_OK) return s;
+  if (p.n_rows == 0) return DLM_OK;
+  if (!k_out || !v_out) return fail(DLM_EINVAL, "NULL buffer");
+  if (!aligned16(k_out) || !aligned16(v_out)) return fail(DLM_EINVAL, "a buffer is not 16-byte aligned");
+  const dlm_config& cf = c->model->cfg;
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  if (cf.dtype == DLM_BF16)
+    HIPCHECK(mx_kv_read<bf16>(p, cf.n_kv_heads, cf.head_dim, c->mx_layer(layer),
+                              reinterpret_cast<bf16*>(k_out), reinterpret_cast<bf16*>(v_out), st));
+  else
+    HIPCHECK(mx_kv_read<float>(p, cf.n_kv_heads, cf.head_dim, c->mx_layer(layer),
+                               reinterpret_cast<float*>(k_out), reinterpret_cast<float*>(v_out), st));
+  return DLM_OK;
+}
+
+dlm_status dlm_mx_kv_attention_workspace(const dlm_cache* c, int32_t n_req, const dlm_kv_rows* rows,
+                                         size_t* out_bytes) {
+  g_err.clear();
+  StepPlan p;
+  dlm_status s = make_kv_plan(c, 0, n_req, rows, false, false, &p);
+  if (s != DLM_OK) return s;
+  if (!out_bytes) return fail(DLM_EINVAL, "out_bytes is NULL");
+  const dlm_model* m = c->model;
+  const dlm_config& cf = m->cfg;
+  *out_bytes = mx_attention_scratch(
+      p.n_rows, cf.n_q_heads, cf.head_dim,
+      mx_attention_splits(p, cf.n_q_heads, cf.n_kv_heads, cf.head_dim, m->es, SIZE_MAX, m->num_cu));
+  return DLM_OK;
+}
+
+dlm_status dlm_mx_kv_attention(const dlm_cache* c, int32_t layer, int32_t n_req,
+                               const dlm_kv_rows* rows, const void* q, void* out, void* workspace,
+                               size_t ws_bytes, void* stream) {
+  g_err.clear();
+  StepPlan p;
+  dlm_status s = make_kv_plan(c, layer, n_req, rows, false, false, &p);
+  if (s != DLM_OK) return s;
+  if (p.n_rows == 0) return DLM_OK;
+  if (!q || !out) return fail(DLM_EINVAL, "NULL buffer");
+  if (!aligned16(q) || !aligned16(out)) return fail(DLM_EINVAL, "a buffer is not 16-byte aligned");
+  const dlm_model* m = c->model;
+  const dlm_config& cf = m->cfg;
+  const int splits =
+      mx_attention_splits(p, cf.n_q_heads, cf.n_kv_heads, cf.head_dim, m->es, SIZE_MAX, m->num_cu);
+  const size_t need = mx_attention_scratch(p.n_rows, cf.n_q_heads, cf.head_dim, splits);
+  if (need) {
+    if (!workspace) return fail(DLM_EINVAL, "workspace is NULL");
+    if (reinterpret_cast<uintptr_t>(workspace) % 256 != 0)
+      return fail(DLM_EINVAL, "workspace is not 256-byte aligned");
+    if (ws_bytes < need) return fail(DLM_ESIZE, "workspace of %zu bytes; needs %zu", ws_bytes, need);
+  }
+  float* scratch = reinterpret_cast<float*>(workspace);
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  if (cf.dtype == DLM_BF16)
+    HIPCHECK(mx_attention<bf16>(p, reinterpret_cast<const bf16*>(q), c->mx_layer(layer), cf.n_q_heads,
+                                cf.n_kv_heads, cf.head_dim, reinterpret_cast<bf16*>(out), splits, scratch,
+                                st));
+  else
+    HIPCHECK(mx_attention<float>(p, reinterpret_cast<const float*>(q), c->mx_layer(layer), cf.n_q_heads,
+                                 cf.n_kv_heads, cf.head_dim, reinterpret_cast<float*>(out), splits, scratch,
+                                 st));
   return DLM_OK;
 }
 

@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, c_float, c_int32, c_size_t, c_uint8, c_void_p
+from ctypes import POINTER, c_float, c_int32, c_int64, c_size_t, c_uint8, c_void_p
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libdlm.so")
@@ -21,6 +21,9 @@ DLM_MAX_BLOCK, DLM_MAX_REQ, DLM_MAX_SEQ = 64, 64, 8192
 DLM_NSTATS = 8
 DLM_SCRATCH_BYTES = 128 << 20
 DLM_REQ_REFRESH = 1
+DLM_MX_GROUP = 32
+DLM_MX_STORE, DLM_MX_ADD, DLM_MX_SWIGLU = 0, 1, 2
+MX_EPILOGUES = {"store": DLM_MX_STORE, "add": DLM_MX_ADD, "swiglu": DLM_MX_SWIGLU}
 MODES = {"none": DLM_CACHE_NONE, "prefix": DLM_CACHE_PREFIX, "dual": DLM_CACHE_DUAL}
 
 EXPORTS = ["dlm_load_weights", "dlm_model_destroy", "dlm_workspace_bytes",
@@ -29,7 +32,10 @@ EXPORTS = ["dlm_load_weights", "dlm_model_destroy", "dlm_workspace_bytes",
            "dlm_debug_logits", "dlm_debug_trace", "dlm_debug_gemm_info", "dlm_debug_gemm",
            "dlm_debug_gemm_plan", "dlm_debug_attention_plan",
            "dlm_head_confidence", "dlm_profile_enable", "dlm_profile_read",
-           "dlm_profile_sample", "dlm_ceiling_mfma", "dlm_ceiling_copy", "dlm_last_error"]
+           "dlm_profile_sample", "dlm_ceiling_mfma", "dlm_ceiling_copy", "dlm_last_error",
+           "dlm_mx_bytes", "dlm_mx_pack", "dlm_mx_unpack", "dlm_mx_linear_workspace",
+           "dlm_mx_linear", "dlm_load_weights_mx", "dlm_kv_cache_alloc_mx", "dlm_mx_kv_append",
+           "dlm_mx_kv_read", "dlm_mx_kv_attention_workspace", "dlm_mx_kv_attention"]
 
 
 class DlmConfig(ctypes.Structure):
@@ -47,6 +53,24 @@ class DlmLayerWeights(ctypes.Structure):
 class DlmWeights(ctypes.Structure):
     _fields_ = [("embed", c_void_p), ("lm_head", c_void_p), ("final_norm", c_void_p),
                 ("layers", POINTER(DlmLayerWeights))]
+
+
+class DlmMx(ctypes.Structure):
+    _fields_ = [("codes", c_void_p), ("scales", c_void_p), ("n", c_int32), ("k", c_int32)]
+
+
+class DlmLayerMx(ctypes.Structure):
+    _fields_ = [("attn_norm", c_void_p), ("w_qkv", DlmMx), ("w_o", DlmMx),
+                ("ffn_norm", c_void_p), ("w_gate_up", DlmMx), ("w_down", DlmMx)]
+
+
+class DlmWeightsMx(ctypes.Structure):
+    _fields_ = [("embed", c_void_p), ("lm_head", c_void_p), ("final_norm", c_void_p),
+                ("layers", POINTER(DlmLayerMx))]
+
+
+class DlmKvRows(ctypes.Structure):
+    _fields_ = [("slot", c_int32), ("seq_len", c_int32), ("pos0", c_int32), ("n_rows", c_int32)]
 
 
 class DlmReq(ctypes.Structure):
@@ -137,6 +161,24 @@ def lib():
         L.dlm_ceiling_mfma.argtypes = [c_int32, c_int32, c_void_p, POINTER(ctypes.c_double),
                                        c_void_p]
         L.dlm_ceiling_copy.argtypes = [c_void_p, c_void_p, c_size_t, c_void_p]
+        L.dlm_mx_bytes.argtypes = [c_int32, c_int32, POINTER(c_size_t), POINTER(c_size_t)]
+        L.dlm_mx_pack.argtypes = [c_int32, c_void_p, c_int64, POINTER(DlmMx), c_void_p]
+        L.dlm_mx_unpack.argtypes = [POINTER(DlmMx), c_int32, c_void_p, c_int64, c_void_p]
+        L.dlm_mx_linear_workspace.argtypes = [c_int32, c_int32, POINTER(DlmMx), c_int32,
+                                              POINTER(c_size_t)]
+        L.dlm_mx_linear.argtypes = [c_int32, c_void_p, c_int64, c_int32, POINTER(DlmMx), c_int32,
+                                    c_void_p, c_int64, c_void_p, c_size_t, c_void_p]
+        L.dlm_load_weights_mx.argtypes = [POINTER(DlmConfig), POINTER(DlmWeightsMx),
+                                          POINTER(c_void_p)]
+        L.dlm_kv_cache_alloc_mx.argtypes = L.dlm_kv_cache_alloc.argtypes
+        L.dlm_mx_kv_append.argtypes = [c_void_p, c_int32, c_int32, POINTER(DlmKvRows), c_void_p,
+                                       c_int32, c_void_p, c_void_p, c_void_p]
+        L.dlm_mx_kv_read.argtypes = [c_void_p, c_int32, c_int32, POINTER(DlmKvRows), c_void_p,
+                                     c_void_p, c_void_p]
+        L.dlm_mx_kv_attention_workspace.argtypes = [c_void_p, c_int32, POINTER(DlmKvRows),
+                                                    POINTER(c_size_t)]
+        L.dlm_mx_kv_attention.argtypes = [c_void_p, c_int32, c_int32, POINTER(DlmKvRows),
+                                          c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
         L.dlm_last_error.argtypes = []
         L.dlm_last_error.restype = ctypes.c_char_p
         for name in ["dlm_load_weights", "dlm_workspace_bytes", "dlm_kv_cache_alloc",
@@ -145,7 +187,10 @@ def lib():
                      "dlm_debug_logits", "dlm_debug_trace", "dlm_head_confidence",
                      "dlm_debug_gemm_info", "dlm_debug_gemm", "dlm_debug_gemm_plan",
                      "dlm_debug_attention_plan", "dlm_profile_enable",
-                     "dlm_profile_read", "dlm_profile_sample"]:
+                     "dlm_profile_read", "dlm_profile_sample", "dlm_mx_bytes", "dlm_mx_pack",
+                     "dlm_mx_unpack", "dlm_mx_linear_workspace", "dlm_mx_linear",
+                     "dlm_load_weights_mx", "dlm_kv_cache_alloc_mx", "dlm_mx_kv_append",
+                     "dlm_mx_kv_read", "dlm_mx_kv_attention_workspace", "dlm_mx_kv_attention"]:
             getattr(L, name).restype = c_int32
         _lib = L
     return _lib
@@ -318,6 +363,170 @@ def debug_gemm(cfg: int, epilogue: int, a, b, c, sub: int = 0, n_tail: int = 0,
         raise ValueError(f"c has shape {tuple(c.shape)}, expected {want}")
     check(lib().dlm_debug_gemm(cfg, epilogue, sub, n_tail, group_m, splits, _ptr(a), _ptr(b),
                                _ptr(c), M, N, K, _stream(stream)))
+
+
+# ------------------------------------------------- 4-bit operands
+def _dtype_id(dtype) -> int:
+    """dlm_dtype of a torch floating type."""
+    name = str(dtype)
+    if name == "torch.bfloat16":
+        return DLM_BF16
+    if name == "torch.float32":
+        return DLM_F32
+    raise ValueError(f"{name}: bfloat16 or float32 expected")
+
+
+def _rows_of(name, t, shape, dtype=None):
+    """Row stride of a 2-d device tensor of the given shape (and dtype) with contiguous rows."""
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{name} is {t.dtype}, expected {dtype}")
+    if not t.is_cuda:
+        raise ValueError(f"{name} is not in device memory")
+    rows, cols = shape
+    ld = t.stride(0) if rows > 1 else max(cols, t.stride(0))
+    if (cols > 1 and t.stride(1) != 1) or ld < cols:
+        raise ValueError(f"{name} has strides {t.stride()}: contiguous, disjoint rows expected")
+    return ld
+
+
+def _flat(name, t, shape, dtype):
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+        raise ValueError(f"{name} is {t.dtype} {tuple(t.shape)}, expected {dtype} {tuple(shape)}")
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name} is not a contiguous device tensor")
+
+
+def _on(stream, *tensors):
+    """The stream argument of a call on these tensors: the given one, or the current stream of
+    their device (which becomes the current device of the call)."""
+    import torch
+    dev = tensors[0].device
+    for t in tensors[1:]:
+        if t.device != dev:
+            raise ValueError(f"tensors on {dev} and {t.device}")
+    if dev.index != torch.cuda.current_device():
+        raise ValueError(f"tensors on {dev}, but the current device is {torch.cuda.current_device()}")
+    return c_void_p(stream if stream is not None else
+                    torch.cuda.current_stream(dev).cuda_stream)
+
+
+def mx_bytes(n: int, k: int):
+    """(bytes of the codes, bytes of the scales) of a packed [n, k] matrix."""
+    c, s = c_size_t(), c_size_t()
+    check(lib().dlm_mx_bytes(n, k, ctypes.byref(c), ctypes.byref(s)))
+    return c.value, s.value
+
+
+def make_mx(codes, scales, n: int, k: int) -> DlmMx:
+    """A packed [n, k] matrix over two contiguous uint8 device tensors."""
+    for name, t, need in zip(("codes", "scales"), (codes, scales), mx_bytes(n, k)):
+        if str(t.dtype) != "torch.uint8" or not t.is_contiguous() or not t.is_cuda:
+            raise ValueError(f"{name}: contiguous uint8 device tensor expected")
+        if t.numel() < need:
+            raise ValueError(f"{name} holds {t.numel()} bytes; a {n} x {k} matrix needs {need}")
+    if codes.device != scales.device:
+        raise ValueError(f"codes on {codes.device}, scales on {scales.device}")
+    q = DlmMx(codes.data_ptr(), scales.data_ptr(), n, k)
+    q._keep = (codes, scales)
+    return q
+
+
+def mx_pack(w, q: DlmMx, stream=None):
+    """Pack the [n, k] tensor w (bf16 or fp32, contiguous rows) into q's buffers."""
+    ld = _rows_of("w", w, (q.n, q.k))
+    check(lib().dlm_mx_pack(_dtype_id(w.dtype), _ptr(w), ld, ctypes.byref(q),
+                            _on(stream, w, q._keep[0])))
+
+
+def mx_unpack(q: DlmMx, out, stream=None):
+    """The packed values, in out's dtype."""
+    ld = _rows_of("out", out, (q.n, q.k))
+    check(lib().dlm_mx_unpack(ctypes.byref(q), _dtype_id(out.dtype), _ptr(out), ld,
+                              _on(stream, out, q._keep[0])))
+
+
+def mx_linear_workspace(dtype, m_rows: int, q: DlmMx, epilogue: int = DLM_MX_STORE) -> int:
+    out = c_size_t()
+    check(lib().dlm_mx_linear_workspace(_dtype_id(dtype), m_rows, ctypes.byref(q), epilogue,
+                                        ctypes.byref(out)))
+    return out.value
+
+
+def mx_linear(x, q: DlmMx, y, epilogue: int = DLM_MX_STORE, workspace=None, stream=None):
+    """y = x @ values.T (fp32), y += x @ values.T (fp32), or silu(gate) * up in x's
+    dtype; workspace: at least mx_linear_workspace bytes, or None where that is 0."""
+    import torch
+    m = x.shape[0]
+    ldx = _rows_of("x", x, (m, q.k))
+    swiglu = epilogue == DLM_MX_SWIGLU
+    ldy = _rows_of("y", y, (m, q.n // 2 if swiglu else q.n), x.dtype if swiglu else torch.float32)
+    ws, n = (None, 0) if workspace is None else (workspace, workspace.numel() *
+                                                 workspace.element_size())
+    check(lib().dlm_mx_linear(_dtype_id(x.dtype), _ptr(x), ldx, m, ctypes.byref(q), epilogue,
+                              _ptr(y), ldy, _ptr(ws), n,
+                              _on(stream, x, y, q._keep[0], *(() if ws is None else (ws,)))))
+
+
+def load_weights_mx(cfg: DlmConfig, weights: DlmWeightsMx) -> c_void_p:
+    h = c_void_p()
+    check(lib().dlm_load_weights_mx(ctypes.byref(cfg), ctypes.byref(weights), ctypes.byref(h)))
+    return h
+
+
+def kv_cache_alloc_mx(model, n_slots: int, max_seq_len: int, dev_buf=None, buf_bytes: int = 0):
+    """kv_cache_alloc of a cache in 4 bits."""
+    req = c_size_t()
+    h = c_void_p()
+    check(lib().dlm_kv_cache_alloc_mx(model, n_slots, max_seq_len, _ptr(dev_buf), buf_bytes,
+                                      ctypes.byref(req), ctypes.byref(h)))
+    return (h if dev_buf is not None else None), req.value
+
+
+def make_kv_rows(rows):
+    """[(slot, seq_len, pos0, n_rows)] as the argument of the mx_kv calls."""
+    return (DlmKvRows * len(rows))(*[DlmKvRows(*r) for r in rows])
+
+
+def mx_kv_append(cache, layer: int, rows, qkv, rot, q_out, stream=None):
+    """qkv fp32 [splits, N, D] or [N, D], rot fp32 [N, head_dim / 2, 2], q_out [N, n_q_heads head_dim]."""
+    import torch
+    n = sum(r.n_rows for r in rows)
+    splits = qkv.shape[0] if qkv.dim() == 3 else 1
+    for name, t in (("qkv", qkv), ("rot", rot)):
+        _flat(name, t, t.shape, torch.float32)
+    if qkv.shape[-2] != n or rot.shape[0] != n:
+        raise ValueError(f"qkv {tuple(qkv.shape)}, rot {tuple(rot.shape)}: the requests have {n} rows")
+    _flat("q_out", q_out, (n, q_out.shape[-1]), q_out.dtype)
+    check(lib().dlm_mx_kv_append(cache, layer, len(rows), rows, _ptr(qkv), splits, _ptr(rot),
+                                 _ptr(q_out), _on(stream, qkv, rot, q_out)))
+
+
+def mx_kv_read(cache, layer: int, rows, k_out, v_out, stream=None):
+    """The stored keys and values of the rows' positions, [N, n_kv_heads head_dim]."""
+    n = sum(r.n_rows for r in rows)
+    for name, t in (("k_out", k_out), ("v_out", v_out)):
+        _flat(name, t, (n, t.shape[-1]), k_out.dtype)
+    check(lib().dlm_mx_kv_read(cache, layer, len(rows), rows, _ptr(k_out), _ptr(v_out),
+                               _on(stream, k_out, v_out)))
+
+
+def mx_kv_attention_workspace(cache, rows) -> int:
+    out = c_size_t()
+    check(lib().dlm_mx_kv_attention_workspace(cache, len(rows), rows, ctypes.byref(out)))
+    return out.value
+
+
+def mx_kv_attention(cache, layer: int, rows, q, out, workspace=None, stream=None):
+    """out = attention of q over the 4-bit cache; both [N, n_q_heads head_dim]."""
+    n = sum(r.n_rows for r in rows)
+    _flat("q", q, (n, q.shape[-1]), q.dtype)
+    _flat("out", out, q.shape, q.dtype)
+    ws, size = (None, 0) if workspace is None else (workspace, workspace.numel() *
+                                                    workspace.element_size())
+    check(lib().dlm_mx_kv_attention(cache, layer, len(rows), rows, _ptr(q), _ptr(out), _ptr(ws), size,
+                                    _on(stream, q, out, *(() if ws is None else (ws,)))))
 
 
 def profile_enable(model, on: bool, only_class: str | None = None):

@@ -50,31 +50,59 @@ class ModelShape:
                           cfg.rope_theta, cfg.vocab - 1)
 
 
+def pack_layer(layer: dict) -> dict:
+    """A layer's weights with its projections packed into 4 bits (those that are not yet)."""
+    out = dict(layer)
+    for name in ("w_qkv", "w_o", "w_gate_up", "w_down"):
+        w = layer[name]
+        if isinstance(w, dlm.DlmMx):
+            continue
+        codes, scales = (torch.empty(b, dtype=torch.uint8, device=w.device)
+                         for b in dlm.mx_bytes(*w.shape))
+        out[name] = dlm.make_mx(codes, scales, *w.shape)
+        dlm.mx_pack(w, out[name])
+    return out
+
+
 class DeviceModel:
     """Caller-owned device weights plus the library's model handle.
 
     ``tensors``: embed, lm_head, final_norm and ``layers`` (list of dicts with
     attn_norm, w_qkv, w_o, ffn_norm, w_gate_up, w_down), torch CUDA tensors in
-    the layouts of include/dlm.h."""
+    the layouts of include/dlm.h.
 
-    def __init__(self, shape: ModelShape, tensors: dict, inv_tau: float):
+    packed: the layers' projections are held in 4 bits (dlm_load_weights_mx).
+    Each is then either a tensor, packed here and not kept, or a dlm.DlmMx that
+    is packed already. ``self.tensors`` holds the packed ones in their place."""
+
+    def __init__(self, shape: ModelShape, tensors: dict, inv_tau: float, packed: bool = False):
         self.shape = shape
-        self.tensors = tensors
+        self.packed = packed
         self.inv_tau = float(inv_tau)
-        self._layer_arr = (dlm.DlmLayerWeights * shape.n_layers)(*[
-            dlm.DlmLayerWeights(l["attn_norm"].data_ptr(), l["w_qkv"].data_ptr(),
-                                l["w_o"].data_ptr(), l["ffn_norm"].data_ptr(),
-                                l["w_gate_up"].data_ptr(), l["w_down"].data_ptr())
-            for l in tensors["layers"]])
-        self.weights = dlm.DlmWeights(tensors["embed"].data_ptr(), tensors["lm_head"].data_ptr(),
-                                      tensors["final_norm"].data_ptr(),
-                                      self._layer_arr)
+        if packed:
+            tensors = dict(tensors, layers=[pack_layer(l) for l in tensors["layers"]])
+        self.tensors = tensors
+        if packed:
+            self._layer_arr = (dlm.DlmLayerMx * shape.n_layers)(*[
+                dlm.DlmLayerMx(l["attn_norm"].data_ptr(), l["w_qkv"], l["w_o"],
+                               l["ffn_norm"].data_ptr(), l["w_gate_up"], l["w_down"])
+                for l in tensors["layers"]])
+        else:
+            self._layer_arr = (dlm.DlmLayerWeights * shape.n_layers)(*[
+                dlm.DlmLayerWeights(l["attn_norm"].data_ptr(), l["w_qkv"].data_ptr(),
+                                    l["w_o"].data_ptr(), l["ffn_norm"].data_ptr(),
+                                    l["w_gate_up"].data_ptr(), l["w_down"].data_ptr())
+                for l in tensors["layers"]])
+        self.weights = (dlm.DlmWeightsMx if packed else dlm.DlmWeights)(
+            tensors["embed"].data_ptr(), tensors["lm_head"].data_ptr(),
+            tensors["final_norm"].data_ptr(), self._layer_arr)
         mask_id = shape.vocab - 1 if shape.mask_id is None else shape.mask_id
         self.config = dlm.DlmConfig(shape.n_layers, shape.d_model, shape.n_q_heads,
                                     shape.n_kv_heads, shape.head_dim, shape.d_ffn, shape.vocab,
                                     mask_id, shape.rms_eps, shape.rope_theta, self.inv_tau,
                                     dlm.DLM_BF16 if shape.dtype == "bf16" else dlm.DLM_F32)
-        self.handle = dlm.load_weights(self.config, self.weights)
+        load = dlm.load_weights_mx if packed else dlm.load_weights
+        self.handle = load(self.config, self.weights)
 
     def close(self):
         if self.handle:
@@ -136,20 +164,24 @@ def advance(r: Request, unmasked: int) -> None:
 
 
 class Engine:
-    """Slots, workspace and packed token/mask buffers for a fixed set of slots."""
+    """Slots, workspace and packed token/mask buffers for a fixed set of slots.
+
+    packed_kv: the key/value cache is held in 4 bits (dlm_kv_cache_alloc_mx)."""
 
     def __init__(self, model: DeviceModel, n_slots: int, max_seq_len: int, mode: str,
-                 max_rows: Optional[int] = None, device="cuda:0", stats: bool = False):
+                 max_rows: Optional[int] = None, device="cuda:0", stats: bool = False,
+                 packed_kv: bool = False):
         self.model = model
         self.mode = mode
         self.mode_id = dlm.MODES[mode]
         self.device = torch.device(device)
         self.n_slots = n_slots
         self.max_seq_len = max_seq_len
-        _, need = dlm.kv_cache_alloc(model.handle, n_slots, max_seq_len)
+        self.packed_kv = packed_kv
+        alloc = dlm.kv_cache_alloc_mx if packed_kv else dlm.kv_cache_alloc
+        _, need = alloc(model.handle, n_slots, max_seq_len)
         self.cache_buf = torch.empty(need, dtype=torch.uint8, device=self.device)
-        self.cache, _ = dlm.kv_cache_alloc(model.handle, n_slots, max_seq_len, self.cache_buf,
-                                           need)
+        self.cache, _ = alloc(model.handle, n_slots, max_seq_len, self.cache_buf, need)
         if max_rows is None:
             max_rows = n_slots * max_seq_len
         self.max_rows = max_rows
@@ -319,9 +351,15 @@ class Engine:
         [length, n_kv_heads, head_dim] float tensors on the host, read from the
         cache layout of dlm_kv_cache_alloc (per layer a key region
         [slot][kv_head][pos][head_dim] then a value region
-        [slot][kv_head][head_dim][pos], slots of max_seq_len rounded up to 64)."""
+        [slot][kv_head][head_dim][pos], slots of max_seq_len rounded up to 64), or
+        as dlm_mx_kv_read gives them from a packed cache."""
         sh = self.model.shape
         dt = sh.torch_dtype
+        if self.packed_kv:
+            k, v = (torch.empty(length, sh.n_kv_heads * sh.head_dim, dtype=dt, device=self.device)
+                    for _ in range(2))
+            dlm.mx_kv_read(self.cache, layer, dlm.make_kv_rows([(slot, length, 0, length)]), k, v)
+            return tuple(x.view(length, sh.n_kv_heads, sh.head_dim).float().cpu() for x in (k, v))
         s_max = (self.max_seq_len + 63) // 64 * 64
         per = self.n_slots * sh.n_kv_heads * s_max * sh.head_dim
         region = self.cache_buf.view(dt)

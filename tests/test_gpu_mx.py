@@ -1,0 +1,440 @@
+"""4-bit operators against their 64-bit definitions (mx_reference)."""
+import dataclasses
+import math
+
+import pytest
+import torch
+
+import mx_reference as ref
+from paper_2606_29094_amd import dlm, engine
+
+pytestmark = pytest.mark.gpu
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+def _randn(*shape, seed=0, dtype=F32, std=1.0):
+    return (torch.randn(*shape, generator=torch.Generator().manual_seed(seed)) * std).to(dtype)
+
+
+def _packed(gpu, n, k, seed=0, w=None):
+    """A packed [n, k] matrix on the GPU and its values (CPU, 64 bits)."""
+    codes, scales = ref.pack(_randn(n, k, seed=seed) if w is None else w)
+    return dlm.make_mx(codes.to(gpu), scales.to(gpu), n, k), ref.values(codes, scales, k)
+
+
+# ------------------------------------------------------------ pack, unpack
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n,k,pad", [(1, 1, 0), (3, 31, 0), (5, 33, 7), (16, 512, 0), (17, 688, 8),
+                                     (300, 1031, 1)])
+def test_pack_unpack(gpu, n, k, pad, dtype):
+    big = _randn(n, k + pad, seed=n + k) * torch.logspace(-40, 38, n)[:, None]
+    w = big.to(dtype)[:, :k]
+    codes, scales = ref.pack(w)
+    c = torch.full_like(codes, 0xAB).to(gpu)
+    s = torch.full_like(scales, 0xCD).to(gpu)
+    q = dlm.make_mx(c, s, n, k)
+    dlm.mx_pack(big.to(dtype).to(gpu)[:, :k], q)
+    assert torch.equal(s.cpu(), scales)
+    assert torch.equal(c.cpu(), codes)
+    out = torch.full((n, k + pad), 7.0, dtype=dtype, device=gpu)
+    dlm.mx_unpack(q, out[:, :k])
+    # (a group that 1e38 times a normal value overflows is NaN)
+    torch.testing.assert_close(out[:, :k].cpu().double(), ref.values(codes, scales, k), rtol=0, atol=0,
+                               equal_nan=True)
+    assert torch.equal(out[:, k:].cpu(), torch.full((n, pad), 7.0, dtype=dtype))
+
+
+def test_pack_borders_and_non_finite(gpu):
+    """Every border of two codes and its neighbours, each scale's ends, signs of zero; a group
+    with an infinity or a NaN becomes NaN alone."""
+    border = torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0])
+    near = torch.cat([border, torch.nextafter(border, torch.tensor(9.0)),
+                      torch.nextafter(border, torch.tensor(0.0))])
+    rows = []
+    for amax in (3.5000002, 4.0, 6.0, 7.0):
+        rows.append(torch.cat([near, -near[:7], torch.tensor([amax])]))
+    w = torch.cat([torch.stack(rows) * 2.0 ** e for e in (-126, -100, 0, 3, 100, 124)])
+    w = torch.cat([w, torch.zeros(1, 32), -torch.zeros(1, 32), torch.full((1, 32), 3.4e38),
+                   torch.full((1, 32), 1e-45)])
+    w = torch.cat([w, _randn(w.shape[0], 64, seed=1)], 1)
+    w[2, 40], w[3, 40], w[5, 95] = math.inf, -math.inf, math.nan
+    codes, scales = ref.pack(w)
+    q = dlm.make_mx(torch.empty_like(codes).to(gpu), torch.empty_like(scales).to(gpu), *w.shape)
+    dlm.mx_pack(w.to(gpu), q)
+    assert torch.equal(q._keep[1].cpu(), scales)
+    assert torch.equal(q._keep[0].cpu(), codes)
+    assert scales[2, 1] == scales[3, 1] == scales[5, 2] == 255 and scales[2, 0] != 255
+    for dt in (F32, BF16):
+        out = torch.empty(w.shape, dtype=dt, device=gpu)
+        dlm.mx_unpack(q, out)
+        torch.testing.assert_close(out.cpu().double(), ref.values(codes, scales, w.shape[1]), rtol=0,
+                                   atol=0, equal_nan=True)
+
+
+def test_unpack_every_code_and_scale(gpu):
+    """All 256 bytes under all scale bytes; beyond a type's range: infinite."""
+    codes = torch.arange(256, dtype=torch.uint8).reshape(1, 256).repeat(256, 1)
+    scales = torch.arange(256, dtype=torch.uint8)[:, None].repeat(1, 16).contiguous()
+    q = dlm.make_mx(codes.to(gpu), scales.to(gpu), 256, 512)
+    v = ref.values(codes, scales, 512)
+    for dt in (F32, BF16):
+        out = torch.empty(256, 512, dtype=dt, device=gpu)
+        dlm.mx_unpack(q, out)
+        want = torch.where(v.abs() >= 2.0 ** 128, v.sign() * math.inf, v)
+        torch.testing.assert_close(out.cpu().double(), want, rtol=0, atol=0, equal_nan=True)
+
+
+# ---------------------------------------------------------------- products
+def _check_linear(gpu, m, n, k, dtype, epilogue, pad=0, seed=0, out_pad=0):
+    q, w = _packed(gpu, n, k, seed=seed)
+    x = _randn(m, k + pad, seed=seed + 1, dtype=dtype)
+    xd = x.to(gpu)[:, :k]
+    x = x[:, :k].double()
+    p, bound = x @ w.T, ref.product_bound(x, w, dtype)
+    epi = dlm.MX_EPILOGUES[epilogue]
+    cols = n // 2 if epilogue == "swiglu" else n
+    ydt = dtype if epilogue == "swiglu" else F32
+    y = _randn(m, cols + out_pad, seed=seed + 2).to(ydt).to(gpu)
+    before = y.cpu()
+    need = dlm.mx_linear_workspace(dtype, m, q, epi)
+    ws = torch.full((need + 256,), 0xFF, dtype=torch.uint8, device=gpu) if need else None
+    dlm.mx_linear(xd, q, y[:, :cols], epi, ws)
+    got = y.cpu()
+    assert torch.equal(got[:, cols:], before[:, cols:])
+    if need:
+        assert bool((ws[need:] == 0xFF).all())
+    if epilogue == "swiglu":
+        g, u = p.chunk(2, -1)
+        tg, tu = bound.chunk(2, -1)
+        want, bound = ref.silu_mul(g, u), ref.swiglu_bound(g, u, tg, tu, dtype)
+    elif epilogue == "add":
+        want = before[:, :cols].double() + p
+        bound = bound + ref.U * want.abs()
+    else:
+        want = p
+    err = (got[:, :cols].double() - want).abs()
+    assert bool((err <= bound + 1e-37).all()), float((err / (bound + 1e-37)).max())
+    # the same call again gives the same bits
+    y2 = before.to(gpu)
+    dlm.mx_linear(xd, q, y2[:, :cols], epi, ws)
+    assert torch.equal(y2.cpu(), got)
+
+
+@pytest.mark.parametrize("epilogue", ["store", "add", "swiglu"])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("m", [1, 5, 16, 17, 32, 33, 64, 65, 130, 257])
+def test_linear_rows(gpu, m, dtype, epilogue):
+    _check_linear(gpu, m, 160, 512, dtype, epilogue, seed=m)
+
+
+@pytest.mark.parametrize("epilogue", ["store", "swiglu"])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n,k", [(2, 1), (18, 31), (34, 33), (66, 127), (130, 129), (256, 688),
+                                 (94, 1031), (688, 264), (4096, 256), (512, 4096)])
+def test_linear_shapes(gpu, n, k, dtype, epilogue):
+    _check_linear(gpu, 19, n, k, dtype, epilogue, seed=n)
+
+
+@pytest.mark.parametrize("m", [3, 70, 300])
+@pytest.mark.parametrize("pad,out_pad", [(8, 0), (3, 5), (0, 1)])
+def test_linear_strides(gpu, m, pad, out_pad):
+    for dtype in (BF16, F32):
+        for epilogue in ("store", "add", "swiglu"):
+            _check_linear(gpu, m, 96, 200, dtype, epilogue, pad, seed=m, out_pad=out_pad)
+
+
+@pytest.mark.parametrize("m", [2, 32, 300])
+def test_linear_long_k(gpu, m):
+    _check_linear(gpu, m, 144, 18944, BF16, "add", seed=3)
+
+
+def test_linear_ignores_codes_behind_k(gpu):
+    """Codes behind k count for nothing, whatever they are; x behind k is never read."""
+    for dtype in (BF16, F32):
+        for k in (40, 33):
+            q, w = _packed(gpu, 48, k)
+            q._keep[0].view(48, -1)[:, (k + 1) // 2:] = 0x77
+            x = torch.full((20, k + 24), math.nan, dtype=dtype, device=gpu)
+            x[:, :k] = _randn(20, k, seed=5, dtype=dtype).to(gpu)
+            if k % 2:      # the last byte's high half is behind k
+                c = q._keep[0].view(48, -1)
+                c[:, k // 2] = (c[:, k // 2] & 15) | 0x70
+            y = torch.empty(20, 48, device=gpu)
+            ws = torch.empty(max(256, dlm.mx_linear_workspace(dtype, 20, q)), dtype=torch.uint8, device=gpu)
+            dlm.mx_linear(x[:, :k], q, y, workspace=ws)
+            xx = x[:, :k].cpu().double()
+            assert bool(((y.cpu().double() - xx @ w.T).abs() <= ref.product_bound(xx, w, dtype)).all())
+
+
+def test_linear_non_finite(gpu):
+    """A NaN group makes its column NaN, and no other; so does an infinite or NaN input its row."""
+    w = _randn(40, 96, seed=1)
+    w[7, 50] = math.nan
+    q, v = _packed(gpu, 40, 96, w=w)
+    for dtype in (BF16, F32):
+        x = _randn(6, 96, seed=2, dtype=dtype)
+        x[2, 3], x[4, 90] = math.inf, math.nan
+        y = torch.empty(6, 40, device=gpu)
+        ws = torch.empty(1 << 16, dtype=torch.uint8, device=gpu)
+        dlm.mx_linear(x.to(gpu), q, y, workspace=ws)
+        y = y.cpu()
+        want = x.double() @ v.T
+        assert torch.equal(y.isnan(), want.isnan())
+        assert torch.equal(y.isinf(), want.isinf())
+        assert torch.equal(y.sign()[want.isinf()].double(), want.sign()[want.isinf()])
+
+
+def test_linear_large_offsets(gpu):
+    """Rows of the output more than 2^31 bytes behind the first."""
+    q, w = _packed(gpu, 32, 64)
+    y = torch.zeros(3, 400_000_000, device=gpu)
+    x = _randn(3, 64, seed=1, dtype=BF16)
+    dlm.mx_linear(x.to(gpu), q, y[:, -32:])
+    xx = x.double()
+    assert bool(((y[:, -32:].cpu().double() - xx @ w.T).abs() <= ref.product_bound(xx, w, BF16)).all())
+    assert not y[:, :-32].any()
+
+
+# ------------------------------------------------------------------- cache
+def _model(gpu, hq, hkv, dh, dtype, n_layers=1):
+    d, f, v = 64, 64, 64
+    z = lambda *s, dtype=dtype: torch.zeros(*s, dtype=dtype, device=gpu)
+    sh = engine.ModelShape(n_layers, d, hq, hkv, dh, f, v, "bf16" if dtype == BF16 else "f32")
+    layer = {"attn_norm": z(d, dtype=F32), "w_qkv": z(sh.qkv_dim, d), "w_o": z(d, hq * dh),
+             "ffn_norm": z(d, dtype=F32), "w_gate_up": z(2 * f, d), "w_down": z(d, f)}
+    return engine.DeviceModel(sh, {"embed": z(v, d), "lm_head": z(v, d), "final_norm": z(d, dtype=F32),
+                                   "layers": [layer] * n_layers}, 1.0)
+
+
+class Cache:
+    """A 4-bit cache whose buffer starts as the given byte everywhere."""
+
+    def __init__(self, gpu, hq, hkv, dh, dtype, slots, seq, n_layers=1, fill=0xFF):
+        self.model = _model(gpu, hq, hkv, dh, dtype, n_layers)
+        self.dims = (hq, hkv, dh, dtype, slots, -(-seq // 64) * 64)
+        _, need = dlm.kv_cache_alloc_mx(self.model.handle, slots, seq)
+        self.buf = torch.full((need,), fill, dtype=torch.uint8, device=gpu)
+        self.handle, _ = dlm.kv_cache_alloc_mx(self.model.handle, slots, seq, self.buf, need)
+        self.n_layers = n_layers
+
+    def parts(self, layer=0):
+        """Views [slot, head, pos, bytes] of the layer's codes and scales: kc, vc, ks, vs."""
+        hq, hkv, dh, _, slots, s = self.dims
+        up = lambda b: -(-b // 256) * 256
+        sizes = [slots * hkv * s * dh // 2] * 2 + [slots * hkv * s * dh // 32] * 2
+        at = layer * sum(up(b) for b in sizes)
+        out = []
+        for b in sizes:
+            out.append(self.buf[at:at + b].view(slots, hkv, s, -1))
+            at += up(b)
+        return out
+
+    def fill(self, slot, length, seed, layer=0):
+        """Random keys and values at [0, length) of a slot; their values [length, hkv, dh]."""
+        hq, hkv, dh, _, _, _ = self.dims
+        kc, vc, ks, vs = self.parts(layer)
+        out = []
+        for c, s, sd in ((kc, ks, seed), (vc, vs, seed + 1)):
+            codes, scales = ref.pack(_randn(hkv * length, dh, seed=sd))
+            c[slot, :, :length] = codes.view(hkv, length, dh // 2).to(c.device)
+            s[slot, :, :length] = scales[:, :dh // 32].reshape(hkv, length, dh // 32).to(c.device)
+            out.append(ref.values(codes, scales, dh).view(hkv, length, dh).permute(1, 0, 2))
+        return out
+
+    def close(self):
+        dlm.cache_destroy(self.handle)
+        self.model.close()
+
+
+def _rot(pos, dh):
+    ang = pos.double()[:, None] * 10000.0 ** (-torch.arange(dh // 2).double() / (dh // 2))
+    return torch.stack([ang.cos(), ang.sin()], -1).float()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("hq,hkv,dh", [(4, 4, 64), (7, 1, 128), (12, 2, 64), (32, 32, 128), (3, 3, 128)])
+@pytest.mark.parametrize("splits", [1, 3])
+def test_append_and_read(gpu, hq, hkv, dh, dtype, splits):
+    """Bit for bit the packed fp32 rotation; every other byte of the cache stays."""
+    c = Cache(gpu, hq, hkv, dh, dtype, 4, 130, n_layers=2)
+    reqs = [(2, 130, 1, 66), (0, 64, 63, 1), (3, 9, 9, 0), (1, 77, 0, 77)]
+    n = sum(r[3] for r in reqs)
+    pos = torch.cat([torch.arange(p, p + m) for _, _, p, m in reqs])
+    D = (hq + 2 * hkv) * dh
+    qkv = _randn(splits, n, D, seed=hq + dh)
+    qkv[:, 0, -1] = math.nan                       # the last value group of the first row
+    rot = _rot(pos, dh)
+    q_out = torch.empty(n, hq * dh, dtype=dtype, device=gpu)
+    before = c.buf.clone()
+    rows = dlm.make_kv_rows(reqs)
+    dlm.mx_kv_append(c.handle, 1, rows, qkv.to(gpu), rot.to(gpu), q_out)
+    x = qkv[0]
+    for s in range(1, splits):
+        x = x + qkv[s]
+    x = x.view(n, hq + 2 * hkv, dh)
+    want_q = ref.rotate32(x[:, :hq], rot).to(dtype).reshape(n, -1)
+    # (fp32 queries: one rounding of each of the three operations)
+    torch.testing.assert_close(q_out.cpu(), want_q, rtol=0, atol=0)
+    k, v = ref.rotate32(x[:, hq:hq + hkv], rot), x[:, hq + hkv:]
+    kc, vc, ks, vs = c.parts(1)
+    old = before.clone()
+    c.buf, old = old, c.buf                        # write the expectation into the old bytes
+    ekc, evc, eks, evs = c.parts(1)
+    at = 0
+    for slot, _, p, m in reqs:
+        for t, ec, es in ((k, ekc, eks), (v, evc, evs)):
+            codes, scales = ref.pack(t[at:at + m].reshape(-1, dh))
+            ec[slot, :, p:p + m] = codes.view(m, hkv, dh // 2).permute(1, 0, 2).to(gpu)
+            es[slot, :, p:p + m] = scales[:, :dh // 32].reshape(m, hkv, dh // 32).permute(1, 0, 2).to(gpu)
+        at += m
+    c.buf, old = old, c.buf
+    assert torch.equal(c.buf, old)
+    ko, vo = (torch.empty(n, hkv * dh, dtype=dtype, device=gpu) for _ in range(2))
+    dlm.mx_kv_read(c.handle, 1, rows, ko, vo)
+    for got, t in ((ko, k), (vo, v)):
+        codes, scales = ref.pack(t.reshape(-1, dh))
+        torch.testing.assert_close(got.cpu().double().view(-1, dh), ref.values(codes, scales, dh), rtol=0,
+                                   atol=0, equal_nan=True)
+    assert vo[0, -1].isnan() and vo[0, -dh:].isnan().sum() == 32
+    c.close()
+
+
+def _check_attention(gpu, c, reqs, seed, std=1.5, layer=0, kv=None):
+    hq, hkv, dh, dtype, _, _ = c.dims
+    n = sum(r[3] for r in reqs)
+    q = _randn(n, hq * dh, seed=seed, dtype=dtype, std=std)
+    if kv is None:
+        kv = {}
+        for i, (slot, length, _, _) in enumerate(reqs):
+            if slot not in kv:
+                kv[slot] = c.fill(slot, max(l for s, l, _, _ in reqs if s == slot), seed + 7 * i, layer)
+    rows = dlm.make_kv_rows(reqs)
+    need = dlm.mx_kv_attention_workspace(c.handle, rows)
+    ws = torch.full((need + 256,), 0xFF, dtype=torch.uint8, device=gpu) if need else None
+    out = torch.full((n + 1, hq * dh), 7.0, dtype=dtype, device=gpu)
+    before = c.buf.clone()
+    dlm.mx_kv_attention(c.handle, layer, rows, q.to(gpu), out[:n], ws)
+    got = out.cpu()
+    assert bool((got[n] == 7.0).all()) and torch.equal(c.buf, before)
+    if need:
+        assert bool((ws[need:] == 0xFF).all())
+    at, worst = 0, 0.0
+    for slot, length, _, m in reqs:
+        k, v = kv[slot]
+        want, bound = ref.attention(q[at:at + m].double().view(m, hq, dh), k[:length], v[:length], dtype)
+        err = (got[at:at + m].double().view(m, hq, dh) - want).abs()
+        assert bool((err <= bound).all()), (slot, length, m, float((err / bound.clamp_min(1e-300)).max()))
+        at += m
+    again = torch.empty_like(out[:n])
+    dlm.mx_kv_attention(c.handle, layer, rows, q.to(gpu), again, ws)
+    assert torch.equal(again.cpu(), got[:n])
+    return need
+
+
+HEADS = [(4, 4, 64), (7, 1, 128), (12, 2, 64), (8, 8, 128), (6, 3, 128), (5, 5, 64)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("hq,hkv,dh", HEADS)
+def test_attention_ragged(gpu, hq, hkv, dh, dtype):
+    """Lengths around the tiles, rows around the row tiles, an empty sequence, garbage (NaN
+    scales) behind every sequence, a slot listed twice."""
+    c = Cache(gpu, hq, hkv, dh, dtype, 8, 330)
+    reqs = [(5, 1, 0, 1), (0, 63, 0, 3), (1, 64, 0, 16), (2, 65, 0, 17), (3, 0, 0, 5), (4, 129, 0, 33),
+            (6, 330, 0, 70), (7, 31, 0, 0), (6, 200, 0, 2)]
+    _check_attention(gpu, c, reqs, seed=hq + dh)
+    c.close()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("hq,hkv,dh", [(4, 4, 64), (7, 1, 128), (2, 2, 128)])
+@pytest.mark.parametrize("length,rows", [(517, 32), (2304, 5), (8192, 1), (8191, 40)])
+def test_attention_long(gpu, hq, hkv, dh, dtype, length, rows):
+    """Few rows over long sequences (the keys split over blocks), with an empty and a short
+    sequence in the same call."""
+    c = Cache(gpu, hq, hkv, dh, dtype, 3, 8192)
+    _check_attention(gpu, c, [(1, length, 0, rows), (0, 0, 0, 2), (2, 70, 0, 3)], seed=length)
+    c.close()
+
+
+@pytest.mark.parametrize("hq,hkv,dh", [(28, 4, 128), (8, 8, 128), (8, 8, 64)])
+def test_attention_many_rows(gpu, hq, hkv, dh):
+    """Whole sequences: many row tiles."""
+    c = Cache(gpu, hq, hkv, dh, BF16, 3, 400)
+    _check_attention(gpu, c, [(2, 400, 0, 400), (0, 129, 0, 129), (1, 333, 0, 64)], seed=9)
+    c.close()
+
+
+def test_attention_layers_and_large_scores(gpu):
+    """The second of two layers; scores of hundreds, where one key takes all the weight."""
+    c = Cache(gpu, 4, 2, 64, BF16, 2, 300, n_layers=2)
+    _check_attention(gpu, c, [(1, 300, 0, 40), (0, 150, 0, 33)], seed=4, std=60.0, layer=1)
+    c.close()
+
+
+def test_attention_nan_keys_reach_their_rows_only(gpu):
+    """A NaN among a sequence's keys or values makes its request NaN (a value: that
+    element), and no other request's."""
+    c = Cache(gpu, 2, 1, 64, BF16, 3, 100)
+    for slot in range(3):
+        c.fill(slot, 100, seed=slot)
+    kc, vc, ks, vs = c.parts()
+    ks[1, 0, 40, 0] = 255
+    vs[2, 0, 99, 1] = 255
+    q = _randn(30, 128, seed=1, dtype=BF16).to(gpu)
+    out = torch.empty_like(q)
+    dlm.mx_kv_attention(c.handle, 0, dlm.make_kv_rows([(s, 100, 0, 10) for s in range(3)]), q, out)
+    nan = out.isnan().view(30, 2, 64).cpu()
+    assert not nan[:10].any() and nan[10:20].all()
+    assert nan[20:, :, 32:].all() and not nan[20:, :, :32].any()
+    c.close()
+
+
+# ----------------------------------------------------- streams, graphs, set
+def test_other_stream_and_graph(gpu):
+    """The set on a side stream and in a graph that is replayed between eager calls: append,
+    attention and product, each replay equal to the eager results on its inputs."""
+    hq, hkv, dh = 4, 2, 64
+    c = Cache(gpu, hq, hkv, dh, BF16, 2, 700)
+    c.fill(0, 700, seed=1)
+    c.fill(1, 90, seed=2)
+    rows = dlm.make_kv_rows([(0, 700, 600, 32), (1, 90, 10, 20)])
+    n, D = 52, (hq + 2 * hkv) * dh
+    qkv = torch.empty(1, n, D, device=gpu)
+    rot = _rot(torch.cat([torch.arange(600, 632), torch.arange(10, 30)]), dh).to(gpu)
+    q = torch.empty(n, hq * dh, dtype=BF16, device=gpu)
+    o = torch.empty_like(q)
+    w, _ = _packed(gpu, 200, hq * dh, seed=3)
+    y = torch.empty(n, 200, device=gpu)
+    ws = torch.empty(max(256, dlm.mx_kv_attention_workspace(c.handle, rows)), dtype=torch.uint8, device=gpu)
+    ws2 = torch.empty(max(256, dlm.mx_linear_workspace(BF16, n, w)), dtype=torch.uint8, device=gpu)
+
+    def step():
+        dlm.mx_kv_append(c.handle, 0, rows, qkv, rot, q)
+        dlm.mx_kv_attention(c.handle, 0, rows, q, o, ws)
+        dlm.mx_linear(o, w, y, workspace=ws2)
+
+    def eager(seed):
+        qkv.copy_(_randn(1, n, D, seed=seed))
+        step()
+        torch.cuda.synchronize()
+        return o.clone(), y.clone(), c.buf.clone()
+
+    want = [eager(s) for s in (10, 11, 12)]
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        qkv.copy_(_randn(1, n, D, seed=10))
+        step()
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip((o, y, c.buf), want[0]))
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step()
+    for i, s in enumerate((11, 10, 12, 11)):
+        qkv.copy_(_randn(1, n, D, seed=s))
+        o.zero_(), y.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((o, y, c.buf), want[s - 10])), i
+        assert all(torch.equal(a, b) for a, b in zip(eager(12), want[2]))
+    c.close()

@@ -1,0 +1,199 @@
+"""Models with 4-bit projections and engines with a 4-bit cache: the step's path through
+the operators of test_gpu_mx."""
+import dataclasses
+
+import numpy as np
+import pytest
+import torch
+
+import mx_reference as ref
+import oracle
+import synth
+import synth.device as sdev
+from helpers import calibrated_inv_tau, host_weights, logit_err, run_teacher_forced
+from paper_2606_29094_amd import dlm, engine
+
+pytestmark = pytest.mark.gpu
+
+GQA_SMALL = dataclasses.replace(synth.GQA_7B, n_layers=2, d_model=512, n_q_heads=14, n_kv_heads=2,
+                                head_dim=64, d_ffn=1424, vocab=4096)
+MHA_SMALL = dataclasses.replace(synth.MHA_8B, n_layers=2, d_model=1024, n_q_heads=8, n_kv_heads=8,
+                                head_dim=128, d_ffn=2048, vocab=4096)
+MODELS = {"tiny": synth.TINY_FP32, "gqa": GQA_SMALL, "mha": MHA_SMALL}
+
+
+def _shape(cfg):
+    return engine.ModelShape.of(cfg)
+
+
+def _unpacked(packed, tensors, cfg):
+    """The tensors with the packed projections' values in the model dtype."""
+    out = dict(tensors, layers=[])
+    for lp, l in zip(packed.tensors["layers"], tensors["layers"]):
+        layer = dict(l)
+        for name in ("w_qkv", "w_o", "w_gate_up", "w_down"):
+            layer[name] = torch.empty_like(l[name])
+            dlm.mx_unpack(lp[name], layer[name])
+        out["layers"].append(layer)
+    return out
+
+
+def _requests(cfg, specs, block):
+    return [engine.Request(synth.tokens(30 + i, P, cfg.vocab), G, block, g)
+            for i, (P, G, g) in enumerate(specs)]
+
+
+SPECS = [(100, 64, 0.9), (37, 50, 0.7), (64, 33, 0.95)]
+
+
+@pytest.mark.parametrize("name", list(MODELS))
+@pytest.mark.parametrize("mode", ["none", "dual", "prefix"])
+def test_packed_model_against_the_oracle(gpu, name, mode):
+    """Steps of the packed model against the oracle on the packed values."""
+    cfg = MODELS[name]
+    t = sdev.model_tensors(cfg)
+    packed = engine.DeviceModel(_shape(cfg), t, 1.0, packed=True)
+    W = host_weights(_unpacked(packed, t, cfg), cfg)
+    oreqs = [oracle.Request.new(synth.tokens(30 + i, P, cfg.vocab), G, 32, g, cfg.mask_id)
+             for i, (P, G, g) in enumerate(SPECS)]
+    inv_tau = calibrated_inv_tau(cfg, W, oreqs, mode)
+    model = engine.DeviceModel(_shape(cfg), packed.tensors, inv_tau, packed=True)
+    reqs = _requests(cfg, SPECS, 32)
+    eng = engine.Engine(model, 3, 164, mode)
+    for r in reqs:
+        eng.admit(r, cfg.mask_id)
+    if cfg.dtype == "bf16":
+        print(run_teacher_forced(cfg, W, eng, reqs, oreqs, mode, inv_tau, 3))
+    else:
+        import helpers
+        # (the fp32 model's steps are compared at fp32 tolerances)
+        for _ in range(3):
+            for r, oq in zip(reqs, oreqs):
+                eng.set_state(r, oq.tokens, oq.mask, oq.k)
+            z, out, starts = helpers.gpu_step_with_logits(eng, reqs)
+            for j, oq in enumerate(oreqs):
+                res = oracle.denoise_step(cfg, W, oq, mode, inv_tau, keep_logits=True)
+                helpers.check_step_e2e(res, {k: v[j] for k, v in out.items()}, starts[j],
+                                       reqs[j].threshold, z[j], "f32")
+    eng.close()
+
+
+@pytest.mark.parametrize("name", list(MODELS))
+def test_packed_model_is_the_dense_model_of_its_values(gpu, name):
+    """Logits of a recompute step next to those of a model that holds the packed values: the
+    products differ in the order of their fp32 sums only. Rows above and below the row
+    count from which matrices are unpacked for the GEMM kernels."""
+    cfg = MODELS[name]
+    t = sdev.model_tensors(cfg)
+    packed = engine.DeviceModel(_shape(cfg), t, 10.0, packed=True)
+    dense = engine.DeviceModel(_shape(cfg), _unpacked(packed, t, cfg), 10.0)
+    for specs in ([(20, 12, 0.9)], [(400, 100, 0.9), (300, 64, 0.9)]):
+        z = []
+        for model in (packed, dense):
+            reqs = _requests(cfg, specs, 32)
+            eng = engine.Engine(model, len(reqs), 512, "dual")
+            for r in reqs:
+                eng.admit(r, cfg.mask_id)
+            z.append(eng.debug_logits(reqs).cpu().numpy())
+            eng.close()
+        # bf16 activations: a rounding that falls to the other side is 2^-8 of a value; the
+        # logits of two layers move by less than the end-to-end tolerance of the GPU tests
+        assert logit_err(z[0], z[1]) < (2e-2 if cfg.dtype == "bf16" else 1e-4)
+
+
+@pytest.mark.parametrize("name", list(MODELS))
+@pytest.mark.parametrize("packed", [False, True])
+def test_packed_cache_step(gpu, name, packed):
+    """One layer of a recompute and of a cache step over a packed cache: what is stored is the
+    packed rotation of the step's own products, and its attention is the definition's on
+    the step's queries and the stored values."""
+    cfg = MODELS[name]
+    t = sdev.model_tensors(cfg)
+    model = engine.DeviceModel(_shape(cfg), t, 10.0, packed=packed)
+    hq, hkv, dh = cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim
+    dt = torch.bfloat16 if cfg.dtype == "bf16" else torch.float32
+    for mode in ("dual", "prefix", "none"):
+        reqs = _requests(cfg, SPECS, 32)
+        eng = engine.Engine(model, 3, 164, mode, packed_kv=True)
+        for r in reqs:
+            eng.admit(r, cfg.mask_id)
+        for step in range(2):
+            ranges = eng.step_rows(reqs)
+            saved = [r.refreshed_block for r in reqs]
+            buf, splits = eng.debug_trace(reqs, 1)
+            for r, s in zip(reqs, saved):
+                r.refreshed_block = s
+            qkv = buf["qkv"].cpu()
+            x = qkv[0]
+            for s in range(1, splits):
+                x = x + qkv[s]
+            x = x.view(-1, hq + 2 * hkv, dh)
+            at = 0
+            for r, (r0, r1) in zip(reqs, ranges):
+                m = r1 - r0
+                k, v = (y.double() for y in eng.read_kv(1, r.slot, r.seq_len))
+                q = buf["q"][at:at + m].cpu().double().view(m, hq, dh)
+                want, bound = ref.attention(q, k, v, dt)
+                err = (buf["attn_out"][at:at + m].cpu().double().view(m, hq, dh) - want).abs()
+                assert bool((err <= bound).all()), float((err / bound).max())
+                # values are packed as they come out of the product
+                codes, scales = ref.pack(x[at:at + m, hq + hkv:].reshape(-1, dh))
+                assert torch.equal(v[r0:r1].reshape(-1, dh), ref.values(codes, scales, dh))
+                # keys: the angles are the library's own; a stored key is within a step of 2 of
+                # its group's scale (and half of that for the rounding) of the rotated one
+                ang = torch.arange(r0, r1).double()[:, None] * \
+                    cfg.rope_theta ** (-torch.arange(dh // 2).double() / (dh // 2))
+                a, b = x[at:at + m, hq:hq + hkv].double().chunk(2, -1)
+                c, s_ = ang.cos()[:, None], ang.sin()[:, None]
+                kr = torch.cat([a * c - b * s_, b * c + a * s_], -1).reshape(-1, 32)
+                top = kr.abs().amax(-1, keepdim=True)
+                assert bool(((k[r0:r1].reshape(-1, 32) - kr).abs() <= top * (1 / 3.5 + 1e-3)).all())
+                at += m
+            eng.step(reqs)
+        eng.close()
+
+
+def test_packed_generation_runs_and_repeats(gpu):
+    """Whole generations with packed weights and cache: every position is unmasked, and a second
+    run gives the same tokens."""
+    cfg = GQA_SMALL
+    t = sdev.model_tensors(cfg)
+    model = engine.DeviceModel(_shape(cfg), t, 10.0, packed=True)
+    runs = []
+    for _ in range(2):
+        reqs = _requests(cfg, SPECS, 32)
+        eng = engine.Engine(model, 3, 164, "dual", packed_kv=True)
+        for r in reqs:
+            eng.admit(r, cfg.mask_id)
+        while any(not r.done for r in reqs):
+            eng.step([r for r in reqs if not r.done])
+        runs.append([eng.read_state(r) for r in reqs])
+        eng.close()
+    for (a, ma), (b, mb) in zip(*runs):
+        assert not ma.any() and np.array_equal(a, b)
+
+
+def test_packed_step_without_allocation(gpu):
+    """dlm_denoise_step_noalloc on a packed model and cache: the step's outputs."""
+    cfg = GQA_SMALL
+    t = sdev.model_tensors(cfg)
+    model = engine.DeviceModel(_shape(cfg), t, 10.0, packed=True)
+    outs = []
+    for noalloc in (False, True):
+        reqs = _requests(cfg, SPECS, 32)
+        eng = engine.Engine(model, 3, 164, "dual", packed_kv=True)
+        for r in reqs:
+            eng.admit(r, cfg.mask_id)
+        eng.step(reqs)
+        if noalloc:
+            batch = dlm.make_batch(eng.dlm_reqs(reqs), eng.tokens, eng.mask, eng.mode_id)
+            dlm.denoise_step_noalloc(model.handle, eng.cache, batch, [r.threshold for r in reqs], eng.step_out)
+            torch.cuda.synchronize()
+        else:
+            eng.enqueue_step(reqs)
+            torch.cuda.synchronize()
+        outs.append(eng.read_outputs(3))
+        eng.close()
+    for k in outs[0]:
+        if k in ("n", "block_conf", "block_tok"):
+            assert np.array_equal(outs[0][k], outs[1][k]), k
