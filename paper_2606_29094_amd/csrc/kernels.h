@@ -194,16 +194,23 @@ template <typename T>
 hipError_t mx_pack(const T* w, long ldw, int k, const MxView& o, hipStream_t st);
 template <typename T>
 hipError_t mx_unpack(const MxView& w, int k, T* out, long ldo, hipStream_t st);
-// y = x w^T: store or add fp32 [rows, n], or silu(gate) * up in T ([rows, n / 2], rows
-// [0, n / 2) of w the gate). scratch: mx_linear_scratch bytes, 16-byte aligned; aligned:
-// x rows start at multiples of 16 bytes and k is a multiple of 8.
-size_t mx_linear_scratch(int elem, int rows, int k, bool aligned);
-template <typename T>
-hipError_t mx_linear(const T* x, long ldx, int rows, const MxView& w, int k, bool swiglu, bool add,
-                     void* y, long ldy, void* scratch, hipStream_t st);
-// A product's way: straight from the codes, or (gemm) over the matrix unpacked to the
-// scratch and the GEMM kernels of its type.
-struct MxPlan { bool gemm = false; GemmPlan g{}; size_t scratch = 0; };
+// Products y = x w^T: fp32 [rows, n] stored or added, or silu(gate) * up in T
+// ([rows, n / 2], rows [0, n / 2) of w the gate).
+// A product's way: straight from the codes with K in `slices` (kMxFew: 16 mt rows x 16 nf
+// columns a block of `waves` waves; tiles of 64 x 128 and 128 x 256), or (gemm) over the matrix unpacked to the scratch and the GEMM kernels
+// of its type. scratch: bytes, 256-byte aligned. staged: x is first copied into the
+// scratch's first `stage` bytes (fp32 x, or rows that 16-byte loads cannot read).
+enum { kMxFew, kMxTile64, kMxTile128 };
+constexpr int kMxTileK = 1 << 24;   // the tiles take rows (and row strides) of up to that many elements
+struct MxTile { int kind, mt, nf, slices, waves; };
+struct MxPlan {
+  bool gemm = false, staged = false;
+  GemmPlan g{};
+  MxTile tile{};
+  size_t stage = 0, scratch = 0;
+};
+// aligned: x (and y) start at multiples of 16 bytes, as do their rows, at most kMxTileK
+// elements apart
 MxPlan mx_plan(int elem, int rows, int n, int k, bool swiglu, bool aligned, int num_cu);
 // epilogue: dlm_mx_epilogue
 template <typename T>
@@ -217,6 +224,9 @@ struct MxLinear {
   int m, k;                // k: elements of x a row holds (a multiple of 8)
   void* y;
   long ldy;
+  float* slices;           // [slice][m][n] partial sums, where K is sliced
+  int per_slice;           // k steps of the kernel in a slice
+  int planes;
   bool swiglu, add;
 };
 

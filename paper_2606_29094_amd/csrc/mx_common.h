@@ -29,6 +29,26 @@ __device__ __forceinline__ bf16x8 mx_bf16x8(uint32_t w, float s) {
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
+// Four dwords of each of the four 16-lane groups, transposed: lane l of group g comes
+// with dword j of row g in v[j] and leaves with dword g of row j.
+__device__ __forceinline__ u32x4 transpose_groups(u32x4 v) {
+  typedef uint32_t pair __attribute__((ext_vector_type(2)));
+  auto swap32 = [](uint32_t& a, uint32_t& b) {   // upper half of a with the lower one of b
+    const pair r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+    a = r[0], b = r[1];
+  };
+  auto swap16 = [](uint32_t& a, uint32_t& b) {   // odd groups of a with the even ones of b
+    const pair r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+    a = r[0], b = r[1];
+  };
+  uint32_t a = v[0], b = v[1], c = v[2], d = v[3];
+  swap32(a, c);
+  swap32(b, d);
+  swap16(a, b);
+  swap16(c, d);
+  return u32x4{a, b, c, d};
+}
+
 // Scale byte of a group from the largest magnitude's bits (any value's bits without
 // the sign, compared as integers: NaN and infinity come out above every number).
 // e is the exponent that puts the largest magnitude into (3.5, 7] scales, so it

@@ -2,6 +2,10 @@
 // gemm.hip.
 #pragma once
 
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+
 #include "../../include/dlm.h"
 #include "kernels.h"
 #include "mx_common.h"
@@ -35,15 +39,20 @@ __global__ __launch_bounds__(256) void mx_stage_kernel(const T* __restrict__ x, 
 
 __device__ __forceinline__ float silu_mul(float g, float u) { return g / (1.f + __expf(-g)) * u; }
 
-// One block: 16 MT rows x 16 NF columns, W waves that take the 128-wide k chunks
-// in turn and add their partial sums in LDS, in wave order. In a chunk lane l reads
-// the 32 codes of group l / 16 of weight row l % 16 as one 16-byte load; the MFMA
-// j = 0..3 multiplies their dword j with the same eight elements of x (the order
-// of k inside a chunk is the same on both sides). The weights are read once, by
-// the one block row that needs them; x comes from the caches.
+// Few rows. One block: 16 MT rows x 16 NF columns, W waves that take the 512-wide k
+// ranges ("walks") of the block's K slice in turn and add their partial sums in LDS, in
+// wave order. In a chunk of 128 k lane l reads the 32 codes of group l / 16 of weight
+// row l % 16 as one 16-byte load; four register swaps between the 16-lane groups turn
+// that into the dword of group j that the MFMA j = 0..3 takes (whose lanes then read
+// 64 consecutive bytes of each x row). A walk's codes and scales (one 16-byte load for its 16 groups) are all requested
+// before the first is used. The weights are read once, by the one block row that
+// needs them; x comes from the caches, once for every 16 NF columns.
+constexpr int kWalk = 512;
+
 template <int MT, int NF, int W, int NP>
 __global__ __launch_bounds__(W * 64) void mx_linear_kernel(MxLinear a) {
   __shared__ f32x4 part[W][MT * NF][64];
+  constexpr int XJ = NP > 1 ? 1 : 2;   // k steps whose x is requested together
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int col = lane & 15, g = lane >> 4;
   const int n0 = blockIdx.x * (a.swiglu ? NF * 8 : NF * 16), m0 = blockIdx.y * MT * 16;
@@ -60,12 +69,12 @@ __global__ __launch_bounds__(W * 64) void mx_linear_kernel(MxLinear a) {
       n = min(n0 + 16 * f + col, n_end - 1);
     }
     wc[f] = a.w.codes + ((long)n * a.w.groups + g) * 16;
-    ws[f] = a.w.scales + (long)n * a.w.scale_ld + g;
+    ws[f] = a.w.scales + (long)n * a.w.scale_ld;
   }
   const bf16* xr[MT];
 #pragma unroll
   for (int t = 0; t < MT; ++t)
-    xr[t] = a.x + (long)min(m0 + 16 * t + col, a.m - 1) * a.ldx + 32 * g;
+    xr[t] = a.x + (long)min(m0 + 16 * t + col, a.m - 1) * a.ldx + 8 * g;
 
   f32x4 acc[MT][NF];
 #pragma unroll
@@ -73,32 +82,70 @@ __global__ __launch_bounds__(W * 64) void mx_linear_kernel(MxLinear a) {
 #pragma unroll
     for (int f = 0; f < NF; ++f) acc[t][f] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  const int chunks = (a.w.groups + 3) / 4;
-  for (int c = wave; c < chunks; c += W) {
-    const bool ok = 4 * c + g < a.w.groups;
-    u32x4 codes[NF];
-    float s[NF];
+  // one walk; TAIL: the last one, whose groups and elements may end inside it
+  auto walk = [&](int s, auto tail) {
+    constexpr bool TAIL = decltype(tail)::value;
+    const int k0 = s * kWalk;
+    u32x4 codes[4][NF], scales[NF];
 #pragma unroll
     for (int f = 0; f < NF; ++f) {
-      codes[f] = ok ? *reinterpret_cast<const u32x4*>(wc[f] + (long)c * 64) : u32x4{0u, 0u, 0u, 0u};
-      s[f] = mx_scale(ok ? ws[f][4 * c] : 127u);
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        codes[c][f] = !TAIL || 16 * s + 4 * c + g < a.w.groups
+                          ? *reinterpret_cast<const u32x4*>(wc[f] + (long)s * 256 + c * 64)
+                          : u32x4{0u, 0u, 0u, 0u};
+      scales[f] = *reinterpret_cast<const u32x4*>(ws[f] + 16 * s);
     }
+    bf16x8 xv[2][XJ][NP][MT];
+    auto xload = [&](int i) {   // x of steps XJ i .. of the walk
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      bf16x8 b[NF];
+      for (int u = 0; u < XJ; ++u) {
+        const int c = (XJ * i + u) / 4, j = (XJ * i + u) % 4;
+        const bool in = !TAIL || k0 + 128 * c + 32 * j + 8 * g < a.k;
 #pragma unroll
-      for (int f = 0; f < NF; ++f) b[f] = mx_bf16x8(codes[f][j], s[f]);
-      const bool in = 128 * c + 32 * g + 8 * j < a.k;
+        for (int p = 0; p < NP; ++p)
 #pragma unroll
-      for (int p = 0; p < NP; ++p)
+          for (int t = 0; t < MT; ++t) {
+            bf16x8 v = {};
+            if (in) v = *reinterpret_cast<const bf16x8*>(xr[t] + p * a.plane + k0 + 128 * c + 32 * j);
+            xv[i & 1][u][p][t] = v;
+          }
+      }
+    };
+    xload(0);
 #pragma unroll
-        for (int t = 0; t < MT; ++t) {
-          bf16x8 v = {};
-          if (in) v = *reinterpret_cast<const bf16x8*>(xr[t] + p * a.plane + 128 * c + 8 * j);
+    for (int i = 0; i < 16 / XJ; ++i) {
+      if (i + 1 < 16 / XJ) xload(i + 1);
+      __builtin_amdgcn_sched_barrier(0);   // (or the loads are moved down to their uses)
 #pragma unroll
-          for (int f = 0; f < NF; ++f) acc[t][f] = mfma16_bf16(v, b[f], acc[t][f]);
+      for (int u = 0; u < XJ; ++u) {
+        const int c = (XJ * i + u) / 4, j = (XJ * i + u) % 4;
+        if (j == 0) {
+#pragma unroll
+          for (int f = 0; f < NF; ++f) codes[c][f] = transpose_groups(codes[c][f]);
         }
+        bf16x8 b[NF];
+#pragma unroll
+        for (int f = 0; f < NF; ++f) {
+          uint32_t e = (scales[f][c] >> (8 * j)) & 255u;
+          if (TAIL && 16 * s + 4 * c + j >= a.w.groups) e = 127u;
+          b[f] = mx_bf16x8(codes[c][f][j], mx_scale(e));
+        }
+#pragma unroll
+        for (int p = 0; p < NP; ++p)
+#pragma unroll
+          for (int t = 0; t < MT; ++t)
+#pragma unroll
+            for (int f = 0; f < NF; ++f) acc[t][f] = mfma16_bf16(xv[i & 1][u][p][t], b[f], acc[t][f]);
+      }
     }
+  };
+  const int walks = ceil_div(a.w.groups, kWalk / kMxGroup);
+  const int s_end = min(((int)blockIdx.z + 1) * a.per_slice, walks);
+  const int full = a.k / kWalk;   // (x holds every k of these, and so do the groups)
+  for (int s = blockIdx.z * a.per_slice + wave; s < s_end; s += W) {
+    if (s < full) walk(s, std::false_type{});
+    else walk(s, std::true_type{});
   }
 #pragma unroll
   for (int t = 0; t < MT; ++t)
@@ -113,7 +160,8 @@ __global__ __launch_bounds__(W * 64) void mx_linear_kernel(MxLinear a) {
     for (int w = 1; w < W; ++w) v += part[w][i][lane];
     return v;
   };
-  if (a.swiglu) {
+  const bool sliced = gridDim.z > 1;   // fp32 sums to the scratch, mx_join_kernel does the rest
+  if (a.swiglu && !sliced) {
     constexpr int H = NF > 1 ? NF / 2 : 1;
     for (int i = wave; i < MT * H; i += W) {
       const int t = i / H, f = i % H;
@@ -130,108 +178,388 @@ __global__ __launch_bounds__(W * 64) void mx_linear_kernel(MxLinear a) {
     }
     return;
   }
+  float* out = sliced ? a.slices + (long)blockIdx.z * a.m * a.w.n : reinterpret_cast<float*>(a.y);
+  const long ldo = sliced ? a.w.n : a.ldy;
   for (int i = wave; i < MT * NF; i += W) {
     const int t = i / NF, f = i % NF;
     const f32x4 v = sum(i);
-    const int n = n0 + 16 * f + col;
+    int n = n0 + 16 * f + col;
+    bool ok = n < n_end;
+    if (a.swiglu) {
+      n = n0 + 16 * (f % (NF > 1 ? NF / 2 : 1)) + col;
+      ok = n < n_end;
+      n += 2 * f >= NF ? n_end : 0;
+    }
+    float* o = out + (long)(m0 + 16 * t + 4 * g) * ldo + n;
+    f32x4 old = {0.f, 0.f, 0.f, 0.f};
+    if (a.add && !sliced) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int m = m0 + 16 * t + 4 * g + e;
-      if (m >= a.m || n >= n_end) continue;
-      float* o = reinterpret_cast<float*>(a.y) + (long)m * a.ldy + n;
-      *o = a.add ? *o + v[e] : v[e];
+      for (int e = 0; e < 4; ++e)
+        if (ok && m0 + 16 * t + 4 * g + e < a.m) old[e] = o[e * ldo];
     }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (ok && m0 + 16 * t + 4 * g + e < a.m) o[e * ldo] = old[e] + v[e];
   }
 }
 
-template <int NP>
-hipError_t launch_linear(const MxLinear& a, hipStream_t st) {
+// More rows: one block of WM x WN waves computes 16 MT WM rows x 16 NF WN columns. x goes
+// through LDS in chunks of 128 k by direct loads, three stages of them, shared by all
+// waves; each wave reads its own columns' codes from memory into registers two chunks
+// ahead and unpacks them there (once for 16 MT rows), so the weights need no LDS.
+// Row r of a stage is 256 bytes, its 16-byte slot s stored at s ^ (r & 15): the 16 rows
+// that a fragment reads at one slot come from distinct banks.
+// Blocks of one column tile are 8 apart in the launch (one XCD): its row tiles read the
+// codes through one L2.
+__device__ const uint4 kZeros[1] = {};   // what x holds behind k
+
+template <int WM, int WN, int MT, int NF, int NS, bool PLANES>
+__global__ __launch_bounds__(WM * WN * 64) void mx_tile_kernel(MxLinear a, int n_tiles, int m_tiles) {
+  typedef typename std::conditional<PLANES, float, bf16>::type T;
+  constexpr int NW = WM * WN, BM = 16 * MT * WM, STAGE = BM * 256;
+  constexpr int XL = STAGE / 1024 / NW;    // direct loads of a wave for a stage
+  constexpr int LOADS = XL + 2 * NF;       // memory operations of a wave for a chunk
+  static_assert(STAGE % (1024 * NW) == 0, "whole loads");
+  __shared__ __attribute__((aligned(16))) char smem[NS * STAGE];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int col = lane & 15, g = lane >> 4;
+  const int wm = wave / WN, wn = wave % WN;
+  const int id = blockIdx.x / kXcds;
+  const int n_tile = id / m_tiles * kXcds + blockIdx.x % kXcds;
+  if (n_tile >= n_tiles) return;
+  const int m0 = id % m_tiles * BM;
+  const int n_end = a.swiglu ? a.w.n / 2 : a.w.n;
+  constexpr int H = NF / 2;
+  const int n0 = (n_tile * WN + wn) * (a.swiglu ? 16 * H : 16 * NF);   // the wave's first column
+
+  // Addresses as a base of the wave, which scalar registers hold, and an offset of the
+  // lane in 32 bits; with SwiGLU the second half of the fragments are the up rows.
+  const int n_base = min(n0, n_end - 1);
+  const uint8_t* const codes0 = a.w.codes + (long)n_base * a.w.groups * 16;
+  const uint8_t* const scales0 = a.w.scales + (long)n_base * a.w.scale_ld;
+  const long up_codes = a.swiglu ? (long)n_end * a.w.groups * 16 : 0;
+  const long up_scales = a.swiglu ? (long)n_end * a.w.scale_ld : 0;
+  uint32_t wc[NF], ws[NF];
+#pragma unroll
+  for (int f = 0; f < NF; ++f) {
+    const int n = min(n0 + 16 * (a.swiglu ? f % H : f) + col, n_end - 1) - n_base;
+    wc[f] = (uint32_t)(n * a.w.groups + g) * 16;
+    ws[f] = (uint32_t)n * a.w.scale_ld;
+  }
+  const char* const x0 = reinterpret_cast<const char*>(a.x + (long)m0 * a.ldx);
+  uint32_t xs[XL];         // this lane's slot in each of the wave's direct loads
+#pragma unroll
+  for (int u = 0; u < XL; ++u) {
+    const int r = 4 * (u * NW + wave) + g;
+    xs[u] = (uint32_t)min(r, a.m - 1 - m0) * (uint32_t)a.ldx * 2 + 16 * (col ^ (r & 15));
+  }
+  uint32_t slot[4];        // of the lane's fragments in a row of a stage
+#pragma unroll
+  for (int j = 0; j < 4; ++j) slot[j] = (wm * MT * 16 + col) * 256 + ((4 * j + g) ^ col) * 16;
+  // (the planes of fp32 x are so many products with the same weights, one after the other)
+  const int chunks = ceil_div(a.w.groups, 4);
+  const int c0 = blockIdx.z * a.per_slice, c1 = min(c0 + a.per_slice, chunks * a.planes);
+
+  f32x4 acc[MT][NF];
+#pragma unroll
+  for (int t = 0; t < MT; ++t)
+#pragma unroll
+    for (int f = 0; f < NF; ++f) acc[t][f] = f32x4{0.f, 0.f, 0.f, 0.f};
+  u32x4 codes[NS][NF];
+  uint32_t scales[NS][NF];
+  auto load = [&](int b, int at) {
+    char* dst = smem + b * STAGE + wave * 1024;
+    const int p = PLANES ? at / chunks : 0, c = PLANES ? at % chunks : at;
+    const char* xc = x0 + p * a.plane * 2 + (long)c * 256;
+#pragma unroll
+    for (int u = 0; u < XL; ++u) {   // what lies behind k counts as zero
+      const int k = 128 * c + 8 * (col ^ ((4 * (u * NW + wave) + g) & 15));
+      load_lds16(k < a.k ? xc + xs[u] : reinterpret_cast<const char*>(kZeros), dst + u * NW * 1024);
+    }
+    // (a lane behind the last group reads that one; its scale is set to one and x is zero)
+    const uint32_t back = 16 * max(4 * c + g - (a.w.groups - 1), 0);
+    const uint8_t* cb = codes0 + (long)c * 64;
+    const uint8_t* sb = scales0 + (long)c * 4;
+#pragma unroll
+    for (int f = 0; f < NF; ++f) {
+      codes[b][f] = *reinterpret_cast<const u32x4*>(cb + (f >= H ? up_codes : 0) + (wc[f] - back));
+      scales[b][f] = *reinterpret_cast<const uint32_t*>(sb + (f >= H ? up_scales : 0) + ws[f]);
+    }
+  };
+  auto compute = [&](int b, int at) {
+    const int c = PLANES ? at % chunks : at;
+    const int left = a.w.groups - 4 * c;   // groups of the chunk
+    const uint32_t keep = left >= 4 ? ~0u : (1u << (8 * left)) - 1;
+    u32x4 cd[NF];
+    uint32_t sc[NF];
+#pragma unroll
+    for (int f = 0; f < NF; ++f) {
+      cd[f] = transpose_groups(codes[b][f]);
+      sc[f] = (scales[b][f] & keep) | (0x7f7f7f7fu & ~keep);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      bf16x8 xv[MT], w[NF];
+#pragma unroll
+      for (int t = 0; t < MT; ++t)
+        xv[t] = *reinterpret_cast<const bf16x8*>(smem + slot[j] + b * STAGE + t * 4096);
+#pragma unroll
+      for (int f = 0; f < NF; ++f) w[f] = mx_bf16x8(cd[f][j], mx_scale((sc[f] >> (8 * j)) & 255u));
+#pragma unroll
+      for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int f = 0; f < NF; ++f) acc[t][f] = mfma16_bf16(xv[t], w[f], acc[t][f]);
+    }
+  };
+  // Every step issues the loads of a chunk, past the end those of the last one again: the
+  // waits count loads, and one that some path skips would have to be counted out.
+#pragma unroll
+  for (int b = 0; b < NS - 1; ++b) {
+    load(b, min(c0 + b, c1 - 1));
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  for (int c = c0; c < c1;) {
+#pragma unroll
+    for (int b = 0; b < NS; ++b) {
+      if (c >= c1) break;
+      wait_vmcnt<(NS - 2) * LOADS>();    // chunk c is here, later ones may be in flight,
+      __builtin_amdgcn_s_barrier();      // and every wave is done with c - 1
+      load((b + NS - 1) % NS, min(c + NS - 1, c1 - 1));
+      __builtin_amdgcn_sched_barrier(0);
+      compute(b, c);
+      __builtin_amdgcn_sched_barrier(0);
+      ++c;
+    }
+  }
+  wait_vmcnt<0>();                       // (no load may reach LDS after the block has left it)
+  const bool sliced = gridDim.z > 1;
+  float* out = sliced ? a.slices + (long)blockIdx.z * a.m * a.w.n : reinterpret_cast<float*>(a.y);
+  const long ldo = sliced ? a.w.n : a.ldy;
+#pragma unroll
+  for (int t = 0; t < MT; ++t) {
+    const int m = m0 + (wm * MT + t) * 16 + 4 * g;   // and the three rows behind
+    if (a.swiglu && !sliced) {
+#pragma unroll
+      for (int f = 0; f < H; ++f) {
+        const int n = n0 + 16 * f + col;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (m + e < a.m && n < n_end)
+            reinterpret_cast<T*>(a.y)[(m + e) * a.ldy + n] =
+                from_f32<T>(silu_mul(acc[t][f][e], acc[t][f + H][e]));
+      }
+      continue;
+    }
+    float* o[NF];            // nullptr: a column behind the last
+#pragma unroll
+    for (int f = 0; f < NF; ++f) {
+      const int n = n0 + 16 * (a.swiglu ? f % H : f) + col;
+      o[f] = n < n_end ? out + m * ldo + n + (a.swiglu && f >= H ? n_end : 0) : nullptr;
+    }
+    if (a.add && !sliced) {  // (all of the tile's old values before the first store)
+#pragma unroll
+      for (int f = 0; f < NF; ++f)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (o[f] && m + e < a.m) acc[t][f][e] += o[f][e * ldo];
+    }
+#pragma unroll
+    for (int f = 0; f < NF; ++f)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (o[f] && m + e < a.m) o[f][e * ldo] = acc[t][f][e];
+  }
+}
+
+// The K slices of a product, added in order, and its epilogue: V columns of a row a
+// thread (four where every row of the output starts at a multiple of 16 bytes).
+template <typename T, int V>
+__global__ __launch_bounds__(256) void mx_join_kernel(MxLinear a, int n_slices) {
+  typedef float vec __attribute__((ext_vector_type(V)));
   const int n_out = a.swiglu ? a.w.n / 2 : a.w.n;
-#define MX_LAUNCH(MT_, NF_, W_)                                                              \
-  do {                                                                                       \
-    const int bn_ = a.swiglu ? NF_ * 8 : NF_ * 16;                                           \
-    DLM_LAUNCH((mx_linear_kernel<MT_, NF_, W_, NP>),                                         \
-               dim3(ceil_div(n_out, bn_), ceil_div(a.m, MT_ * 16)), dim3(W_ * 64), 0, st, a); \
-    return hipGetLastError();                                                                \
-  } while (0)
-  if (a.m <= 16) MX_LAUNCH(1, 2, 8);
-  if (a.m <= 32) MX_LAUNCH(2, 2, 8);
-  MX_LAUNCH(4, 2, 8);
-#undef MX_LAUNCH
-}
-
-}  // namespace
-
-namespace {
-template <typename T>
-bool direct_x(const T* x, long ldx, int k) {
-  return sizeof(T) == 2 && k % 8 == 0 && ldx % 8 == 0 && reinterpret_cast<uintptr_t>(x) % 16 == 0;
-}
-}  // namespace
-
-size_t mx_linear_scratch(int elem, int rows, int k, bool aligned) {
-  if (elem == 2 && aligned) return 0;
-  return (size_t)rows * ceil_div(k, kMxGroup) * kMxGroup * 2 * (elem == 2 ? 1 : 3);
-}
-
-template <typename T>
-hipError_t mx_linear(const T* x, long ldx, int rows, const MxView& w, int k, bool swiglu, bool add,
-                     void* y, long ldy, void* scratch, hipStream_t st) {
-  if (rows <= 0 || w.n <= 0) return hipSuccess;
-  MxLinear a{};
-  a.w = w, a.m = rows, a.k = k, a.swiglu = swiglu, a.add = add, a.y = y, a.ldy = ldy;
-  if constexpr (sizeof(T) == 2) {
-    if (direct_x(x, ldx, k)) {
-      a.x = x, a.ldx = ldx;
-      return launch_linear<1>(a, st);
-    }
+  const int n = (blockIdx.x * 256 + threadIdx.x) * V, m = blockIdx.y;
+  if (n >= n_out) return;
+  const long slice = (long)a.m * a.w.n;
+  const float* p = a.slices + (long)m * a.w.n + n;
+  vec v = *reinterpret_cast<const vec*>(p), u = {};
+  if (a.swiglu) u = *reinterpret_cast<const vec*>(p + n_out);
+#pragma unroll 4
+  for (int s = 1; s < n_slices; ++s) {
+    v += *reinterpret_cast<const vec*>(p + s * slice);
+    if (a.swiglu) u += *reinterpret_cast<const vec*>(p + s * slice + n_out);
   }
-  constexpr int NP = sizeof(T) == 2 ? 1 : 3;
-  const int kp = w.groups * kMxGroup;
-  const long total = (long)rows * kp;
-  bf16* xs = reinterpret_cast<bf16*>(scratch);
-  DLM_LAUNCH((mx_stage_kernel<T, NP>), dim3((unsigned)((total + 255) / 256)), dim3(256), 0, st, x,
-             ldx, k, kp, total, xs, total);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  a.x = xs, a.ldx = kp, a.plane = total, a.k = kp;
-  return launch_linear<NP>(a, st);
+  if (a.swiglu) {
+    T* o = reinterpret_cast<T*>(a.y) + (long)m * a.ldy + n;
+#pragma unroll
+    for (int i = 0; i < V; ++i) o[i] = from_f32<T>(silu_mul(v[i], u[i]));
+  } else {
+    vec* o = reinterpret_cast<vec*>(reinterpret_cast<float*>(a.y) + (long)m * a.ldy + n);
+    *o = a.add ? *o + v : v;
+  }
 }
 
-// Above this many rows the matrix is unpacked once and goes through the GEMM kernels.
-constexpr int kMxDirectRows = 256;
+// Launch of a planned product; x of NP planes.
+template <int NP>
+hipError_t launch_linear(MxLinear a, const MxTile& tl, hipStream_t st) {
+  const int n_out = a.swiglu ? a.w.n / 2 : a.w.n;
+  const int cols = a.swiglu ? 8 : 16;    // output columns of a fragment
+  a.planes = NP;
+  dim3 grid;
+  const int steps = tl.kind == kMxFew ? ceil_div(a.w.groups, kWalk / kMxGroup)
+                                      : NP * ceil_div(a.w.groups, 4);
+  a.per_slice = ceil_div(steps, tl.slices);
+  grid.z = ceil_div(steps, a.per_slice);
+  if (tl.kind == kMxFew) {
+    grid.x = ceil_div(n_out, cols * tl.nf), grid.y = ceil_div(a.m, 16 * tl.mt);
+#define MX_FEW(MT_, NF_, W_)                                                                       \
+  if (tl.mt == MT_ && tl.nf == NF_ && tl.waves == W_)                                              \
+  DLM_LAUNCH((mx_linear_kernel<MT_, NF_, W_, NP>), grid, dim3(W_ * 64), 0, st, a)
+    MX_FEW(1, 1, 8);
+    MX_FEW(1, 2, 8);
+    if constexpr (NP == 1) {
+      MX_FEW(1, 4, 8);
+      MX_FEW(1, 4, 4);
+      MX_FEW(2, 1, 8);
+      MX_FEW(2, 2, 8);
+      MX_FEW(2, 4, 8);
+      MX_FEW(2, 4, 4);
+    }
+#undef MX_FEW
+  } else {
+#define MX_TILE(KIND_, WM_, WN_, MT_, NF_, NS_)                                                    \
+  if (tl.kind == KIND_) {                                                                          \
+    const int n_tiles = ceil_div(n_out, cols * NF_ * WN_), m_tiles = ceil_div(a.m, 16 * MT_ * WM_); \
+    grid.x = ceil_div(n_tiles, kXcds) * kXcds * m_tiles, grid.y = 1;                               \
+    DLM_LAUNCH((mx_tile_kernel<WM_, WN_, MT_, NF_, NS_, (NP > 1)>), grid, dim3(WM_ * WN_ * 64), 0, \
+               st, a, n_tiles, m_tiles);                                                           \
+  }
+    MX_TILE(kMxTile64, 1, 4, 4, 2, 3)
+    MX_TILE(kMxTile128, 1, 8, 8, 2, 3)
+#undef MX_TILE
+  }
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || grid.z == 1) return e;
+  typedef typename std::conditional<NP == 1, bf16, float>::type T;
+  // (vector accesses of the slices and of fp32 outputs)
+  const bool v4 = n_out % 4 == 0 && a.ldy % 4 == 0 && reinterpret_cast<uintptr_t>(a.y) % 16 == 0;
+  if (v4)
+    DLM_LAUNCH((mx_join_kernel<T, 4>), dim3(ceil_div(n_out, 1024), a.m), dim3(256), 0, st, a, (int)grid.z);
+  else
+    DLM_LAUNCH((mx_join_kernel<T, 1>), dim3(ceil_div(n_out, 256), a.m), dim3(256), 0, st, a, (int)grid.z);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+// Way of a product. Times in us on MI355X (256 CUs), weights from HBM; what is modelled
+// is what decides between the ways:
+//  * few rows (mx_linear_kernel): 3.5 + the weights at 4.5 TB/s (less while blocks leave
+//    CUs idle) + x, once for each column tile and K slice, at 9 TB/s out of the L2s. So one row takes one
+//    column fragment a block and no slices (4096 x 4096 4.9, with two fragments 6.6),
+//    32 rows four (24576 x 4096 27.4, two 31.7), and a long K slices (4096 x 12288,
+//    16 rows: four fragments in four slices 13.7, one whole 18.4).
+//  * tiles (mx_tile_kernel): 4 + chunks of a slice x (0.67 us for each 64 x 128 block that
+//    a CU runs, at least 0.85; 1.9 for each 128 x 256 block). 24576 x 4096: 64 rows 33
+//    in the small ones, 256 rows 64 in the large ones, 72 in the small ones; 37888 x
+//    3584, 256 rows: 296 large blocks on 256 CUs 114, small ones 91.
+//  * slices cost 2 + 0.8 a MB of them (mx_join_kernel and the stores).
+MxTile mx_tile(int elem, int rows, int n, int k, int groups, bool swiglu, int num_cu) {
+  const int n_out = swiglu ? n / 2 : n, cols = swiglu ? 8 : 16, planes = elem == 2 ? 1 : 3;
+  const double mb = (double)n * groups * 17e-6, x_mb = (double)rows * k * 2e-6 * planes;
+  MxTile best{};
+  double best_t = 1e30;
+  auto take = [&](MxTile t, double us) {
+    if (t.slices > 1) us += 2.0 + 0.8 * t.slices * rows * (double)n * 4e-6;
+    if (us < best_t) best_t = us, best = t;
+  };
+  const int walks = ceil_div(groups, kWalk / kMxGroup), chunks = planes * ceil_div(groups, 4);
+  // (the tiles address their rows in 32 bits, the join its rows in one grid dimension)
+  const bool wide = k > kMxTileK;
+  for (int s = 1; s <= (rows <= 4096 ? 8 : 1); s *= 2) {
+    if (rows <= 32 || planes > 1 || wide) {
+      const int mt = rows <= 16 || planes > 1 ? 1 : 2, m_tiles = ceil_div(rows, 16 * mt);
+      for (int nf = swiglu ? 2 : 1; nf <= (planes > 1 ? 2 : 4); nf *= 2) {
+        if (s > walks) break;
+        const int n_tiles = ceil_div(n_out, cols * nf);
+        const double blocks = (double)n_tiles * m_tiles * s;
+        const double idle = std::max(1.0, 0.875 * num_cu / blocks);
+        const int waves = nf == 4 && blocks > num_cu ? 4 : 8;
+        take({kMxFew, mt, nf, s, waves}, 3.5 + mb * m_tiles * idle / 4.5 + x_mb * n_tiles / 9.0);
+      }
+    }
+    if (s > chunks || wide) continue;
+    const int per = ceil_div(chunks, s);
+    auto rounds = [&](int bm, int bn) {
+      return std::ceil((double)ceil_div(rows, bm) * ceil_div(n_out, bn * cols / 16) * s / num_cu);
+    };
+    take({kMxTile64, 0, 0, s, 0}, 4 + per * std::max(0.85, 0.67 * rounds(64, 128)));
+    take({kMxTile128, 0, 0, s, 0}, 4 + per * 1.9 * rounds(128, 256));
+  }
+  return best;
+}
+
+// From this many rows on a bf16 matrix is unpacked once and goes through the GEMM kernels.
+// Straight from the codes / unpacked (the unpacking included), us: 24576 x 4096 at 1024
+// rows 198 / 233, at 2048 389 / 357; 4096 x 12288 110 / 133 and 202 / 202; 12288 x 4096
+// at 1536 186 / 158. (fp32 stays with the codes: three bf16 products take half
+// of an fp32 one, 24576 x 4096 at 1024 rows 548.)
+constexpr int kMxGemmRows = 1280;
 
 MxPlan mx_plan(int elem, int rows, int n, int k, bool swiglu, bool aligned, int num_cu) {
   MxPlan p;
-  if (aligned && rows > kMxDirectRows && k % (16 / elem) == 0 && (!swiglu || n % 32 == 0)) {
+  if (elem == 2 && aligned && rows >= kMxGemmRows && k % 8 == 0 && (!swiglu || n % 32 == 0)) {
     p.gemm = true;
     p.g = gemm_plan(elem, rows, n, k, false, num_cu, !swiglu, true, !swiglu);
     p.scratch = (size_t)n * k * elem;
-  } else {
-    p.scratch = mx_linear_scratch(elem, rows, k, aligned && k % 8 == 0);
+    return p;
   }
+  const int groups = ceil_div(k, kMxGroup), planes = elem == 2 ? 1 : 3;
+  p.tile = mx_tile(elem, std::max(rows, 1), n, k, groups, swiglu, num_cu);
+  p.staged = elem != 2 || !aligned || k % 8 != 0;
+  if (p.staged) p.stage = ((size_t)rows * groups * kMxGroup * 2 * planes + 255) / 256 * 256;
+  p.scratch = p.stage;
+  if (p.tile.slices > 1) p.scratch += (size_t)p.tile.slices * rows * n * sizeof(float);
   return p;
 }
 
 template <typename T>
 hipError_t mx_matmul(const MxPlan& plan, const T* x, long ldx, int rows, const MxView& w, int k,
                      int epilogue, void* y, long ldy, void* scratch, hipStream_t st) {
+  if (rows <= 0 || w.n <= 0) return hipSuccess;
   const bool swiglu = epilogue == DLM_MX_SWIGLU, add = epilogue == DLM_MX_ADD;
-  if (!plan.gemm) return mx_linear<T>(x, ldx, rows, w, k, swiglu, add, y, ldy, scratch, st);
-  T* dense = reinterpret_cast<T*>(scratch);
-  const hipError_t e = mx_unpack<T>(w, k, dense, k, st);
-  if (e != hipSuccess) return e;
-  if (swiglu)
-    return gemm_swiglu<T>(plan.g, x, (int)ldx, dense, k, rows, w.n / 2, k, reinterpret_cast<T*>(y),
-                          (int)ldy, st);
-  float* c = reinterpret_cast<float*>(y);
-  return add ? gemm_add_f32<T>(plan.g, x, (int)ldx, dense, k, rows, w.n, k, c, (int)ldy, st)
-             : gemm_store_f32<T>(plan.g, x, (int)ldx, dense, k, rows, w.n, k, c, (int)ldy, st);
+  if (plan.gemm) {
+    T* dense = reinterpret_cast<T*>(scratch);
+    const hipError_t e = mx_unpack<T>(w, k, dense, k, st);
+    if (e != hipSuccess) return e;
+    if (swiglu)
+      return gemm_swiglu<T>(plan.g, x, (int)ldx, dense, k, rows, w.n / 2, k, reinterpret_cast<T*>(y),
+                            (int)ldy, st);
+    float* c = reinterpret_cast<float*>(y);
+    return add ? gemm_add_f32<T>(plan.g, x, (int)ldx, dense, k, rows, w.n, k, c, (int)ldy, st)
+               : gemm_store_f32<T>(plan.g, x, (int)ldx, dense, k, rows, w.n, k, c, (int)ldy, st);
+  }
+  constexpr int NP = sizeof(T) == 2 ? 1 : 3;
+  MxLinear a{};
+  a.w = w, a.m = rows, a.k = k, a.swiglu = swiglu, a.add = add, a.y = y, a.ldy = ldy;
+  a.slices = reinterpret_cast<float*>(reinterpret_cast<char*>(scratch) + plan.stage);
+  if (plan.staged) {
+    const int kp = w.groups * kMxGroup;
+    const long total = (long)rows * kp;
+    bf16* xs = reinterpret_cast<bf16*>(scratch);
+    DLM_LAUNCH((mx_stage_kernel<T, NP>), dim3((unsigned)((total + 255) / 256)), dim3(256), 0, st, x,
+               ldx, k, kp, total, xs, total);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    a.x = xs, a.ldx = kp, a.plane = total, a.k = kp;
+  } else if constexpr (NP == 1) {
+    a.x = x, a.ldx = ldx;
+  } else {
+    return hipErrorInvalidValue;
+  }
+  return launch_linear<NP>(a, plan.tile, st);
 }
 
 #define INST(T)                                                                                 \
-  template hipError_t mx_linear<T>(const T*, long, int, const MxView&, int, bool, bool, void*,  \
-                                   long, void*, hipStream_t);                                  \
   template hipError_t mx_matmul<T>(const MxPlan&, const T*, long, int, const MxView&, int, int, \
                                    void*, long, void*, hipStream_t);
 INST(bf16)

@@ -1150,7 +1150,7 @@ dlm_status dlm_mx_linear(int32_t dtype, const void* x, int64_t ldx, int32_t m_ro
                 (long long)ldx, (long long)ldy, w->k, swiglu ? w->n / 2 : w->n);
   const int es = dtype == DLM_BF16 ? 2 : 4;
   const bool al = aligned16(x) && ldx * es % 16 == 0 && w->k * (long)es % 16 == 0 && aligned16(y) &&
-                  ldy % 8 == 0 && ldx < INT32_MAX && ldy < INT32_MAX;
+                  ldy % 8 == 0 && ldx <= kMxTileK && ldy < INT32_MAX;
   const MxPlan plan = mx_plan(es, m_rows, w->n, w->k, swiglu, al, device_cus());
   if (plan.scratch) {
     if (!workspace) return fail(DLM_EINVAL, "workspace is NULL");
