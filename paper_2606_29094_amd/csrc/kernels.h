@@ -245,11 +245,15 @@ hipError_t mx_kv_read(const StepPlan& p, int hkv, int dh, const MxKv& kv, T* k, 
 // Attention of every row over [0, seq_len) of its request's slot (zeros where that is
 // empty). splits > 1: the keys of a request are split over blocks, their partials go to
 // scratch (mx_attention_scratch bytes) and a second kernel joins them.
-int mx_attention_splits(const StepPlan& p, int hq, int hkv, int dh, size_t elem,
-                        size_t scratch_bytes, int num_cu);
+// Blocks of 32 items (16 in fp32; an item is a query row of one head) whose four waves
+// split the keys, or of 64 or 128 items whose waves share the keys.
+enum MxAttnKind { kMxAttnFew, kMxAttnShared64, kMxAttnShared128 };
+struct MxAttnPlan { int kind = kMxAttnFew; int splits = 1; };
+MxAttnPlan mx_attention_plan(const StepPlan& p, int hq, int hkv, int dh, size_t elem,
+                             size_t scratch_bytes, int num_cu);
 size_t mx_attention_scratch(int rows, int hq, int dh, int splits);
 template <typename T>
 hipError_t mx_attention(const StepPlan& p, const T* q, const MxKv& kv, int hq, int hkv, int dh,
-                        T* out, int splits, float* scratch, hipStream_t st);
+                        T* out, MxAttnPlan plan, float* scratch, hipStream_t st);
 
 }  // namespace dlm

@@ -49,6 +49,14 @@ __device__ __forceinline__ u32x4 transpose_groups(u32x4 v) {
   return u32x4{a, b, c, d};
 }
 
+// A block's LDS written before is seen by its other waves; loads from memory stay in
+// flight.
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
 // Scale byte of a group from the largest magnitude's bits (any value's bits without
 // the sign, compared as integers: NaN and infinity come out above every number).
 // e is the exponent that puts the largest magnitude into (3.5, 7] scales, so it

@@ -410,8 +410,8 @@ dlm_status run_forward(dlm_model* m, dlm_cache* c, const dlm_batch* b, const Ste
   T* act = reinterpret_cast<T*>(ws + L.act);
   // part and act (consecutive) hold nothing while attention runs: its key splits' partials go there
   const AttnPlan ap = attention_plan(p, hq, hkv, dh, sizeof(T), L.lm_rows - L.part, m->num_cu);
-  const int mx_splits =
-      c->mx ? mx_attention_splits(p, hq, hkv, dh, sizeof(T), L.lm_rows - L.part, m->num_cu) : 1;
+  const MxAttnPlan mx_ap =
+      c->mx ? mx_attention_plan(p, hq, hkv, dh, sizeof(T), L.lm_rows - L.part, m->num_cu) : MxAttnPlan{};
   const bool w4 = !m->mx.empty();
   void* const mxs = ws + L.mx;
 
@@ -445,7 +445,7 @@ dlm_status run_forward(dlm_model* m, dlm_cache* c, const dlm_batch* b, const Ste
                                  c->s_max, st));
     if (t) TRACE_COPY(t->q, q, (size_t)n * qd * es);
     if (c->mx) {
-      LAUNCH(m, st, "attention", mx_attention<T>(p, q, kv4, hq, hkv, dh, ao, mx_splits, part, st));
+      LAUNCH(m, st, "attention", mx_attention<T>(p, q, kv4, hq, hkv, dh, ao, mx_ap, part, st));
     } else {
       LAUNCH(m, st, "attention", attention<T>(p, q, kc, vc, c->s_max, hq, hkv, dh, ao, ap, part, st));
       if constexpr (sizeof(T) == 2)
@@ -1225,7 +1225,7 @@ dlm_status dlm_mx_kv_attention_workspace(const dlm_cache* c, int32_t n_req, cons
   const dlm_config& cf = m->cfg;
   *out_bytes = mx_attention_scratch(
       p.n_rows, cf.n_q_heads, cf.head_dim,
-      mx_attention_splits(p, cf.n_q_heads, cf.n_kv_heads, cf.head_dim, m->es, SIZE_MAX, m->num_cu));
+      mx_attention_plan(p, cf.n_q_heads, cf.n_kv_heads, cf.head_dim, m->es, SIZE_MAX, m->num_cu).splits);
   return DLM_OK;
 }
 
@@ -1241,9 +1241,9 @@ dlm_status dlm_mx_kv_attention(const dlm_cache* c, int32_t layer, int32_t n_req,
   if (!aligned16(q) || !aligned16(out)) return fail(DLM_EINVAL, "a buffer is not 16-byte aligned");
   const dlm_model* m = c->model;
   const dlm_config& cf = m->cfg;
-  const int splits =
-      mx_attention_splits(p, cf.n_q_heads, cf.n_kv_heads, cf.head_dim, m->es, SIZE_MAX, m->num_cu);
-  const size_t need = mx_attention_scratch(p.n_rows, cf.n_q_heads, cf.head_dim, splits);
+  const MxAttnPlan plan =
+      mx_attention_plan(p, cf.n_q_heads, cf.n_kv_heads, cf.head_dim, m->es, SIZE_MAX, m->num_cu);
+  const size_t need = mx_attention_scratch(p.n_rows, cf.n_q_heads, cf.head_dim, plan.splits);
   if (need) {
     if (!workspace) return fail(DLM_EINVAL, "workspace is NULL");
     if (reinterpret_cast<uintptr_t>(workspace) % 256 != 0)
@@ -1254,11 +1254,11 @@ dlm_status dlm_mx_kv_attention(const dlm_cache* c, int32_t layer, int32_t n_req,
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   if (cf.dtype == DLM_BF16)
     HIPCHECK(mx_attention<bf16>(p, reinterpret_cast<const bf16*>(q), c->mx_layer(layer), cf.n_q_heads,
-                                cf.n_kv_heads, cf.head_dim, reinterpret_cast<bf16*>(out), splits, scratch,
+                                cf.n_kv_heads, cf.head_dim, reinterpret_cast<bf16*>(out), plan, scratch,
                                 st));
   else
     HIPCHECK(mx_attention<float>(p, reinterpret_cast<const float*>(q), c->mx_layer(layer), cf.n_q_heads,
-                                 cf.n_kv_heads, cf.head_dim, reinterpret_cast<float*>(out), splits, scratch,
+                                 cf.n_kv_heads, cf.head_dim, reinterpret_cast<float*>(out), plan, scratch,
                                  st));
   return DLM_OK;
 }

@@ -90,7 +90,9 @@ def attention(q, k, v, dtype):
     """(output, bound) of q [n, hq, dh] over k, v [len, hkv, dh], all 64 bits. The bound: a
     weight is off by the fp32 error of its score (dh / 32 + 6 roundings of the dot product's
     terms, and the scaled difference), its exponential (8 u) and, in bf16 models, its
-    rounding (2^-9); the sums over the keys by one rounding for each 32."""
+    rounding (2^-9); the sums over the keys by one rounding for each 32. A weight below 2^-126
+    of the largest one counts as zero (the exponential has no subnormal results), which
+    takes less than 2^-126 |v| from the output for each key."""
     n, hq, dh = q.shape
     L, hkv = k.shape[0], k.shape[1]
     if L == 0:
@@ -106,7 +108,7 @@ def attention(q, k, v, dtype):
     rel = rel + (2.0 ** -9 if dtype == torch.bfloat16 else 2.0 ** -24)
     o = p @ vh
     # numerator and denominator are each off by rel
-    bound = rel * (p @ vh.abs()) + rel * o.abs()
+    bound = rel * (p @ vh.abs()) + rel * o.abs() + 2.0 ** -126 * vh.abs().sum(1, keepdim=True)
     back = lambda t: t.reshape(hkv, gh, n, dh).permute(2, 0, 1, 3).reshape(n, hq, dh)
     o, bound = back(o), back(bound)
     return o, bound + half_ulp(o, dtype)

@@ -189,7 +189,8 @@ def test_linear_large_offsets(gpu):
     q, w = _packed(gpu, 32, 64)
     y = torch.zeros(3, 400_000_000, device=gpu)
     x = _randn(3, 64, seed=1, dtype=BF16)
-    dlm.mx_linear(x.to(gpu), q, y[:, -32:])
+    ws = torch.empty(max(256, dlm.mx_linear_workspace(BF16, 3, q)), dtype=torch.uint8, device=gpu)
+    dlm.mx_linear(x.to(gpu), q, y[:, -32:], workspace=ws)
     xx = x.double()
     assert bool(((y[:, -32:].cpu().double() - xx @ w.T).abs() <= ref.product_bound(xx, w, BF16)).all())
     assert not y[:, :-32].any()
@@ -383,7 +384,9 @@ def test_attention_nan_keys_reach_their_rows_only(gpu):
     vs[2, 0, 99, 1] = 255
     q = _randn(30, 128, seed=1, dtype=BF16).to(gpu)
     out = torch.empty_like(q)
-    dlm.mx_kv_attention(c.handle, 0, dlm.make_kv_rows([(s, 100, 0, 10) for s in range(3)]), q, out)
+    rows = dlm.make_kv_rows([(s, 100, 0, 10) for s in range(3)])
+    ws = torch.empty(max(256, dlm.mx_kv_attention_workspace(c.handle, rows)), dtype=torch.uint8, device=gpu)
+    dlm.mx_kv_attention(c.handle, 0, rows, q, out, ws)
     nan = out.isnan().view(30, 2, 64).cpu()
     assert not nan[:10].any() and nan[10:20].all()
     assert nan[20:, :, 32:].all() and not nan[20:, :, :32].any()
