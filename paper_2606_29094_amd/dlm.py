@@ -56,6 +56,7 @@ class DlmWeights(ctypes.Structure):
 
 
 class DlmMx(ctypes.Structure):
+    _keep = ()              # the tensors of make_mx
     _fields_ = [("codes", c_void_p), ("scales", c_void_p), ("n", c_int32), ("k", c_int32)]
 
 
@@ -220,6 +221,7 @@ def _stream(stream):
 def load_weights(cfg: DlmConfig, weights: DlmWeights) -> c_void_p:
     h = c_void_p()
     check(lib().dlm_load_weights(ctypes.byref(cfg), ctypes.byref(weights), ctypes.byref(h)))
+    h.config = cfg
     return h
 
 
@@ -368,48 +370,45 @@ def debug_gemm(cfg: int, epilogue: int, a, b, c, sub: int = 0, n_tail: int = 0,
 # ------------------------------------------------- 4-bit operands
 def _dtype_id(dtype) -> int:
     """dlm_dtype of a torch floating type."""
-    name = str(dtype)
-    if name == "torch.bfloat16":
+    import torch
+    if dtype == torch.bfloat16:
         return DLM_BF16
-    if name == "torch.float32":
+    if dtype == torch.float32:
         return DLM_F32
-    raise ValueError(f"{name}: bfloat16 or float32 expected")
+    raise ValueError(f"{dtype}: bfloat16 or float32 expected")
 
 
 def _rows_of(name, t, shape, dtype=None):
     """Row stride of a 2-d device tensor of the given shape (and dtype) with contiguous rows."""
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     if dtype is not None and t.dtype != dtype:
         raise ValueError(f"{name} is {t.dtype}, expected {dtype}")
-    if not t.is_cuda:
-        raise ValueError(f"{name} is not in device memory")
     rows, cols = shape
-    ld = t.stride(0) if rows > 1 else max(cols, t.stride(0))
-    if (cols > 1 and t.stride(1) != 1) or ld < cols:
+    ld, step = t.stride()
+    if rows < 2:
+        ld = max(cols, ld)
+    if (cols > 1 and step != 1) or ld < cols:
         raise ValueError(f"{name} has strides {t.stride()}: contiguous, disjoint rows expected")
     return ld
 
 
 def _flat(name, t, shape, dtype):
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+    if t.shape != shape or t.dtype != dtype:
         raise ValueError(f"{name} is {t.dtype} {tuple(t.shape)}, expected {dtype} {tuple(shape)}")
-    if not t.is_cuda or not t.is_contiguous():
-        raise ValueError(f"{name} is not a contiguous device tensor")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} is not contiguous")
 
 
 def _on(stream, *tensors):
-    """The stream argument of a call on these tensors: the given one, or the current stream of
-    their device (which becomes the current device of the call)."""
+    """The stream argument of a call on these tensors, which have to be on the current device:
+    the given one, or that device's current stream."""
     import torch
-    dev = tensors[0].device
-    for t in tensors[1:]:
-        if t.device != dev:
-            raise ValueError(f"tensors on {dev} and {t.device}")
-    if dev.index != torch.cuda.current_device():
-        raise ValueError(f"tensors on {dev}, but the current device is {torch.cuda.current_device()}")
-    return c_void_p(stream if stream is not None else
-                    torch.cuda.current_stream(dev).cuda_stream)
+    dev = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else -2
+    for t in tensors:
+        if t.get_device() != dev:
+            raise ValueError(f"a tensor is on {t.device}, not on the current GPU")
+    return stream if stream is not None else torch._C._cuda_getCurrentRawStream(dev)
 
 
 def mx_bytes(n: int, k: int):
@@ -436,15 +435,15 @@ def make_mx(codes, scales, n: int, k: int) -> DlmMx:
 def mx_pack(w, q: DlmMx, stream=None):
     """Pack the [n, k] tensor w (bf16 or fp32, contiguous rows) into q's buffers."""
     ld = _rows_of("w", w, (q.n, q.k))
-    check(lib().dlm_mx_pack(_dtype_id(w.dtype), _ptr(w), ld, ctypes.byref(q),
-                            _on(stream, w, q._keep[0])))
+    check(lib().dlm_mx_pack(_dtype_id(w.dtype), w.data_ptr(), ld, ctypes.byref(q),
+                            _on(stream, w, *q._keep)))
 
 
 def mx_unpack(q: DlmMx, out, stream=None):
     """The packed values, in out's dtype."""
     ld = _rows_of("out", out, (q.n, q.k))
-    check(lib().dlm_mx_unpack(ctypes.byref(q), _dtype_id(out.dtype), _ptr(out), ld,
-                              _on(stream, out, q._keep[0])))
+    check(lib().dlm_mx_unpack(ctypes.byref(q), _dtype_id(out.dtype), out.data_ptr(), ld,
+                              _on(stream, out, *q._keep)))
 
 
 def mx_linear_workspace(dtype, m_rows: int, q: DlmMx, epilogue: int = DLM_MX_STORE) -> int:
@@ -458,20 +457,24 @@ def mx_linear(x, q: DlmMx, y, epilogue: int = DLM_MX_STORE, workspace=None, stre
     """y = x @ values.T (fp32), y += x @ values.T (fp32), or silu(gate) * up in x's
     dtype; workspace: at least mx_linear_workspace bytes, or None where that is 0."""
     import torch
-    m = x.shape[0]
+    m, dt = x.shape[0], x.dtype
     ldx = _rows_of("x", x, (m, q.k))
-    swiglu = epilogue == DLM_MX_SWIGLU
-    ldy = _rows_of("y", y, (m, q.n // 2 if swiglu else q.n), x.dtype if swiglu else torch.float32)
-    ws, n = (None, 0) if workspace is None else (workspace, workspace.numel() *
-                                                 workspace.element_size())
-    check(lib().dlm_mx_linear(_dtype_id(x.dtype), _ptr(x), ldx, m, ctypes.byref(q), epilogue,
-                              _ptr(y), ldy, _ptr(ws), n,
-                              _on(stream, x, y, q._keep[0], *(() if ws is None else (ws,)))))
+    if epilogue == DLM_MX_SWIGLU:
+        ldy = _rows_of("y", y, (m, q.n // 2), dt)
+    else:
+        ldy = _rows_of("y", y, (m, q.n), torch.float32)
+    if workspace is None:
+        st, ws, size = _on(stream, x, y, *q._keep), None, 0
+    else:
+        st, ws, size = _on(stream, x, y, workspace, *q._keep), workspace.data_ptr(), workspace.nbytes
+    check(lib().dlm_mx_linear(_dtype_id(dt), x.data_ptr(), ldx, m, ctypes.byref(q), epilogue,
+                              y.data_ptr(), ldy, ws, size, st))
 
 
 def load_weights_mx(cfg: DlmConfig, weights: DlmWeightsMx) -> c_void_p:
     h = c_void_p()
     check(lib().dlm_load_weights_mx(ctypes.byref(cfg), ctypes.byref(weights), ctypes.byref(h)))
+    h.config = cfg
     return h
 
 
@@ -481,35 +484,46 @@ def kv_cache_alloc_mx(model, n_slots: int, max_seq_len: int, dev_buf=None, buf_b
     h = c_void_p()
     check(lib().dlm_kv_cache_alloc_mx(model, n_slots, max_seq_len, _ptr(dev_buf), buf_bytes,
                                       ctypes.byref(req), ctypes.byref(h)))
+    h.config = model.config
     return (h if dev_buf is not None else None), req.value
+
+
+def _heads(cache):
+    """(query width, key/value width, rotary pairs, torch dtype) of a 4-bit cache's model."""
+    import torch
+    c = cache.config
+    return (c.n_q_heads * c.head_dim, c.n_kv_heads * c.head_dim, c.head_dim // 2,
+            torch.bfloat16 if c.dtype == DLM_BF16 else torch.float32)
 
 
 def make_kv_rows(rows):
     """[(slot, seq_len, pos0, n_rows)] as the argument of the mx_kv calls."""
-    return (DlmKvRows * len(rows))(*[DlmKvRows(*r) for r in rows])
+    arr = (DlmKvRows * len(rows))(*[DlmKvRows(*r) for r in rows])
+    arr.total = sum(r[3] for r in rows)        # N, read by every call on these requests
+    return arr
 
 
 def mx_kv_append(cache, layer: int, rows, qkv, rot, q_out, stream=None):
-    """qkv fp32 [splits, N, D] or [N, D], rot fp32 [N, head_dim / 2, 2], q_out [N, n_q_heads head_dim]."""
+    """qkv fp32 [splits, N, (n_q_heads + 2 n_kv_heads) head_dim] or without splits, rot fp32
+    [N, head_dim / 2, 2], q_out [N, n_q_heads head_dim] in the model dtype. rows: make_kv_rows."""
     import torch
-    n = sum(r.n_rows for r in rows)
+    n, (qd, kd, pairs, dt) = rows.total, _heads(cache)
     splits = qkv.shape[0] if qkv.dim() == 3 else 1
-    for name, t in (("qkv", qkv), ("rot", rot)):
-        _flat(name, t, t.shape, torch.float32)
-    if qkv.shape[-2] != n or rot.shape[0] != n:
-        raise ValueError(f"qkv {tuple(qkv.shape)}, rot {tuple(rot.shape)}: the requests have {n} rows")
-    _flat("q_out", q_out, (n, q_out.shape[-1]), q_out.dtype)
-    check(lib().dlm_mx_kv_append(cache, layer, len(rows), rows, _ptr(qkv), splits, _ptr(rot),
-                                 _ptr(q_out), _on(stream, qkv, rot, q_out)))
+    _flat("qkv", qkv, (splits, n, qd + 2 * kd) if qkv.dim() == 3 else (n, qd + 2 * kd), torch.float32)
+    _flat("rot", rot, (n, pairs, 2), torch.float32)
+    _flat("q_out", q_out, (n, qd), dt)
+    st = _on(stream, qkv, rot, q_out)
+    check(lib().dlm_mx_kv_append(cache, layer, len(rows), rows, qkv.data_ptr(), splits,
+                                 rot.data_ptr(), q_out.data_ptr(), st))
 
 
 def mx_kv_read(cache, layer: int, rows, k_out, v_out, stream=None):
     """The stored keys and values of the rows' positions, [N, n_kv_heads head_dim]."""
-    n = sum(r.n_rows for r in rows)
-    for name, t in (("k_out", k_out), ("v_out", v_out)):
-        _flat(name, t, (n, t.shape[-1]), k_out.dtype)
-    check(lib().dlm_mx_kv_read(cache, layer, len(rows), rows, _ptr(k_out), _ptr(v_out),
-                               _on(stream, k_out, v_out)))
+    n, (_, kd, _, dt) = rows.total, _heads(cache)
+    _flat("k_out", k_out, (n, kd), dt)
+    _flat("v_out", v_out, (n, kd), dt)
+    st = _on(stream, k_out, v_out)
+    check(lib().dlm_mx_kv_read(cache, layer, len(rows), rows, k_out.data_ptr(), v_out.data_ptr(), st))
 
 
 def mx_kv_attention_workspace(cache, rows) -> int:
@@ -519,14 +533,16 @@ def mx_kv_attention_workspace(cache, rows) -> int:
 
 
 def mx_kv_attention(cache, layer: int, rows, q, out, workspace=None, stream=None):
-    """out = attention of q over the 4-bit cache; both [N, n_q_heads head_dim]."""
-    n = sum(r.n_rows for r in rows)
-    _flat("q", q, (n, q.shape[-1]), q.dtype)
-    _flat("out", out, q.shape, q.dtype)
-    ws, size = (None, 0) if workspace is None else (workspace, workspace.numel() *
-                                                    workspace.element_size())
-    check(lib().dlm_mx_kv_attention(cache, layer, len(rows), rows, _ptr(q), _ptr(out), _ptr(ws), size,
-                                    _on(stream, q, out, *(() if ws is None else (ws,)))))
+    """out = attention of q over the 4-bit cache; both [N, n_q_heads head_dim]; workspace: at
+    least mx_kv_attention_workspace bytes, or None where that is 0."""
+    n, (qd, _, _, dt) = rows.total, _heads(cache)
+    _flat("q", q, (n, qd), dt)
+    _flat("out", out, (n, qd), dt)
+    if workspace is None:
+        st, ws, size = _on(stream, q, out), None, 0
+    else:
+        st, ws, size = _on(stream, q, out, workspace), workspace.data_ptr(), workspace.nbytes
+    check(lib().dlm_mx_kv_attention(cache, layer, len(rows), rows, q.data_ptr(), out.data_ptr(), ws, size, st))
 
 
 def profile_enable(model, on: bool, only_class: str | None = None):

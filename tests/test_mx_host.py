@@ -238,3 +238,20 @@ def test_binding_refuses_host_tensors_and_shapes():
         dlm.make_mx(torch.zeros(8, 32, dtype=torch.uint8), torch.zeros(8, 16, dtype=torch.uint8), 8, 64)
     with pytest.raises(ValueError):
         dlm.mx_linear_workspace(torch.float16, 4, q)
+
+
+def test_binding_refuses_other_widths_and_types(cache):
+    """What the model's heads and type do not fit is refused before its address is used."""
+    r = dlm.make_kv_rows([(0, 10, 0, 2)])
+    qkv, rot = torch.zeros(1, 2, 512), torch.zeros(2, 32, 2)
+    q, k = torch.zeros(2, 256, dtype=torch.bfloat16), torch.zeros(2, 128, dtype=torch.bfloat16)
+    for a in [(qkv[:, :, :511], rot, q), (qkv[:, :1], rot, q), (qkv, rot[:1], q), (qkv, rot[:, :31], q),
+              (qkv, rot, q.float()), (qkv, rot, q[:, :255]), (qkv.double(), rot, q), (qkv, rot, q)]:
+        with pytest.raises(ValueError):      # (the last one: not in device memory)
+            dlm.mx_kv_append(cache, 0, r, *a)
+    for a in [(k.float(), k), (k, k[:1]), (k[:, :64], k), (k, k)]:
+        with pytest.raises(ValueError):
+            dlm.mx_kv_read(cache, 0, r, *a)
+    for a in [(q.float(), q), (q, q[:, ::2]), (q[:1], q), (q, q)]:
+        with pytest.raises(ValueError):
+            dlm.mx_kv_attention(cache, 0, r, *a)
