@@ -2,6 +2,8 @@
 // rotated keys and values, reading them back. Part of rowwise.hip.
 #pragma once
 
+#include <algorithm>
+
 #include "kernels.h"
 #include "mx_common.h"
 
@@ -10,28 +12,92 @@ namespace dlm {
 namespace {
 
 // ------------------------------------------------------------ pack, unpack --
-// One thread per group: 32 values, 16 bytes of codes, a scale byte. Streaming;
-// bound by memory. Threads of the padding groups of a row clear its scale bytes.
-template <typename T>
-__device__ __forceinline__ void load_group(const T* p, int n, bool vec, float (&x)[kMxGroup]) {
-  if (vec && n >= kMxGroup) {
-    constexpr int V = 16 / sizeof(T);
-    typedef T vt __attribute__((ext_vector_type(V)));
-#pragma unroll
-    for (int i = 0; i < kMxGroup / V; ++i) {
-      const vt v = reinterpret_cast<const vt*>(p)[i];
-#pragma unroll
-      for (int j = 0; j < V; ++j) x[i * V + j] = to_f32((T)v[j]);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < kMxGroup; ++i) x[i] = i < n ? to_f32(p[i]) : 0.f;
-  }
+// Bound by memory. Rows whose vectors are aligned: a lane takes 16 bytes of the wide
+// matrix, so a group is held by four lanes (bf16) or eight (fp32) that find its largest
+// magnitude by exchanges within the row of lanes, and the wide matrix moves in whole
+// lines. (One thread for each group, its lines in 64- and 128-byte strides: 4096 x 4096
+// bf16, both directions 25.5 us, 37888 x 3584 fp32 340.) Other rows: one thread for each group.
+constexpr int kPackVecs = 4;             // vectors of a thread, loaded together
+
+// largest of the 16 / sizeof(T) lanes that hold a group
+template <int LANES>
+__device__ __forceinline__ uint32_t group_max(uint32_t v) {
+  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xb1, 0xf, 0xf, true));   // lane ^ 1
+  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4e, 0xf, 0xf, true));   // lane ^ 2
+  if constexpr (LANES == 8)
+    v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x141, 0xf, 0xf, true));  // 7 - lane
+  return v;
 }
 
 template <typename T>
 __global__ __launch_bounds__(256) void mx_pack_kernel(const T* __restrict__ w, long ldw, int k,
-                                                      int vec, MxView o, long total) {
+                                                      MxView o) {
+  constexpr int V = 16 / sizeof(T), LANES = kMxGroup / V;
+  typedef T vt __attribute__((ext_vector_type(V)));
+  const int vecs = o.groups * LANES;
+  const int at0 = blockIdx.x * 256 * kPackVecs + threadIdx.x;
+  for (long row = blockIdx.y; row < o.n; row += gridDim.y) {
+    vt x[kPackVecs];
+#pragma unroll
+    for (int u = 0; u < kPackVecs; ++u) {
+      const int at = at0 + u * 256;
+      x[u] = at * V < k ? *reinterpret_cast<const vt*>(w + row * ldw + at * V) : vt{};
+    }
+#pragma unroll
+    for (int u = 0; u < kPackVecs; ++u) {
+      const int at = at0 + u * 256;       // (all lanes of a group are in or out)
+      uint32_t amax = 0;
+#pragma unroll
+      for (int i = 0; i < V; ++i) amax = max(amax, __float_as_uint(to_f32((T)x[u][i])) & 0x7fffffffu);
+      const uint32_t e = mx_scale_byte(group_max<LANES>(amax));
+      if (at >= vecs) continue;
+      const float s = mx_scale(e);
+      uint32_t c[V / 4];
+#pragma unroll
+      for (int i = 0; i < V / 4; ++i)
+        c[i] = e == 255u ? 0u : mx_codes4(to_f32((T)x[u][4 * i]), to_f32((T)x[u][4 * i + 1]),
+                                          to_f32((T)x[u][4 * i + 2]), to_f32((T)x[u][4 * i + 3]), s);
+      uint8_t* codes = o.codes + row * o.groups * 16 + at * (V / 2);
+      if constexpr (V == 8) *reinterpret_cast<uint32_t*>(codes) = c[0] | c[1] << 16;
+      else *reinterpret_cast<uint16_t*>(codes) = (uint16_t)c[0];
+      if (at % LANES == 0) o.scales[row * o.scale_ld + at / LANES] = (uint8_t)e;
+    }
+    const int g = o.groups + threadIdx.x;   // the row's padding scales
+    if (blockIdx.x == 0 && g < o.scale_ld) o.scales[row * o.scale_ld + g] = 0;
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void mx_unpack_kernel(MxView w, int k, T* __restrict__ out, long ldo) {
+  constexpr int V = 16 / sizeof(T), LANES = kMxGroup / V;
+  typedef T vt __attribute__((ext_vector_type(V)));
+  const int at0 = blockIdx.x * 256 * kPackVecs + threadIdx.x;
+  for (long row = blockIdx.y; row < w.n; row += gridDim.y) {
+    uint32_t c[kPackVecs], e[kPackVecs];
+#pragma unroll
+    for (int u = 0; u < kPackVecs; ++u) {
+      const int at = at0 + u * 256;
+      if (at * V >= k) continue;
+      const uint8_t* p = w.codes + row * w.groups * 16 + at * (V / 2);
+      c[u] = V == 8 ? *reinterpret_cast<const uint32_t*>(p) : *reinterpret_cast<const uint16_t*>(p);
+      e[u] = w.scales[row * w.scale_ld + at / LANES];
+    }
+#pragma unroll
+    for (int u = 0; u < kPackVecs; ++u) {
+      const int at = at0 + u * 256;
+      if (at * V >= k) continue;
+      const bf16x8 x = mx_bf16x8(c[u], mx_scale(e[u]));
+      vt v;
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[i] = (T)(float)x[i];
+      *reinterpret_cast<vt*>(out + row * ldo + at * V) = v;
+    }
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void mx_pack_any_kernel(const T* __restrict__ w, long ldw, int k,
+                                                          MxView o, long total) {
   const long at = (long)blockIdx.x * 256 + threadIdx.x;
   if (at >= total) return;
   const long row = at / o.scale_ld;
@@ -40,11 +106,15 @@ __global__ __launch_bounds__(256) void mx_pack_kernel(const T* __restrict__ w, l
     o.scales[at] = 0;
     return;
   }
+  const T* p = w + row * ldw + g * kMxGroup;
+  const int n = k - g * kMxGroup;
   float x[kMxGroup];
-  load_group(w + row * ldw + g * kMxGroup, k - g * kMxGroup, vec != 0, x);
   uint32_t amax = 0;
 #pragma unroll
-  for (int i = 0; i < kMxGroup; ++i) amax = max(amax, __float_as_uint(x[i]) & 0x7fffffffu);
+  for (int i = 0; i < kMxGroup; ++i) {
+    x[i] = i < n ? to_f32(p[i]) : 0.f;
+    amax = max(amax, __float_as_uint(x[i]) & 0x7fffffffu);
+  }
   const uint32_t e = mx_scale_byte(amax);
   const float s = mx_scale(e);
   u32x4 c;
@@ -58,8 +128,8 @@ __global__ __launch_bounds__(256) void mx_pack_kernel(const T* __restrict__ w, l
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void mx_unpack_kernel(MxView w, int k, int vec,
-                                                        T* __restrict__ out, long ldo, long total) {
+__global__ __launch_bounds__(256) void mx_unpack_any_kernel(MxView w, int k, T* __restrict__ out,
+                                                            long ldo, long total) {
   const long at = (long)blockIdx.x * 256 + threadIdx.x;
   if (at >= total) return;
   const long row = at / w.groups;
@@ -71,20 +141,9 @@ __global__ __launch_bounds__(256) void mx_unpack_kernel(MxView w, int k, int vec
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const bf16x8 v = mx_bf16x8(c[i], s);
-    if (vec && n >= kMxGroup) {
-      if constexpr (sizeof(T) == 2) {
-        reinterpret_cast<bf16x8*>(o)[i] = v;
-      } else {
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-          reinterpret_cast<f32x4*>(o)[2 * i + h] = f32x4{(float)v[4 * h], (float)v[4 * h + 1],
-                                                         (float)v[4 * h + 2], (float)v[4 * h + 3]};
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (8 * i + j < n) o[8 * i + j] = (T)(float)v[j];
-    }
+    for (int j = 0; j < 8; ++j)
+      if (8 * i + j < n) o[8 * i + j] = (T)(float)v[j];
   }
 }
 
@@ -187,21 +246,39 @@ __global__ __launch_bounds__(256) void mx_read_kernel(StepPlan p, int hkv, MxKv 
 
 }  // namespace
 
+// whether rows of k elements, ld apart, are whole 16-byte vectors (whose index fits in int)
+template <typename T>
+static bool whole_vectors(const T* p, long ld, int k) {
+  constexpr int V = 16 / sizeof(T);
+  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % V == 0 && k % V == 0 && k < (1 << 30);
+}
+
+template <typename T>
+static dim3 pack_grid(const MxView& w) {
+  return dim3(ceil_div(w.groups * (kMxGroup / (16 / (int)sizeof(T))), 256 * kPackVecs), std::min(w.n, 65535));
+}
+
 template <typename T>
 hipError_t mx_pack(const T* w, long ldw, int k, const MxView& o, hipStream_t st) {
-  const long total = (long)o.n * o.scale_ld;
-  const int vec = reinterpret_cast<uintptr_t>(w) % 16 == 0 && ldw * sizeof(T) % 16 == 0;
-  DLM_LAUNCH(mx_pack_kernel<T>, dim3((unsigned)((total + 255) / 256)), dim3(256), 0, st, w, ldw, k,
-             vec, o, total);
+  if (whole_vectors(w, ldw, k)) {
+    DLM_LAUNCH(mx_pack_kernel<T>, pack_grid<T>(o), dim3(256), 0, st, w, ldw, k, o);
+  } else {
+    const long total = (long)o.n * o.scale_ld;
+    DLM_LAUNCH(mx_pack_any_kernel<T>, dim3((unsigned)((total + 255) / 256)), dim3(256), 0, st, w, ldw, k,
+               o, total);
+  }
   return hipGetLastError();
 }
 
 template <typename T>
 hipError_t mx_unpack(const MxView& w, int k, T* out, long ldo, hipStream_t st) {
-  const long total = (long)w.n * w.groups;
-  const int vec = reinterpret_cast<uintptr_t>(out) % 16 == 0 && ldo * sizeof(T) % 16 == 0;
-  DLM_LAUNCH(mx_unpack_kernel<T>, dim3((unsigned)((total + 255) / 256)), dim3(256), 0, st, w, k, vec,
-             out, ldo, total);
+  if (whole_vectors(out, ldo, k)) {
+    DLM_LAUNCH(mx_unpack_kernel<T>, pack_grid<T>(w), dim3(256), 0, st, w, k, out, ldo);
+  } else {
+    const long total = (long)w.n * w.groups;
+    DLM_LAUNCH(mx_unpack_any_kernel<T>, dim3((unsigned)((total + 255) / 256)), dim3(256), 0, st, w, k,
+               out, ldo, total);
+  }
   return hipGetLastError();
 }
 
