@@ -204,8 +204,7 @@ __global__ __launch_bounds__(256) void mx_append_kernel(StepPlan p, const float*
     uint32_t amax = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) amax = max(amax, __float_as_uint(x[j]) & 0x7fffffffu);
-#pragma unroll
-    for (int o = 1; o < 8; o <<= 1) amax = max(amax, (uint32_t)__shfl_xor((int)amax, o, kWave));
+    amax = group_max<8>(amax);
     const uint32_t e = mx_scale_byte(amax);
     const uint32_t w = e == 255u ? 0u : mx_codes4(x[0], x[1], x[2], x[3], mx_scale(e));
     const int d = i + h * HALF;
@@ -214,34 +213,27 @@ __global__ __launch_bounds__(256) void mx_append_kernel(StepPlan p, const float*
   }
 }
 
-// The stored values: one thread per group.
+// The stored values: a lane writes 16 bytes of them, so that a wave's stores are whole lines.
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void mx_read_kernel(StepPlan p, int hkv, MxKv kv,
                                                       T* __restrict__ k, T* __restrict__ v) {
-  constexpr int GROUPS = DH / kMxGroup;
+  constexpr int GROUPS = DH / kMxGroup, V = 16 / sizeof(T), VECS = DH / V;   // vectors of a head
+  typedef T vt __attribute__((ext_vector_type(V)));
   const int row = blockIdx.x;
   const int r = plan_req_of_row(p, row);
   const ReqPlan& q = p.r[r];
-  for (int i = threadIdx.x; i < 2 * hkv * GROUPS; i += 256) {
-    const bool is_v = i >= hkv * GROUPS;
-    const int j = i - (is_v ? hkv * GROUPS : 0), head = j / GROUPS, g = j % GROUPS;
-    const long at = ((long)q.slot * hkv + head) * kv.s_max + q.pos0 + (row - q.row0);
-    const u32x4 c = reinterpret_cast<const u32x4*>(is_v ? kv.vc : kv.kc)[at * GROUPS + g];
-    const float s = mx_scale((is_v ? kv.vs : kv.ks)[at * GROUPS + g]);
-    T* o = (is_v ? v : k) + (long)row * hkv * DH + head * DH + g * kMxGroup;
+  const int i = blockIdx.y * 256 + threadIdx.x;
+  if (i >= 2 * hkv * VECS) return;
+  const bool is_v = i >= hkv * VECS;
+  const int j = i - (is_v ? hkv * VECS : 0), head = j / VECS, x = j % VECS;
+  const long at = ((long)q.slot * hkv + head) * kv.s_max + q.pos0 + (row - q.row0);
+  const uint8_t* c = (is_v ? kv.vc : kv.kc) + at * (DH / 2) + x * (V / 2);
+  const uint32_t w = V == 8 ? *reinterpret_cast<const uint32_t*>(c) : *reinterpret_cast<const uint16_t*>(c);
+  const bf16x8 b = mx_bf16x8(w, mx_scale((is_v ? kv.vs : kv.ks)[at * GROUPS + x * V / kMxGroup]));
+  vt o;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const bf16x8 x = mx_bf16x8(c[w], s);
-      if constexpr (sizeof(T) == 2) {
-        reinterpret_cast<bf16x8*>(o)[w] = x;
-      } else {
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-          reinterpret_cast<f32x4*>(o)[2 * w + h] =
-              f32x4{(float)x[4 * h], (float)x[4 * h + 1], (float)x[4 * h + 2], (float)x[4 * h + 3]};
-      }
-    }
-  }
+  for (int e = 0; e < V; ++e) o[e] = (T)(float)b[e];
+  *reinterpret_cast<vt*>((is_v ? v : k) + (long)row * hkv * DH + j * V) = o;
 }
 
 }  // namespace
@@ -303,10 +295,11 @@ template <typename T>
 hipError_t mx_kv_read(const StepPlan& p, int hkv, int dh, const MxKv& kv, T* k, T* v,
                       hipStream_t st) {
   if (p.n_rows == 0) return hipSuccess;
+  const dim3 grid(p.n_rows, ceil_div(2 * hkv * dh / (16 / (int)sizeof(T)), 256));
   if (dh == 128)
-    DLM_LAUNCH((mx_read_kernel<T, 128>), dim3(p.n_rows), dim3(256), 0, st, p, hkv, kv, k, v);
+    DLM_LAUNCH((mx_read_kernel<T, 128>), grid, dim3(256), 0, st, p, hkv, kv, k, v);
   else if (dh == 64)
-    DLM_LAUNCH((mx_read_kernel<T, 64>), dim3(p.n_rows), dim3(256), 0, st, p, hkv, kv, k, v);
+    DLM_LAUNCH((mx_read_kernel<T, 64>), grid, dim3(256), 0, st, p, hkv, kv, k, v);
   else
     return hipErrorInvalidValue;
   return hipGetLastError();
