@@ -204,14 +204,16 @@ enum { kMxFew, kMxTile64, kMxTile128 };
 constexpr int kMxTileK = 1 << 24;   // the tiles take rows (and row strides) of up to that many elements
 struct MxTile { int kind, mt, nf, slices, waves; };
 struct MxPlan {
-  bool gemm = false, staged = false;
+  bool gemm = false, staged = false, join = true;
   GemmPlan g{};
   MxTile tile{};
   size_t stage = 0, scratch = 0;
 };
 // aligned: x (and y) start at multiples of 16 bytes, as do their rows, at most kMxTileK
-// elements apart
-MxPlan mx_plan(int elem, int rows, int n, int k, bool swiglu, bool aligned, int num_cu);
+// elements apart. join: K slices are added by the product; otherwise (DLM_MX_STORE alone)
+// y takes tile.slices of them, [slices, rows, n], for a consumer that adds them.
+MxPlan mx_plan(int elem, int rows, int n, int k, bool swiglu, bool aligned, bool join,
+               int num_cu);
 // epilogue: dlm_mx_epilogue
 template <typename T>
 hipError_t mx_matmul(const MxPlan& plan, const T* x, long ldx, int rows, const MxView& w, int k,

@@ -297,18 +297,39 @@ __global__ __launch_bounds__(WM * WN * 64) void mx_tile_kernel(MxLinear a, int n
       cd[f] = transpose_groups(codes[b][f]);
       sc[f] = (scales[b][f] & keep) | (0x7f7f7f7fu & ~keep);
     }
+    // In the large tiles the fragments of step j + 1 are read and unpacked between the
+    // MFMAs of step j (3584 x 18944, 1000 rows 157 -> 151 us; the small tiles, three of
+    // which share a CU, lose by it: 37888 x 3584, 256 rows 91 -> 97).
+    constexpr int AHEAD = MT >= 8 ? 1 : 0;
+    bf16x8 xv[AHEAD + 1][MT], w[AHEAD + 1][NF];
+    auto fetch = [&](int j) {
+#pragma unroll
+      for (int t = 0; t < MT; ++t)
+        xv[j & AHEAD][t] = *reinterpret_cast<const bf16x8*>(smem + slot[j] + b * STAGE + t * 4096);
+#pragma unroll
+      for (int f = 0; f < NF; ++f)
+        w[j & AHEAD][f] = mx_bf16x8(cd[f][j], mx_scale((sc[f] >> (8 * j)) & 255u));
+    };
+    if (AHEAD) fetch(0);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      bf16x8 xv[MT], w[NF];
-#pragma unroll
-      for (int t = 0; t < MT; ++t)
-        xv[t] = *reinterpret_cast<const bf16x8*>(smem + slot[j] + b * STAGE + t * 4096);
-#pragma unroll
-      for (int f = 0; f < NF; ++f) w[f] = mx_bf16x8(cd[f][j], mx_scale((sc[f] >> (8 * j)) & 255u));
+      if (j + AHEAD < 4) fetch(j + AHEAD);
 #pragma unroll
       for (int t = 0; t < MT; ++t)
 #pragma unroll
-        for (int f = 0; f < NF; ++f) acc[t][f] = mfma16_bf16(xv[t], w[f], acc[t][f]);
+        for (int f = 0; f < NF; ++f)
+          acc[t][f] = mfma16_bf16(xv[j & AHEAD][t], w[j & AHEAD][f], acc[t][f]);
+    }
+    if constexpr (AHEAD) {   // the order asked for: LDS reads, MFMAs and vector work in turn
+      __builtin_amdgcn_sched_group_barrier(0x100, MT, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, 8 * NF, 0);
+#pragma unroll
+      for (int i = 0; i < 3 * MT; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, NF, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, (6 * NF + MT - 1) / MT, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x008, MT * NF, 0);
     }
   };
   // Every step issues the loads of a chunk, past the end those of the last one again: the
@@ -400,7 +421,7 @@ __global__ __launch_bounds__(256) void mx_join_kernel(MxLinear a, int n_slices) 
 
 // Launch of a planned product; x of NP planes.
 template <int NP>
-hipError_t launch_linear(MxLinear a, const MxTile& tl, hipStream_t st) {
+hipError_t launch_linear(MxLinear a, const MxTile& tl, bool join, hipStream_t st) {
   const int n_out = a.swiglu ? a.w.n / 2 : a.w.n;
   const int cols = a.swiglu ? 8 : 16;    // output columns of a fragment
   a.planes = NP;
@@ -438,7 +459,7 @@ hipError_t launch_linear(MxLinear a, const MxTile& tl, hipStream_t st) {
 #undef MX_TILE
   }
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || grid.z == 1) return e;
+  if (e != hipSuccess || grid.z == 1 || !join) return e;
   typedef typename std::conditional<NP == 1, bf16, float>::type T;
   // (vector accesses of the slices and of fp32 outputs)
   const bool v4 = n_out % 4 == 0 && a.ldy % 4 == 0 && reinterpret_cast<uintptr_t>(a.y) % 16 == 0;
@@ -462,14 +483,17 @@ hipError_t launch_linear(MxLinear a, const MxTile& tl, hipStream_t st) {
 //    a CU runs, at least 0.85; 1.9 for each 128 x 256 block). 24576 x 4096: 64 rows 33
 //    in the small ones, 256 rows 64 in the large ones, 72 in the small ones; 37888 x
 //    3584, 256 rows: 296 large blocks on 256 CUs 114, small ones 91.
-//  * slices cost 2 + 0.8 a MB of them (mx_join_kernel and the stores).
-MxTile mx_tile(int elem, int rows, int n, int k, int groups, bool swiglu, int num_cu) {
+//  * slices cost 2 + 0.8 a MB of them (mx_join_kernel and the stores), or, left to the
+//    kernel that reads the output anyway, 0.5 + 0.3 a MB.
+MxTile mx_tile(int elem, int rows, int n, int k, int groups, bool swiglu, bool join, int num_cu) {
   const int n_out = swiglu ? n / 2 : n, cols = swiglu ? 8 : 16, planes = elem == 2 ? 1 : 3;
   const double mb = (double)n * groups * 17e-6, x_mb = (double)rows * k * 2e-6 * planes;
   MxTile best{};
   double best_t = 1e30;
-  auto take = [&](MxTile t, double us) {
-    if (t.slices > 1) us += 2.0 + 0.8 * t.slices * rows * (double)n * 4e-6;
+  auto take = [&](MxTile t, int steps, double us) {
+    t.slices = ceil_div(steps, ceil_div(steps, t.slices));   // none of them empty
+    const double slices_mb = t.slices * rows * (double)n * 4e-6;
+    if (t.slices > 1) us += join ? 2.0 + 0.8 * slices_mb : 0.5 + 0.3 * slices_mb;
     if (us < best_t) best_t = us, best = t;
   };
   const int walks = ceil_div(groups, kWalk / kMxGroup), chunks = planes * ceil_div(groups, 4);
@@ -484,7 +508,7 @@ MxTile mx_tile(int elem, int rows, int n, int k, int groups, bool swiglu, int nu
         const double blocks = (double)n_tiles * m_tiles * s;
         const double idle = std::max(1.0, 0.875 * num_cu / blocks);
         const int waves = nf == 4 && blocks > num_cu ? 4 : 8;
-        take({kMxFew, mt, nf, s, waves}, 3.5 + mb * m_tiles * idle / 4.5 + x_mb * n_tiles / 9.0);
+        take({kMxFew, mt, nf, s, waves}, walks, 3.5 + mb * m_tiles * idle / 4.5 + x_mb * n_tiles / 9.0);
       }
     }
     if (s > chunks || wide) continue;
@@ -492,8 +516,8 @@ MxTile mx_tile(int elem, int rows, int n, int k, int groups, bool swiglu, int nu
     auto rounds = [&](int bm, int bn) {
       return std::ceil((double)ceil_div(rows, bm) * ceil_div(n_out, bn * cols / 16) * s / num_cu);
     };
-    take({kMxTile64, 0, 0, s, 0}, 4 + per * std::max(0.85, 0.67 * rounds(64, 128)));
-    take({kMxTile128, 0, 0, s, 0}, 4 + per * 1.9 * rounds(128, 256));
+    take({kMxTile64, 0, 0, s, 0}, chunks, 4 + per * std::max(0.85, 0.67 * rounds(64, 128)));
+    take({kMxTile128, 0, 0, s, 0}, chunks, 4 + per * 1.9 * rounds(128, 256));
   }
   return best;
 }
@@ -505,7 +529,7 @@ MxTile mx_tile(int elem, int rows, int n, int k, int groups, bool swiglu, int nu
 // of an fp32 one, 24576 x 4096 at 1024 rows 548.)
 constexpr int kMxGemmRows = 1280;
 
-MxPlan mx_plan(int elem, int rows, int n, int k, bool swiglu, bool aligned, int num_cu) {
+MxPlan mx_plan(int elem, int rows, int n, int k, bool swiglu, bool aligned, bool join, int num_cu) {
   MxPlan p;
   if (elem == 2 && aligned && rows >= kMxGemmRows && k % 8 == 0 && (!swiglu || n % 32 == 0)) {
     p.gemm = true;
@@ -514,11 +538,12 @@ MxPlan mx_plan(int elem, int rows, int n, int k, bool swiglu, bool aligned, int 
     return p;
   }
   const int groups = ceil_div(k, kMxGroup), planes = elem == 2 ? 1 : 3;
-  p.tile = mx_tile(elem, std::max(rows, 1), n, k, groups, swiglu, num_cu);
+  p.tile = mx_tile(elem, std::max(rows, 1), n, k, groups, swiglu, join, num_cu);
+  p.join = join;
   p.staged = elem != 2 || !aligned || k % 8 != 0;
   if (p.staged) p.stage = ((size_t)rows * groups * kMxGroup * 2 * planes + 255) / 256 * 256;
   p.scratch = p.stage;
-  if (p.tile.slices > 1) p.scratch += (size_t)p.tile.slices * rows * n * sizeof(float);
+  if (join && p.tile.slices > 1) p.scratch += (size_t)p.tile.slices * rows * n * sizeof(float);
   return p;
 }
 
@@ -541,7 +566,8 @@ hipError_t mx_matmul(const MxPlan& plan, const T* x, long ldx, int rows, const M
   constexpr int NP = sizeof(T) == 2 ? 1 : 3;
   MxLinear a{};
   a.w = w, a.m = rows, a.k = k, a.swiglu = swiglu, a.add = add, a.y = y, a.ldy = ldy;
-  a.slices = reinterpret_cast<float*>(reinterpret_cast<char*>(scratch) + plan.stage);
+  a.slices = plan.join ? reinterpret_cast<float*>(reinterpret_cast<char*>(scratch) + plan.stage)
+                       : reinterpret_cast<float*>(y);
   if (plan.staged) {
     const int kp = w.groups * kMxGroup;
     const long total = (long)rows * kp;
@@ -556,7 +582,7 @@ hipError_t mx_matmul(const MxPlan& plan, const T* x, long ldx, int rows, const M
   } else {
     return hipErrorInvalidValue;
   }
-  return launch_linear<NP>(a, plan.tile, st);
+  return launch_linear<NP>(a, plan.tile, plan.join, st);
 }
 
 #define INST(T)                                                                                 \

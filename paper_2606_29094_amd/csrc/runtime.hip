@@ -227,11 +227,13 @@ Layout layout(const dlm_model* m, int n, int n_req) {
   L.s_o = L.g_o.splits;
   L.s_down = L.g_down.splits;
   if (!m->mx.empty()) {
-    L.q_qkv = mx_plan(es_i, n, qkv_dim, c.d_model, false, true, m->num_cu);
-    L.q_o = mx_plan(es_i, n, c.d_model, qd, false, true, m->num_cu);
-    L.q_gu = mx_plan(es_i, n, 2 * c.d_ffn, c.d_model, true, true, m->num_cu);
-    L.q_down = mx_plan(es_i, n, c.d_model, c.d_ffn, false, true, m->num_cu);
-    L.s_qkv = L.s_o = L.s_down = 1;
+    // (the rotation and the residual norms add K slices as they read them)
+    L.q_qkv = mx_plan(es_i, n, qkv_dim, c.d_model, false, true, false, m->num_cu);
+    L.q_o = mx_plan(es_i, n, c.d_model, qd, false, true, false, m->num_cu);
+    L.q_gu = mx_plan(es_i, n, 2 * c.d_ffn, c.d_model, true, true, true, m->num_cu);
+    L.q_down = mx_plan(es_i, n, c.d_model, c.d_ffn, false, true, false, m->num_cu);
+    auto slices = [](const MxPlan& p) { return p.gemm ? 1 : p.tile.slices; };
+    L.s_qkv = slices(L.q_qkv), L.s_o = slices(L.q_o), L.s_down = slices(L.q_down);
   }
   L.tiles = lm_head_tiles(L.g_lm, c.vocab);
   const size_t es = m->es;
@@ -463,7 +465,11 @@ dlm_status run_forward(dlm_model* m, dlm_cache* c, const dlm_batch* b, const Ste
                                                   qd, h, d, st));
       LAUNCH(m, st, "rmsnorm", rmsnorm_rows<T>(h, w.ffn_norm, n, d, cf.rms_eps, a, st));
     } else {
-      LAUNCH(m, st, "gemm_o", gemm_store_f32<T>(L.g_o, ao, qd, reinterpret_cast<const T*>(w.w_o), qd, n, d,
+      if (w4)
+        LAUNCH(m, st, "gemm_o", mx_matmul<T>(L.q_o, ao, qd, n, mx_view(w4l->w_o), qd, DLM_MX_STORE, part, d,
+                                             mxs, st));
+      else
+        LAUNCH(m, st, "gemm_o", gemm_store_f32<T>(L.g_o, ao, qd, reinterpret_cast<const T*>(w.w_o), qd, n, d,
                                                     qd, part, d, st));
       LAUNCH(m, st, "residual_rmsnorm", add_rmsnorm_rows<T>(h, part, L.s_o, (long)n * d, w.ffn_norm, n, d,
                                                                 cf.rms_eps, a, st));
@@ -491,7 +497,11 @@ dlm_status run_forward(dlm_model* m, dlm_cache* c, const dlm_batch* b, const Ste
                                cf.d_ffn, h, d, st));
       if (next_a) LAUNCH(m, st, "rmsnorm", rmsnorm_rows<T>(h, next_norm, n, d, cf.rms_eps, a, st));
     } else {
-      LAUNCH(m, st, "gemm_down", gemm_store_f32<T>(L.g_down, act, cf.d_ffn, reinterpret_cast<const T*>(w.w_down),
+      if (w4)
+        LAUNCH(m, st, "gemm_down", mx_matmul<T>(L.q_down, act, cf.d_ffn, n, mx_view(w4l->w_down), cf.d_ffn,
+                                                DLM_MX_STORE, part, d, mxs, st));
+      else
+        LAUNCH(m, st, "gemm_down", gemm_store_f32<T>(L.g_down, act, cf.d_ffn, reinterpret_cast<const T*>(w.w_down),
                                                        cf.d_ffn, n, d, cf.d_ffn, part, d, st));
       LAUNCH(m, st, "residual_rmsnorm", add_rmsnorm_rows<T>(h, part, L.s_down, (long)n * d, next_norm, n, d,
                                                                 cf.rms_eps, next_a, st));
@@ -1131,7 +1141,7 @@ dlm_status dlm_mx_linear_workspace(int32_t dtype, int32_t m_rows, const dlm_mx* 
   size_t need = 0;
   for (int al = 0; al < 2; ++al)
     need = std::max(need, mx_plan(dtype == DLM_BF16 ? 2 : 4, m_rows, w->n, w->k,
-                                  epilogue == DLM_MX_SWIGLU, al != 0, device_cus()).scratch);
+                                  epilogue == DLM_MX_SWIGLU, al != 0, true, device_cus()).scratch);
   *out_bytes = need;
   return DLM_OK;
 }
@@ -1151,7 +1161,7 @@ dlm_status dlm_mx_linear(int32_t dtype, const void* x, int64_t ldx, int32_t m_ro
   const int es = dtype == DLM_BF16 ? 2 : 4;
   const bool al = aligned16(x) && ldx * es % 16 == 0 && w->k * (long)es % 16 == 0 && aligned16(y) &&
                   ldy % 8 == 0 && ldx <= kMxTileK && ldy < INT32_MAX;
-  const MxPlan plan = mx_plan(es, m_rows, w->n, w->k, swiglu, al, device_cus());
+  const MxPlan plan = mx_plan(es, m_rows, w->n, w->k, swiglu, al, true, device_cus());
   if (plan.scratch) {
     if (!workspace) return fail(DLM_EINVAL, "workspace is NULL");
     if (reinterpret_cast<uintptr_t>(workspace) % 256 != 0)
