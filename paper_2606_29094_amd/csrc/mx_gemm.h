@@ -39,8 +39,8 @@ __global__ __launch_bounds__(256) void mx_stage_kernel(const T* __restrict__ x, 
 
 __device__ __forceinline__ float silu_mul(float g, float u) { return g / (1.f + __expf(-g)) * u; }
 
-// Few rows. One block: 16 MT rows x 16 NF columns, W waves that take the 512-wide k
-// ranges ("walks") of the block's K slice in turn and add their partial sums in LDS, in
+// Up to 16 rows. One block: 16 NF columns, W waves that take the 512-wide k ranges
+// ("walks") of the block's K slice in turn and add their partial sums in LDS, in
 // wave order. In a chunk of 128 k lane l reads the 32 codes of group l / 16 of weight
 // row l % 16 as one 16-byte load; four register swaps between the 16-lane groups turn
 // that into the dword of group j that the MFMA j = 0..3 takes (whose lanes then read
@@ -49,13 +49,13 @@ __device__ __forceinline__ float silu_mul(float g, float u) { return g / (1.f + 
 // needs them; x comes from the caches, once for every 16 NF columns.
 constexpr int kWalk = 512;
 
-template <int MT, int NF, int W, int NP>
+template <int NF, int W, int NP>
 __global__ __launch_bounds__(W * 64) void mx_linear_kernel(MxLinear a) {
-  __shared__ f32x4 part[W][MT * NF][64];
+  __shared__ f32x4 part[W][NF][64];
   constexpr int XJ = NP > 1 ? 1 : 2;   // k steps whose x is requested together
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int col = lane & 15, g = lane >> 4;
-  const int n0 = blockIdx.x * (a.swiglu ? NF * 8 : NF * 16), m0 = blockIdx.y * MT * 16;
+  const int n0 = blockIdx.x * (a.swiglu ? NF * 8 : NF * 16), m0 = blockIdx.y * 16;
   const int n_end = a.swiglu ? a.w.n / 2 : a.w.n;   // columns of the output
 
   const uint8_t* wc[NF];
@@ -71,16 +71,11 @@ __global__ __launch_bounds__(W * 64) void mx_linear_kernel(MxLinear a) {
     wc[f] = a.w.codes + ((long)n * a.w.groups + g) * 16;
     ws[f] = a.w.scales + (long)n * a.w.scale_ld;
   }
-  const bf16* xr[MT];
-#pragma unroll
-  for (int t = 0; t < MT; ++t)
-    xr[t] = a.x + (long)min(m0 + 16 * t + col, a.m - 1) * a.ldx + 8 * g;
+  const bf16* const xr = a.x + (long)min(m0 + col, a.m - 1) * a.ldx + 8 * g;
 
-  f32x4 acc[MT][NF];
+  f32x4 acc[NF];
 #pragma unroll
-  for (int t = 0; t < MT; ++t)
-#pragma unroll
-    for (int f = 0; f < NF; ++f) acc[t][f] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int f = 0; f < NF; ++f) acc[f] = f32x4{0.f, 0.f, 0.f, 0.f};
 
   // one walk; TAIL: the last one, whose groups and elements may end inside it
   auto walk = [&](int s, auto tail) {
@@ -96,20 +91,18 @@ __global__ __launch_bounds__(W * 64) void mx_linear_kernel(MxLinear a) {
                           : u32x4{0u, 0u, 0u, 0u};
       scales[f] = *reinterpret_cast<const u32x4*>(ws[f] + 16 * s);
     }
-    bf16x8 xv[2][XJ][NP][MT];
+    bf16x8 xv[2][XJ][NP];
     auto xload = [&](int i) {   // x of steps XJ i .. of the walk
 #pragma unroll
       for (int u = 0; u < XJ; ++u) {
         const int c = (XJ * i + u) / 4, j = (XJ * i + u) % 4;
         const bool in = !TAIL || k0 + 128 * c + 32 * j + 8 * g < a.k;
 #pragma unroll
-        for (int p = 0; p < NP; ++p)
-#pragma unroll
-          for (int t = 0; t < MT; ++t) {
-            bf16x8 v = {};
-            if (in) v = *reinterpret_cast<const bf16x8*>(xr[t] + p * a.plane + k0 + 128 * c + 32 * j);
-            xv[i & 1][u][p][t] = v;
-          }
+        for (int p = 0; p < NP; ++p) {
+          bf16x8 v = {};
+          if (in) v = *reinterpret_cast<const bf16x8*>(xr + p * a.plane + k0 + 128 * c + 32 * j);
+          xv[i & 1][u][p] = v;
+        }
       }
     };
     xload(0);
@@ -134,9 +127,7 @@ __global__ __launch_bounds__(W * 64) void mx_linear_kernel(MxLinear a) {
 #pragma unroll
         for (int p = 0; p < NP; ++p)
 #pragma unroll
-          for (int t = 0; t < MT; ++t)
-#pragma unroll
-            for (int f = 0; f < NF; ++f) acc[t][f] = mfma16_bf16(xv[i & 1][u][p][t], b[f], acc[t][f]);
+          for (int f = 0; f < NF; ++f) acc[f] = mfma16_bf16(xv[i & 1][u][p], b[f], acc[f]);
       }
     }
   };
@@ -148,12 +139,10 @@ __global__ __launch_bounds__(W * 64) void mx_linear_kernel(MxLinear a) {
     else walk(s, std::true_type{});
   }
 #pragma unroll
-  for (int t = 0; t < MT; ++t)
-#pragma unroll
-    for (int f = 0; f < NF; ++f) part[wave][t * NF + f][lane] = acc[t][f];
+  for (int f = 0; f < NF; ++f) part[wave][f][lane] = acc[f];
   __syncthreads();
 
-  // fragment (or gate / up pair of fragments) i of the tile is wave i % W's
+  // wave f finishes fragment f (or gate / up pair of fragments)
   auto sum = [&](int i) {
     f32x4 v = part[0][i][lane];
 #pragma unroll
@@ -163,13 +152,13 @@ __global__ __launch_bounds__(W * 64) void mx_linear_kernel(MxLinear a) {
   const bool sliced = gridDim.z > 1;   // fp32 sums to the scratch, mx_join_kernel does the rest
   if (a.swiglu && !sliced) {
     constexpr int H = NF > 1 ? NF / 2 : 1;
-    for (int i = wave; i < MT * H; i += W) {
-      const int t = i / H, f = i % H;
-      const f32x4 gate = sum(t * NF + f), up = sum(t * NF + f + NF / 2);
+    if (wave < H) {
+      const int f = wave;
+      const f32x4 gate = sum(f), up = sum(f + NF / 2);
       const int n = n0 + 16 * f + col;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int m = m0 + 16 * t + 4 * g + e;
+        const int m = m0 + 4 * g + e;
         if (m >= a.m || n >= n_end) continue;
         const float v = silu_mul(gate[e], up[e]);
         if constexpr (NP == 1) reinterpret_cast<bf16*>(a.y)[(long)m * a.ldy + n] = (bf16)v;
@@ -180,9 +169,9 @@ __global__ __launch_bounds__(W * 64) void mx_linear_kernel(MxLinear a) {
   }
   float* out = sliced ? a.slices + (long)blockIdx.z * a.m * a.w.n : reinterpret_cast<float*>(a.y);
   const long ldo = sliced ? a.w.n : a.ldy;
-  for (int i = wave; i < MT * NF; i += W) {
-    const int t = i / NF, f = i % NF;
-    const f32x4 v = sum(i);
+  if (wave < NF) {
+    const int f = wave;
+    const f32x4 v = sum(f);
     int n = n0 + 16 * f + col;
     bool ok = n < n_end;
     if (a.swiglu) {
@@ -190,47 +179,47 @@ __global__ __launch_bounds__(W * 64) void mx_linear_kernel(MxLinear a) {
       ok = n < n_end;
       n += 2 * f >= NF ? n_end : 0;
     }
-    float* o = out + (long)(m0 + 16 * t + 4 * g) * ldo + n;
+    float* o = out + (long)(m0 + 4 * g) * ldo + n;
     f32x4 old = {0.f, 0.f, 0.f, 0.f};
     if (a.add && !sliced) {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        if (ok && m0 + 16 * t + 4 * g + e < a.m) old[e] = o[e * ldo];
+        if (ok && m0 + 4 * g + e < a.m) old[e] = o[e * ldo];
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      if (ok && m0 + 16 * t + 4 * g + e < a.m) o[e * ldo] = old[e] + v[e];
+      if (ok && m0 + 4 * g + e < a.m) o[e * ldo] = old[e] + v[e];
   }
 }
 
-// More rows: one block of WM x WN waves computes 16 MT WM rows x 16 NF WN columns. x goes
-// through LDS in chunks of 128 k by direct loads, three stages of them, shared by all
-// waves; each wave reads its own columns' codes from memory into registers two chunks
-// ahead and unpacks them there (once for 16 MT rows), so the weights need no LDS.
+// More rows: WN waves compute 16 MT rows x 16 NF WN columns. x goes through LDS in chunks
+// of 128 k by direct loads, NS stages of them, shared by the waves; each wave reads its
+// own columns' codes from memory into registers NS - 1 chunks ahead, and their scales
+// for four chunks (a walk) at a time one walk ahead, and unpacks them there (once for 16 MT rows),
+// so the weights need no LDS.
 // Row r of a stage is 256 bytes, its 16-byte slot s stored at s ^ (r & 15): the 16 rows
 // that a fragment reads at one slot come from distinct banks.
 // Blocks of one column tile are 8 apart in the launch (one XCD): its row tiles read the
 // codes through one L2.
 __device__ const uint4 kZeros[1] = {};   // what x holds behind k
 
-template <int WM, int WN, int MT, int NF, int NS, bool PLANES>
-__global__ __launch_bounds__(WM * WN * 64) void mx_tile_kernel(MxLinear a, int n_tiles, int m_tiles) {
+template <int WN, int MT, int NF, int NS, bool PLANES>
+__global__ __launch_bounds__(WN * 64) void mx_tile_kernel(MxLinear a, int n_tiles, int m_tiles) {
   typedef typename std::conditional<PLANES, float, bf16>::type T;
-  constexpr int NW = WM * WN, BM = 16 * MT * WM, STAGE = BM * 256;
-  constexpr int XL = STAGE / 1024 / NW;    // direct loads of a wave for a stage
-  constexpr int LOADS = XL + 2 * NF;       // memory operations of a wave for a chunk
-  static_assert(STAGE % (1024 * NW) == 0, "whole loads");
+  constexpr int BM = 16 * MT, STAGE = BM * 256;
+  constexpr int XL = STAGE / 1024 / WN;    // direct loads of a wave for a stage
+  constexpr int LOADS = XL + NF;           // memory operations of a wave for a chunk, without scales
+  static_assert(STAGE % (1024 * WN) == 0 && 4 % NS == 0, "whole loads, whole walks");
   __shared__ __attribute__((aligned(16))) char smem[NS * STAGE];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int col = lane & 15, g = lane >> 4;
-  const int wm = wave / WN, wn = wave % WN;
   const int id = blockIdx.x / kXcds;
   const int n_tile = id / m_tiles * kXcds + blockIdx.x % kXcds;
   if (n_tile >= n_tiles) return;
   const int m0 = id % m_tiles * BM;
   const int n_end = a.swiglu ? a.w.n / 2 : a.w.n;
   constexpr int H = NF / 2;
-  const int n0 = (n_tile * WN + wn) * (a.swiglu ? 16 * H : 16 * NF);   // the wave's first column
+  const int n0 = (n_tile * WN + wave) * (a.swiglu ? 16 * H : 16 * NF);   // the wave's first column
 
   // Addresses as a base of the wave, which scalar registers hold, and an offset of the
   // lane in 32 bits; with SwiGLU the second half of the fragments are the up rows.
@@ -250,56 +239,64 @@ __global__ __launch_bounds__(WM * WN * 64) void mx_tile_kernel(MxLinear a, int n
   uint32_t xs[XL];         // this lane's slot in each of the wave's direct loads
 #pragma unroll
   for (int u = 0; u < XL; ++u) {
-    const int r = 4 * (u * NW + wave) + g;
+    const int r = 4 * (u * WN + wave) + g;
     xs[u] = (uint32_t)min(r, a.m - 1 - m0) * (uint32_t)a.ldx * 2 + 16 * (col ^ (r & 15));
   }
   uint32_t slot[4];        // of the lane's fragments in a row of a stage
 #pragma unroll
-  for (int j = 0; j < 4; ++j) slot[j] = (wm * MT * 16 + col) * 256 + ((4 * j + g) ^ col) * 16;
-  // (the planes of fp32 x are so many products with the same weights, one after the other)
-  const int chunks = ceil_div(a.w.groups, 4);
-  const int c0 = blockIdx.z * a.per_slice, c1 = min(c0 + a.per_slice, chunks * a.planes);
+  for (int j = 0; j < 4; ++j) slot[j] = col * 256 + ((4 * j + g) ^ col) * 16;
+
+  // The walks of this block's slice; the planes of fp32 x are so many products with the
+  // same weights, one after the other.
+  const int walks = ceil_div(a.w.groups, kWalk / kMxGroup);
+  const int s0 = blockIdx.z * a.per_slice, s1 = min(s0 + a.per_slice, walks * a.planes);
+  const int turns = s1 - s0;
+  auto walk = [&](int i) { return min(s0 + i, s1 - 1); };   // (past the end: loaded, not used)
 
   f32x4 acc[MT][NF];
 #pragma unroll
   for (int t = 0; t < MT; ++t)
 #pragma unroll
     for (int f = 0; f < NF; ++f) acc[t][f] = f32x4{0.f, 0.f, 0.f, 0.f};
-  u32x4 codes[NS][NF];
-  uint32_t scales[NS][NF];
-  auto load = [&](int b, int at) {
+  u32x4 codes[NS][NF], scales[2][NF];
+  auto load = [&](int b, int i, int c4) {   // chunk c4 of turn i into stage b
+    const int s = walk(i), c = 4 * (PLANES ? s % walks : s) + c4;
     char* dst = smem + b * STAGE + wave * 1024;
-    const int p = PLANES ? at / chunks : 0, c = PLANES ? at % chunks : at;
-    const char* xc = x0 + p * a.plane * 2 + (long)c * 256;
+    const char* xc = x0 + (PLANES ? s / walks * a.plane * 2 : 0) + (long)c * 256;
 #pragma unroll
     for (int u = 0; u < XL; ++u) {   // what lies behind k counts as zero
-      const int k = 128 * c + 8 * (col ^ ((4 * (u * NW + wave) + g) & 15));
-      load_lds16(k < a.k ? xc + xs[u] : reinterpret_cast<const char*>(kZeros), dst + u * NW * 1024);
+      const int k = 128 * c + 8 * (col ^ ((4 * (u * WN + wave) + g) & 15));
+      load_lds16(k < a.k ? xc + xs[u] : reinterpret_cast<const char*>(kZeros), dst + u * WN * 1024);
     }
-    // (a lane behind the last group reads that one; its scale is set to one and x is zero)
-    const uint32_t back = 16 * max(4 * c + g - (a.w.groups - 1), 0);
-    const uint8_t* cb = codes0 + (long)c * 64;
-    const uint8_t* sb = scales0 + (long)c * 4;
+    // (a lane behind the last group reads that one, a chunk behind the last one that chunk;
+    // scales are set to one there and x is zero)
+    const int cw = min(c, (a.w.groups - 1) / 4);
+    const uint32_t back = 16 * max(4 * cw + g - (a.w.groups - 1), 0);
+    const uint8_t* cb = codes0 + (long)cw * 64;
 #pragma unroll
-    for (int f = 0; f < NF; ++f) {
+    for (int f = 0; f < NF; ++f)
       codes[b][f] = *reinterpret_cast<const u32x4*>(cb + (f >= H ? up_codes : 0) + (wc[f] - back));
-      scales[b][f] = *reinterpret_cast<const uint32_t*>(sb + (f >= H ? up_scales : 0) + ws[f]);
-    }
   };
-  auto compute = [&](int b, int at) {
-    const int c = PLANES ? at % chunks : at;
+  auto load_scales = [&](int b, int i) {    // of turn i
+    const int s = walk(i);
+    const uint8_t* sb = scales0 + (long)(PLANES ? s % walks : s) * 16;
+#pragma unroll
+    for (int f = 0; f < NF; ++f)
+      scales[b][f] = *reinterpret_cast<const u32x4*>(sb + (f >= H ? up_scales : 0) + ws[f]);
+  };
+  auto compute = [&](int b, int sb, int i, int c4) {
+    const int s = walk(i), c = 4 * (PLANES ? s % walks : s) + c4;
     const int left = a.w.groups - 4 * c;   // groups of the chunk
-    const uint32_t keep = left >= 4 ? ~0u : (1u << (8 * left)) - 1;
+    const uint32_t keep = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
     u32x4 cd[NF];
     uint32_t sc[NF];
 #pragma unroll
     for (int f = 0; f < NF; ++f) {
       cd[f] = transpose_groups(codes[b][f]);
-      sc[f] = (scales[b][f] & keep) | (0x7f7f7f7fu & ~keep);
+      sc[f] = (scales[sb][f][c4] & keep) | (0x7f7f7f7fu & ~keep);
     }
     // In the large tiles the fragments of step j + 1 are read and unpacked between the
-    // MFMAs of step j (3584 x 18944, 1000 rows 157 -> 151 us; the small tiles, three of
-    // which share a CU, lose by it: 37888 x 3584, 256 rows 91 -> 97).
+    // MFMAs of step j.
     constexpr int AHEAD = MT >= 8 ? 1 : 0;
     bf16x8 xv[AHEAD + 1][MT], w[AHEAD + 1][NF];
     auto fetch = [&](int j) {
@@ -332,33 +329,41 @@ __global__ __launch_bounds__(WM * WN * 64) void mx_tile_kernel(MxLinear a, int n
       __builtin_amdgcn_sched_group_barrier(0x008, MT * NF, 0);
     }
   };
-  // Every step issues the loads of a chunk, past the end those of the last one again: the
-  // waits count loads, and one that some path skips would have to be counted out.
+  // Every step issues the loads of a chunk, past the end those of the last walk again: the
+  // waits count loads, and one that some path skips would have to be counted out. (Scales
+  // are not counted: the waits are then longer by them where they are in flight.)
+  load_scales(0, 0);
 #pragma unroll
   for (int b = 0; b < NS - 1; ++b) {
-    load(b, min(c0 + b, c1 - 1));
+    load(b, 0, b);
     __builtin_amdgcn_sched_barrier(0);
   }
-  for (int c = c0; c < c1;) {
+  auto turn = [&](int i, auto parity) {
+    constexpr int P = decltype(parity)::value;
 #pragma unroll
-    for (int b = 0; b < NS; ++b) {
-      if (c >= c1) break;
-      wait_vmcnt<(NS - 2) * LOADS>();    // chunk c is here, later ones may be in flight,
-      __builtin_amdgcn_s_barrier();      // and every wave is done with c - 1
-      load((b + NS - 1) % NS, min(c + NS - 1, c1 - 1));
+    for (int c4 = 0; c4 < 4; ++c4) {
+      wait_vmcnt<(NS - 2) * LOADS>();      // the chunk is here, later ones may be in flight,
+      __builtin_amdgcn_s_barrier();        // and every wave is done with the one before
+      constexpr int D = NS - 1;
+      load((c4 + D) % NS, i + (c4 + D) / 4, (c4 + D) % 4);
+      if (c4 == 0) load_scales(1 - P, i + 1);
       __builtin_amdgcn_sched_barrier(0);
-      compute(b, c);
+      compute(c4 % NS, P, i, c4);
       __builtin_amdgcn_sched_barrier(0);
-      ++c;
     }
+  };
+  for (int i = 0; i < turns; i += 2) {
+    turn(i, std::integral_constant<int, 0>{});
+    if (i + 1 < turns) turn(i + 1, std::integral_constant<int, 1>{});
   }
-  wait_vmcnt<0>();                       // (no load may reach LDS after the block has left it)
+  wait_vmcnt<0>();                         // (no load may reach LDS after the block has left it)
+
   const bool sliced = gridDim.z > 1;
   float* out = sliced ? a.slices + (long)blockIdx.z * a.m * a.w.n : reinterpret_cast<float*>(a.y);
   const long ldo = sliced ? a.w.n : a.ldy;
 #pragma unroll
   for (int t = 0; t < MT; ++t) {
-    const int m = m0 + (wm * MT + t) * 16 + 4 * g;   // and the three rows behind
+    const int m = m0 + t * 16 + 4 * g;     // and the three rows behind
     if (a.swiglu && !sliced) {
 #pragma unroll
       for (int f = 0; f < H; ++f) {
@@ -426,36 +431,32 @@ hipError_t launch_linear(MxLinear a, const MxTile& tl, bool join, hipStream_t st
   const int cols = a.swiglu ? 8 : 16;    // output columns of a fragment
   a.planes = NP;
   dim3 grid;
-  const int steps = tl.kind == kMxFew ? ceil_div(a.w.groups, kWalk / kMxGroup)
-                                      : NP * ceil_div(a.w.groups, 4);
+  const int steps = ceil_div(a.w.groups, kWalk / kMxGroup) * (tl.kind == kMxFew ? 1 : NP);
   a.per_slice = ceil_div(steps, tl.slices);
   grid.z = ceil_div(steps, a.per_slice);
   if (tl.kind == kMxFew) {
-    grid.x = ceil_div(n_out, cols * tl.nf), grid.y = ceil_div(a.m, 16 * tl.mt);
-#define MX_FEW(MT_, NF_, W_)                                                                       \
-  if (tl.mt == MT_ && tl.nf == NF_ && tl.waves == W_)                                              \
-  DLM_LAUNCH((mx_linear_kernel<MT_, NF_, W_, NP>), grid, dim3(W_ * 64), 0, st, a)
-    MX_FEW(1, 1, 8);
-    MX_FEW(1, 2, 8);
+    grid.x = ceil_div(n_out, cols * tl.nf), grid.y = ceil_div(a.m, 16);
+#define MX_FEW(NF_, W_)                                                                            \
+  if (tl.nf == NF_ && tl.waves == W_)                                                              \
+  DLM_LAUNCH((mx_linear_kernel<NF_, W_, NP>), grid, dim3(W_ * 64), 0, st, a)
+    MX_FEW(1, 8);
+    MX_FEW(2, 8);
     if constexpr (NP == 1) {
-      MX_FEW(1, 4, 8);
-      MX_FEW(1, 4, 4);
-      MX_FEW(2, 1, 8);
-      MX_FEW(2, 2, 8);
-      MX_FEW(2, 4, 8);
-      MX_FEW(2, 4, 4);
+      MX_FEW(4, 8);
+      MX_FEW(4, 4);
     }
 #undef MX_FEW
   } else {
-#define MX_TILE(KIND_, WM_, WN_, MT_, NF_, NS_)                                                    \
+#define MX_TILE(KIND_, WN_, MT_, NF_, NS_)                                                         \
   if (tl.kind == KIND_) {                                                                          \
-    const int n_tiles = ceil_div(n_out, cols * NF_ * WN_), m_tiles = ceil_div(a.m, 16 * MT_ * WM_); \
+    const int n_tiles = ceil_div(n_out, cols * NF_ * WN_), m_tiles = ceil_div(a.m, 16 * MT_);      \
     grid.x = ceil_div(n_tiles, kXcds) * kXcds * m_tiles, grid.y = 1;                               \
-    DLM_LAUNCH((mx_tile_kernel<WM_, WN_, MT_, NF_, NS_, (NP > 1)>), grid, dim3(WM_ * WN_ * 64), 0, \
-               st, a, n_tiles, m_tiles);                                                           \
+    DLM_LAUNCH((mx_tile_kernel<WN_, MT_, NF_, NS_, (NP > 1)>), grid, dim3(WN_ * 64), 0, st, a,     \
+               n_tiles, m_tiles);                                                                  \
   }
-    MX_TILE(kMxTile64, 1, 4, 4, 2, 3)
-    MX_TILE(kMxTile128, 1, 8, 8, 2, 3)
+    MX_TILE(kMxTile32, 4, 2, 2, 4)
+    MX_TILE(kMxTile64, 4, 4, 2, 2)
+    MX_TILE(kMxTile128, 8, 8, 2, 2)
 #undef MX_TILE
   }
   hipError_t e = hipGetLastError();
@@ -474,20 +475,23 @@ hipError_t launch_linear(MxLinear a, const MxTile& tl, bool join, hipStream_t st
 
 // Way of a product. Times in us on MI355X (256 CUs), weights from HBM; what is modelled
 // is what decides between the ways:
-//  * few rows (mx_linear_kernel): 3.5 + the weights at 4.5 TB/s (less while blocks leave
-//    CUs idle) + x, once for each column tile and K slice, at 9 TB/s out of the L2s. So one row takes one
-//    column fragment a block and no slices (4096 x 4096 4.9, with two fragments 6.6),
-//    32 rows four (24576 x 4096 27.4, two 31.7), and a long K slices (4096 x 12288,
-//    16 rows: four fragments in four slices 13.7, one whole 18.4).
-//  * tiles (mx_tile_kernel): 4 + chunks of a slice x (0.67 us for each 64 x 128 block that
-//    a CU runs, at least 0.85; 1.9 for each 128 x 256 block). 24576 x 4096: 64 rows 33
-//    in the small ones, 256 rows 64 in the large ones, 72 in the small ones; 37888 x
-//    3584, 256 rows: 296 large blocks on 256 CUs 114, small ones 91.
+//  * up to 16 rows (mx_linear_kernel): 3.5 + the weights at 4.5 TB/s (less while blocks
+//    leave CUs idle) + x, once for each column tile and K slice, at 9 TB/s out of the
+//    L2s. So one row takes one column fragment a block and no slices (4096 x 4096 5.3,
+//    two fragments 6.6), and 16 rows over a long K take four in slices (4096 x 12288:
+//    four slices 13.6, one fragment, whole 18.4).
+//  * tiles (mx_tile_kernel): 4 + for each chunk of a slice 0.5, 0.84 or 1.7 (blocks of 32 x
+//    128, 64 x 128 and 128 x 256), or 0.43, 0.55 or 1.7 for each block that a CU runs.
+//    24576 x 4096: 32 rows 19.8 in the first, 128 rows 45, 38 and 63, 256 rows 82, 57
+//    and 55; 37888 x 3584, 256 rows: 296 large blocks on 256 CUs 98, second 77.
 //  * slices cost 2 + 0.8 a MB of them (mx_join_kernel and the stores), or, left to the
 //    kernel that reads the output anyway, 0.5 + 0.3 a MB.
 MxTile mx_tile(int elem, int rows, int n, int k, int groups, bool swiglu, bool join, int num_cu) {
   const int n_out = swiglu ? n / 2 : n, cols = swiglu ? 8 : 16, planes = elem == 2 ? 1 : 3;
   const double mb = (double)n * groups * 17e-6, x_mb = (double)rows * k * 2e-6 * planes;
+  const int walks = ceil_div(groups, kWalk / kMxGroup);
+  // (the tiles address their rows in 32 bits, the join its rows in one grid dimension)
+  const bool wide = k > kMxTileK;
   MxTile best{};
   double best_t = 1e30;
   auto take = [&](MxTile t, int steps, double us) {
@@ -496,38 +500,39 @@ MxTile mx_tile(int elem, int rows, int n, int k, int groups, bool swiglu, bool j
     if (t.slices > 1) us += join ? 2.0 + 0.8 * slices_mb : 0.5 + 0.3 * slices_mb;
     if (us < best_t) best_t = us, best = t;
   };
-  const int walks = ceil_div(groups, kWalk / kMxGroup), chunks = planes * ceil_div(groups, 4);
-  // (the tiles address their rows in 32 bits, the join its rows in one grid dimension)
-  const bool wide = k > kMxTileK;
+  struct Tile { int kind, bm, bn; double one, more; };
+  static const Tile tiles[] = {{kMxTile32, 32, 128, 0.5, 0.43},
+                               {kMxTile64, 64, 128, 0.84, 0.55},
+                               {kMxTile128, 128, 256, 1.7, 1.7}};
   for (int s = 1; s <= (rows <= 4096 ? 8 : 1); s *= 2) {
-    if (rows <= 32 || planes > 1 || wide) {
-      const int mt = rows <= 16 || planes > 1 ? 1 : 2, m_tiles = ceil_div(rows, 16 * mt);
+    if ((rows <= 256 || wide) && s <= walks) {   // (small matrices: also for more than 16 rows)
+      const int m_tiles = ceil_div(rows, 16);
       for (int nf = swiglu ? 2 : 1; nf <= (planes > 1 ? 2 : 4); nf *= 2) {
-        if (s > walks) break;
         const int n_tiles = ceil_div(n_out, cols * nf);
         const double blocks = (double)n_tiles * m_tiles * s;
         const double idle = std::max(1.0, 0.875 * num_cu / blocks);
         const int waves = nf == 4 && blocks > num_cu ? 4 : 8;
-        take({kMxFew, mt, nf, s, waves}, walks, 3.5 + mb * m_tiles * idle / 4.5 + x_mb * n_tiles / 9.0);
+        take({kMxFew, nf, s, waves}, walks, 3.5 + mb * m_tiles * idle / 4.5 + x_mb * n_tiles / 9.0);
       }
     }
-    if (s > chunks || wide) continue;
-    const int per = ceil_div(chunks, s);
-    auto rounds = [&](int bm, int bn) {
-      return std::ceil((double)ceil_div(rows, bm) * ceil_div(n_out, bn * cols / 16) * s / num_cu);
-    };
-    take({kMxTile64, 0, 0, s, 0}, chunks, 4 + per * std::max(0.85, 0.67 * rounds(64, 128)));
-    take({kMxTile128, 0, 0, s, 0}, chunks, 4 + per * 1.9 * rounds(128, 256));
+    if (wide || s > planes * walks) continue;
+    const int chunks = 4 * ceil_div(planes * walks, s);
+    for (const Tile& t : tiles) {
+      const double fill =
+          (double)ceil_div(rows, t.bm) * ceil_div(n_out, t.bn * cols / 16) * s / num_cu;
+      const double share = fill < 4 || t.kind == kMxTile128 ? std::ceil(fill) : fill;
+      take({t.kind, 0, s, 0}, planes * walks, 4 + chunks * std::max(t.one, t.more * share));
+    }
   }
   return best;
 }
 
 // From this many rows on a bf16 matrix is unpacked once and goes through the GEMM kernels.
 // Straight from the codes / unpacked (the unpacking included), us: 24576 x 4096 at 1024
-// rows 198 / 233, at 2048 389 / 357; 4096 x 12288 110 / 133 and 202 / 202; 12288 x 4096
-// at 1536 186 / 158. (fp32 stays with the codes: three bf16 products take half
-// of an fp32 one, 24576 x 4096 at 1024 rows 548.)
-constexpr int kMxGemmRows = 1280;
+// rows 183 / 222, at 2048 357 / 351, at 4096 736 / 631; 4096 x 12288 112 / 121, 179 / 193
+// and 370 / 332. (fp32 stays with the codes: three bf16 products take half of an fp32
+// one, 24576 x 4096 at 1024 rows 496.)
+constexpr int kMxGemmRows = 2048;
 
 MxPlan mx_plan(int elem, int rows, int n, int k, bool swiglu, bool aligned, bool join, int num_cu) {
   MxPlan p;
