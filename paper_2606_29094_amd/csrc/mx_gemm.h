@@ -15,25 +15,31 @@ namespace dlm {
 namespace {
 
 // --------------------------------------------------------------- products --
-// x for the product kernel: NP planes of [rows, kp] bf16 (one for bf16 x, three for
-// fp32 x: split3), kp = 32 groups, zero from k on.
+// x for the product kernels: NP planes of [rows, kp] bf16 (one for bf16 x, three for
+// fp32 x: split3), kp = 32 groups, zero from k on. A thread makes eight elements of a row.
 template <typename T, int NP>
-__global__ __launch_bounds__(256) void mx_stage_kernel(const T* __restrict__ x, long ldx, int k,
-                                                       int kp, long plane, bf16* __restrict__ out,
-                                                       long total) {
-  const long at = (long)blockIdx.x * 256 + threadIdx.x;
-  if (at >= total) return;
-  const long row = at / kp;
-  const int c = (int)(at - row * kp);
-  const float v = c < k ? to_f32(x[row * ldx + c]) : 0.f;
-  if constexpr (NP == 1) {
-    out[at] = (bf16)v;
-  } else {
-    bf16 a, b, d;
-    split3(v, a, b, d);
-    out[at] = a;
-    out[at + plane] = b;
-    out[at + 2 * plane] = d;
+__global__ __launch_bounds__(256) void mx_stage_kernel(const T* __restrict__ x, long ldx, int rows,
+                                                       int k, int kp, long plane,
+                                                       bf16* __restrict__ out) {
+  const long at = ((long)blockIdx.x * 256 + threadIdx.x) * 8;
+  if (at >= kp) return;
+  for (long row = blockIdx.y; row < rows; row += gridDim.y) {
+    bf16x8 v[NP];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float e = at + i < k ? to_f32(x[row * ldx + at + i]) : 0.f;
+      if constexpr (NP == 1) {
+        v[0][i] = (bf16)e;
+      } else {
+        bf16 hi, mid, lo;
+        split3(e, hi, mid, lo);
+        v[0][i] = hi;
+        v[1][i] = mid;
+        v[2][i] = lo;
+      }
+    }
+#pragma unroll
+    for (int p = 0; p < NP; ++p) *reinterpret_cast<bf16x8*>(out + p * plane + row * kp + at) = v[p];
   }
 }
 
@@ -199,8 +205,10 @@ __global__ __launch_bounds__(W * 64) void mx_linear_kernel(MxLinear a) {
 // so the weights need no LDS.
 // Row r of a stage is 256 bytes, its 16-byte slot s stored at s ^ (r & 15): the 16 rows
 // that a fragment reads at one slot come from distinct banks.
-// Blocks of one column tile are 8 apart in the launch (one XCD): its row tiles read the
-// codes through one L2.
+// Blocks 8 apart in the launch run on one XCD: each XCD takes an eighth of the tiles, the row
+// tiles of a column tile one after the other, so they read its codes through one L2. (An
+// eighth of the column tiles to each left XCDs idle where there are few: 41 x 2608 at 3636
+// rows, one column tile, 33 us against 10.)
 __device__ const uint4 kZeros[1] = {};   // what x holds behind k
 
 template <int WN, int MT, int NF, int NS, bool PLANES>
@@ -213,10 +221,10 @@ __global__ __launch_bounds__(WN * 64) void mx_tile_kernel(MxLinear a, int n_tile
   __shared__ __attribute__((aligned(16))) char smem[NS * STAGE];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int col = lane & 15, g = lane >> 4;
-  const int id = blockIdx.x / kXcds;
-  const int n_tile = id / m_tiles * kXcds + blockIdx.x % kXcds;
-  if (n_tile >= n_tiles) return;
-  const int m0 = id % m_tiles * BM;
+  const int per_xcd = ceil_div(n_tiles * m_tiles, kXcds);
+  const int id = blockIdx.x % kXcds * per_xcd + blockIdx.x / kXcds;
+  if (id >= n_tiles * m_tiles) return;
+  const int n_tile = id / m_tiles, m0 = id % m_tiles * BM;
   const int n_end = a.swiglu ? a.w.n / 2 : a.w.n;
   constexpr int H = NF / 2;
   const int n0 = (n_tile * WN + wave) * (a.swiglu ? 16 * H : 16 * NF);   // the wave's first column
@@ -361,10 +369,10 @@ __global__ __launch_bounds__(WN * 64) void mx_tile_kernel(MxLinear a, int n_tile
   const bool sliced = gridDim.z > 1;
   float* out = sliced ? a.slices + (long)blockIdx.z * a.m * a.w.n : reinterpret_cast<float*>(a.y);
   const long ldo = sliced ? a.w.n : a.ldy;
+  if (a.swiglu && !sliced) {
 #pragma unroll
-  for (int t = 0; t < MT; ++t) {
-    const int m = m0 + t * 16 + 4 * g;     // and the three rows behind
-    if (a.swiglu && !sliced) {
+    for (int t = 0; t < MT; ++t) {
+      const int m = m0 + t * 16 + 4 * g;   // and the three rows behind
 #pragma unroll
       for (int f = 0; f < H; ++f) {
         const int n = n0 + 16 * f + col;
@@ -374,27 +382,43 @@ __global__ __launch_bounds__(WN * 64) void mx_tile_kernel(MxLinear a, int n_tile
             reinterpret_cast<T*>(a.y)[(m + e) * a.ldy + n] =
                 from_f32<T>(silu_mul(acc[t][f][e], acc[t][f + H][e]));
       }
-      continue;
     }
-    float* o[NF];            // nullptr: a column behind the last
+    return;
+  }
+  float* o[NF];              // nullptr: a column behind the last
 #pragma unroll
-    for (int f = 0; f < NF; ++f) {
-      const int n = n0 + 16 * (a.swiglu ? f % H : f) + col;
-      o[f] = n < n_end ? out + m * ldo + n + (a.swiglu && f >= H ? n_end : 0) : nullptr;
-    }
-    if (a.add && !sliced) {  // (all of the tile's old values before the first store)
+  for (int f = 0; f < NF; ++f) {
+    const int n = n0 + 16 * (a.swiglu ? f % H : f) + col;
+    o[f] = n < n_end ? out + (m0 + 4 * g) * ldo + n + (a.swiglu && f >= H ? n_end : 0) : nullptr;
+  }
+  if (a.add && !sliced) {    // all of the old values before the first store
+    // In the large tiles no load is conditional, so that they go out together: 3369 x 4187
+    // outputs of 382 inputs 65 us against 93. In the small ones the registers that this
+    // takes would cost a block a CU: 300 rows of 3584 x 18944 71 us against 65.
+    const float* p[NF];
+#pragma unroll
+    for (int f = 0; f < NF; ++f) p[f] = out + min(n0 + 16 * f + col, n_end - 1);
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
 #pragma unroll
       for (int f = 0; f < NF; ++f)
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (o[f] && m + e < a.m) acc[t][f][e] += o[f][e * ldo];
-    }
+        for (int e = 0; e < 4; ++e) {
+          const int m = m0 + t * 16 + 4 * g + e;
+          if constexpr (MT >= 8) {
+            acc[t][f][e] += p[f][min(m, a.m - 1) * ldo];
+          } else {
+            if (o[f] && m < a.m) acc[t][f][e] += o[f][(t * 16 + e) * ldo];
+          }
+        }
+  }
+#pragma unroll
+  for (int t = 0; t < MT; ++t)
 #pragma unroll
     for (int f = 0; f < NF; ++f)
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        if (o[f] && m + e < a.m) o[f][e * ldo] = acc[t][f][e];
-  }
+        if (o[f] && m0 + t * 16 + 4 * g + e < a.m) o[f][(t * 16 + e) * ldo] = acc[t][f][e];
 }
 
 // The K slices of a product, added in order, and its epilogue: V columns of a row a
@@ -450,7 +474,7 @@ hipError_t launch_linear(MxLinear a, const MxTile& tl, bool join, hipStream_t st
 #define MX_TILE(KIND_, WN_, MT_, NF_, NS_)                                                         \
   if (tl.kind == KIND_) {                                                                          \
     const int n_tiles = ceil_div(n_out, cols * NF_ * WN_), m_tiles = ceil_div(a.m, 16 * MT_);      \
-    grid.x = ceil_div(n_tiles, kXcds) * kXcds * m_tiles, grid.y = 1;                               \
+    grid.x = ceil_div(n_tiles * m_tiles, kXcds) * kXcds, grid.y = 1;                                 \
     DLM_LAUNCH((mx_tile_kernel<WN_, MT_, NF_, NS_, (NP > 1)>), grid, dim3(WN_ * 64), 0, st, a,     \
                n_tiles, m_tiles);                                                                  \
   }
@@ -531,12 +555,15 @@ MxTile mx_tile(int elem, int rows, int n, int k, int groups, bool swiglu, bool j
 // Straight from the codes / unpacked (the unpacking included), us: 24576 x 4096 at 1024
 // rows 183 / 222, at 2048 357 / 351, at 4096 736 / 631; 4096 x 12288 112 / 121, 179 / 193
 // and 370 / 332. (fp32 stays with the codes: three bf16 products take half of an fp32
-// one, 24576 x 4096 at 1024 rows 496.)
-constexpr int kMxGemmRows = 2048;
+// one, 24576 x 4096 at 1024 rows 496. Narrow matrices stay too: 512 x 688 at 3815 rows
+// 9 / 25, 41 x 2608 at 3636 14 / 55.)
+constexpr int kMxGemmRows = 2048, kMxGemmCols = 1024;
 
-MxPlan mx_plan(int elem, int rows, int n, int k, bool swiglu, bool aligned, bool join, int num_cu) {
+MxPlan mx_plan(int elem, int rows, int n, int k, bool swiglu, bool x_aligned, bool y_aligned, bool join,
+               int num_cu) {
   MxPlan p;
-  if (elem == 2 && aligned && rows >= kMxGemmRows && k % 8 == 0 && (!swiglu || n % 32 == 0)) {
+  if (elem == 2 && x_aligned && y_aligned && rows >= kMxGemmRows && n >= kMxGemmCols && k % 8 == 0 &&
+      (!swiglu || n % 32 == 0)) {
     p.gemm = true;
     p.g = gemm_plan(elem, rows, n, k, false, num_cu, !swiglu, true, !swiglu);
     p.scratch = (size_t)n * k * elem;
@@ -545,7 +572,7 @@ MxPlan mx_plan(int elem, int rows, int n, int k, bool swiglu, bool aligned, bool
   const int groups = ceil_div(k, kMxGroup), planes = elem == 2 ? 1 : 3;
   p.tile = mx_tile(elem, std::max(rows, 1), n, k, groups, swiglu, join, num_cu);
   p.join = join;
-  p.staged = elem != 2 || !aligned || k % 8 != 0;
+  p.staged = elem != 2 || !x_aligned || k % 8 != 0;
   if (p.staged) p.stage = ((size_t)rows * groups * kMxGroup * 2 * planes + 255) / 256 * 256;
   p.scratch = p.stage;
   if (join && p.tile.slices > 1) p.scratch += (size_t)p.tile.slices * rows * n * sizeof(float);
@@ -577,8 +604,8 @@ hipError_t mx_matmul(const MxPlan& plan, const T* x, long ldx, int rows, const M
     const int kp = w.groups * kMxGroup;
     const long total = (long)rows * kp;
     bf16* xs = reinterpret_cast<bf16*>(scratch);
-    DLM_LAUNCH((mx_stage_kernel<T, NP>), dim3((unsigned)((total + 255) / 256)), dim3(256), 0, st, x,
-               ldx, k, kp, total, xs, total);
+    DLM_LAUNCH((mx_stage_kernel<T, NP>), dim3(ceil_div(kp / 8, 256), std::min(rows, 65535)), dim3(256), 0,
+               st, x, ldx, rows, k, kp, total, xs);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     a.x = xs, a.ldx = kp, a.plane = total, a.k = kp;

@@ -12,11 +12,13 @@ namespace dlm {
 namespace {
 
 // ------------------------------------------------------------ pack, unpack --
-// Bound by memory. Rows whose vectors are aligned: a lane takes 16 bytes of the wide
-// matrix, so a group is held by four lanes (bf16) or eight (fp32) that find its largest
-// magnitude by exchanges within the row of lanes, and the wide matrix moves in whole
-// lines. (One thread for each group, its lines in 64- and 128-byte strides: 4096 x 4096
-// bf16, both directions 25.5 us, 37888 x 3584 fp32 340.) Other rows: one thread for each group.
+// Bound by memory. A lane takes 16 bytes of the wide matrix, so a group is held by four
+// lanes (bf16) or eight (fp32) that find its largest magnitude by exchanges within the
+// row of lanes, and the wide matrix moves in whole lines. (One thread for each group, its
+// lines in 64- and 128-byte strides: 4096 x 4096 bf16, both directions 25.5 us against
+// 21.0, 37888 x 3584 fp32 340 against 237.) VEC: rows are whole 16-byte vectors; else
+// their elements are loaded and stored one by one (2781 x 14407 bf16 both ways 108 us, 304 by
+// a thread for each group).
 constexpr int kPackVecs = 4;             // vectors of a thread, loaded together
 
 // largest of the 16 / sizeof(T) lanes that hold a group
@@ -29,7 +31,7 @@ __device__ __forceinline__ uint32_t group_max(uint32_t v) {
   return v;
 }
 
-template <typename T>
+template <typename T, bool VEC>
 __global__ __launch_bounds__(256) void mx_pack_kernel(const T* __restrict__ w, long ldw, int k,
                                                       MxView o) {
   constexpr int V = 16 / sizeof(T), LANES = kMxGroup / V;
@@ -41,7 +43,13 @@ __global__ __launch_bounds__(256) void mx_pack_kernel(const T* __restrict__ w, l
 #pragma unroll
     for (int u = 0; u < kPackVecs; ++u) {
       const int at = at0 + u * 256;
-      x[u] = at * V < k ? *reinterpret_cast<const vt*>(w + row * ldw + at * V) : vt{};
+      const T* p = w + row * ldw + at * V;
+      if constexpr (VEC) {
+        x[u] = at * V < k ? *reinterpret_cast<const vt*>(p) : vt{};
+      } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[u][i] = at * V + i < k ? p[i] : (T)0.f;
+      }
     }
 #pragma unroll
     for (int u = 0; u < kPackVecs; ++u) {
@@ -67,7 +75,7 @@ __global__ __launch_bounds__(256) void mx_pack_kernel(const T* __restrict__ w, l
   }
 }
 
-template <typename T>
+template <typename T, bool VEC>
 __global__ __launch_bounds__(256) void mx_unpack_kernel(MxView w, int k, T* __restrict__ out, long ldo) {
   constexpr int V = 16 / sizeof(T), LANES = kMxGroup / V;
   typedef T vt __attribute__((ext_vector_type(V)));
@@ -90,60 +98,15 @@ __global__ __launch_bounds__(256) void mx_unpack_kernel(MxView w, int k, T* __re
       vt v;
 #pragma unroll
       for (int i = 0; i < V; ++i) v[i] = (T)(float)x[i];
-      *reinterpret_cast<vt*>(out + row * ldo + at * V) = v;
+      T* p = out + row * ldo + at * V;
+      if constexpr (VEC) {
+        *reinterpret_cast<vt*>(p) = v;
+      } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+          if (at * V + i < k) p[i] = v[i];
+      }
     }
-  }
-}
-
-template <typename T>
-__global__ __launch_bounds__(256) void mx_pack_any_kernel(const T* __restrict__ w, long ldw, int k,
-                                                          MxView o, long total) {
-  const long at = (long)blockIdx.x * 256 + threadIdx.x;
-  if (at >= total) return;
-  const long row = at / o.scale_ld;
-  const int g = (int)(at - row * o.scale_ld);
-  if (g >= o.groups) {
-    o.scales[at] = 0;
-    return;
-  }
-  const T* p = w + row * ldw + g * kMxGroup;
-  const int n = k - g * kMxGroup;
-  float x[kMxGroup];
-  uint32_t amax = 0;
-#pragma unroll
-  for (int i = 0; i < kMxGroup; ++i) {
-    x[i] = i < n ? to_f32(p[i]) : 0.f;
-    amax = max(amax, __float_as_uint(x[i]) & 0x7fffffffu);
-  }
-  const uint32_t e = mx_scale_byte(amax);
-  const float s = mx_scale(e);
-  u32x4 c;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    c[i] = e == 255u ? 0u
-                     : mx_codes4(x[8 * i], x[8 * i + 1], x[8 * i + 2], x[8 * i + 3], s) |
-                           mx_codes4(x[8 * i + 4], x[8 * i + 5], x[8 * i + 6], x[8 * i + 7], s) << 16;
-  reinterpret_cast<u32x4*>(o.codes)[row * o.groups + g] = c;
-  o.scales[at] = (uint8_t)e;
-}
-
-template <typename T>
-__global__ __launch_bounds__(256) void mx_unpack_any_kernel(MxView w, int k, T* __restrict__ out,
-                                                            long ldo, long total) {
-  const long at = (long)blockIdx.x * 256 + threadIdx.x;
-  if (at >= total) return;
-  const long row = at / w.groups;
-  const int g = (int)(at - row * w.groups);
-  const u32x4 c = reinterpret_cast<const u32x4*>(w.codes)[at];
-  const float s = mx_scale(w.scales[row * w.scale_ld + g]);
-  const int n = k - g * kMxGroup;
-  T* o = out + row * ldo + g * kMxGroup;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const bf16x8 v = mx_bf16x8(c[i], s);
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (8 * i + j < n) o[8 * i + j] = (T)(float)v[j];
   }
 }
 
@@ -238,13 +201,14 @@ __global__ __launch_bounds__(256) void mx_read_kernel(StepPlan p, int hkv, MxKv 
 
 }  // namespace
 
-// whether rows of k elements, ld apart, are whole 16-byte vectors (whose index fits in int)
+// whether rows of k elements, ld apart, are whole 16-byte vectors
 template <typename T>
 static bool whole_vectors(const T* p, long ld, int k) {
   constexpr int V = 16 / sizeof(T);
-  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % V == 0 && k % V == 0 && k < (1 << 30);
+  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % V == 0 && k % V == 0;
 }
 
+// blocks over the vectors of a row; the rows go round the second dimension
 template <typename T>
 static dim3 pack_grid(const MxView& w) {
   return dim3(ceil_div(w.groups * (kMxGroup / (16 / (int)sizeof(T))), 256 * kPackVecs), std::min(w.n, 65535));
@@ -252,25 +216,19 @@ static dim3 pack_grid(const MxView& w) {
 
 template <typename T>
 hipError_t mx_pack(const T* w, long ldw, int k, const MxView& o, hipStream_t st) {
-  if (whole_vectors(w, ldw, k)) {
-    DLM_LAUNCH(mx_pack_kernel<T>, pack_grid<T>(o), dim3(256), 0, st, w, ldw, k, o);
-  } else {
-    const long total = (long)o.n * o.scale_ld;
-    DLM_LAUNCH(mx_pack_any_kernel<T>, dim3((unsigned)((total + 255) / 256)), dim3(256), 0, st, w, ldw, k,
-               o, total);
-  }
+  if (whole_vectors(w, ldw, k))
+    DLM_LAUNCH((mx_pack_kernel<T, true>), pack_grid<T>(o), dim3(256), 0, st, w, ldw, k, o);
+  else
+    DLM_LAUNCH((mx_pack_kernel<T, false>), pack_grid<T>(o), dim3(256), 0, st, w, ldw, k, o);
   return hipGetLastError();
 }
 
 template <typename T>
 hipError_t mx_unpack(const MxView& w, int k, T* out, long ldo, hipStream_t st) {
-  if (whole_vectors(out, ldo, k)) {
-    DLM_LAUNCH(mx_unpack_kernel<T>, pack_grid<T>(w), dim3(256), 0, st, w, k, out, ldo);
-  } else {
-    const long total = (long)w.n * w.groups;
-    DLM_LAUNCH(mx_unpack_any_kernel<T>, dim3((unsigned)((total + 255) / 256)), dim3(256), 0, st, w, k,
-               out, ldo, total);
-  }
+  if (whole_vectors(out, ldo, k))
+    DLM_LAUNCH((mx_unpack_kernel<T, true>), pack_grid<T>(w), dim3(256), 0, st, w, k, out, ldo);
+  else
+    DLM_LAUNCH((mx_unpack_kernel<T, false>), pack_grid<T>(w), dim3(256), 0, st, w, k, out, ldo);
   return hipGetLastError();
 }
 

@@ -147,8 +147,8 @@ def test_linear_strides(gpu, m, pad, out_pad):
     (2, 4096, 4096, "store"), (16, 4100, 6000, "add"), (16, 24576, 1024, "swiglu"),       # up to 16 rows
     (31, 3584, 4608, "add"), (60, 8200, 2048, "swiglu"), (100, 12288, 520, "store"),      # tiles of 32 and 64
     (200, 3590, 5000, "add"), (385, 8192, 1288, "store"), (513, 24576, 600, "swiglu"),    # and of 128
-    (2047, 520, 1032, "store"), (2048, 520, 1032, "add"), (2048, 544, 1032, "swiglu"),    # unpacked from 2048 on
-    (2048, 546, 1032, "swiglu"), (2050, 40, 1031, "store")])                              # (not these)
+    (2047, 1040, 1032, "store"), (2048, 1040, 1032, "add"), (2048, 1088, 1032, "swiglu"),  # unpacked from 2048 on
+    (2048, 1090, 1032, "swiglu"), (2050, 1040, 1031, "store"), (2050, 41, 2608, "add")])   # (not these)
 def test_linear_ways(gpu, m, n, k, epilogue):
     _check_linear(gpu, m, n, k, BF16, epilogue, seed=m)
 
