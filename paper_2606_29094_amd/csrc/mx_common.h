@@ -79,12 +79,17 @@ __device__ __forceinline__ uint32_t mx_codes4(float a, float b, float c, float d
 
 // fp32 x as the sum of three bf16 terms, which together hold its 24 bits: products
 // of 4-bit values with fp32 ones run on the bf16 matrix cores, exactly to each term.
-// What no bf16 holds (beyond 3.39e38, infinities, NaN) goes into the first term alone.
+// Infinities and NaN go into the first term alone. The first term is rounded (a finite
+// value that would round to an infinity, from 3.396e38 on, is cut off), the second cut
+// off, so the sum of the first two does not overflow either; what is left after it, at
+// most 8 bits, is the third.
 __device__ __forceinline__ void split3(float x, bf16& hi, bf16& mid, bf16& lo) {
-  hi = (bf16)x;
+  auto cut = [](float v) { return __uint_as_float(__float_as_uint(v) & 0xffff0000u); };
+  const uint32_t mag = __float_as_uint(x) & 0x7fffffffu;
+  hi = (bf16)(mag >= 0x7f7f8000u && mag < 0x7f800000u ? cut(x) : x);
   float r = x - (float)hi;
   r = __builtin_isfinite(r) ? r : 0.f;
-  mid = (bf16)r;
+  mid = (bf16)cut(r);
   lo = (bf16)(r - (float)mid);
 }
 
