@@ -66,7 +66,7 @@ struct LaunchTiming { hipEvent_t start = nullptr, stop = nullptr; };
 extern thread_local LaunchTiming g_launch_timing;
 #define DLM_LAUNCH(kernel, grid, block, shmem, stream, ...)                                     \
   do {                                                                                         \
-    if (::dlm::g_launch_timing.start) {                                                        \
+    if (::dlm::g_launch_timing.start || ::dlm::g_launch_timing.stop) {                         \
       const ::dlm::LaunchTiming lt_ = ::dlm::g_launch_timing;                                  \
       ::dlm::g_launch_timing = ::dlm::LaunchTiming{};                                          \
       hipExtLaunchKernelGGL(kernel, grid, block, shmem, stream, lt_.start, lt_.stop, 0,        \
@@ -75,6 +75,21 @@ extern thread_local LaunchTiming g_launch_timing;
       hipLaunchKernelGGL(kernel, grid, block, shmem, stream, __VA_ARGS__);                     \
     }                                                                                          \
   } while (0)
+
+// For a call of several kernels: the first one carries the hook's start event, and the one
+// launched after last() its stop event, so the time between them is the whole call's.
+struct LaunchSpan {
+  LaunchTiming all;
+  explicit LaunchSpan(bool several) {
+    if (several && g_launch_timing.start) {
+      all = g_launch_timing;
+      g_launch_timing.stop = nullptr;
+    }
+  }
+  void last() const {
+    if (all.stop) g_launch_timing = LaunchTiming{nullptr, all.stop};
+  }
+};
 
 // XCDs the dispatcher spreads a launch's blocks over (block i to XCD i mod 8);
 // each has its own L2

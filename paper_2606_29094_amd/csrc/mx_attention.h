@@ -490,6 +490,7 @@ hipError_t launch_attention(const StepPlan& p, const T* q, const MxAttn& a, MxAt
   const StepPlan t = plan_with_tiles(p, [&](int n) { return ceil_div(n * gh, per); });
   if (t.n_tiles == 0) return hipSuccess;
   const dim3 grid(t.n_tiles * a.hkv, 1, a.splits);
+  const LaunchSpan span(a.splits > 1);
   if constexpr (sizeof(T) == 2) {
     if (plan.kind == kMxAttnShared128)
       DLM_LAUNCH((mx_attn_shared_kernel<DH, 2, 4>), grid, dim3(256), 0, st, t, q, a, out);
@@ -502,6 +503,7 @@ hipError_t launch_attention(const StepPlan& p, const T* q, const MxAttn& a, MxAt
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.splits == 1) return e;
+  span.last();
   const long items = (long)p.n_rows * a.hq;
   DLM_LAUNCH((mx_merge_kernel<T, DH>), dim3((unsigned)((items * (DH / 4) + 255) / 256)), dim3(256), 0,
              st, a, items, out);

@@ -450,7 +450,7 @@ __global__ __launch_bounds__(256) void mx_join_kernel(MxLinear a, int n_slices) 
 
 // Launch of a planned product; x of NP planes.
 template <int NP>
-hipError_t launch_linear(MxLinear a, const MxTile& tl, bool join, hipStream_t st) {
+hipError_t launch_linear(MxLinear a, const MxTile& tl, bool join, const LaunchSpan& span, hipStream_t st) {
   const int n_out = a.swiglu ? a.w.n / 2 : a.w.n;
   const int cols = a.swiglu ? 8 : 16;    // output columns of a fragment
   a.planes = NP;
@@ -485,6 +485,7 @@ hipError_t launch_linear(MxLinear a, const MxTile& tl, bool join, hipStream_t st
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || grid.z == 1 || !join) return e;
+  span.last();
   typedef typename std::conditional<NP == 1, bf16, float>::type T;
   // (vector accesses of the slices and of fp32 outputs)
   const bool v4 = n_out % 4 == 0 && a.ldy % 4 == 0 && reinterpret_cast<uintptr_t>(a.y) % 16 == 0;
@@ -586,8 +587,10 @@ hipError_t mx_matmul(const MxPlan& plan, const T* x, long ldx, int rows, const M
   const bool swiglu = epilogue == DLM_MX_SWIGLU, add = epilogue == DLM_MX_ADD;
   if (plan.gemm) {
     T* dense = reinterpret_cast<T*>(scratch);
+    const LaunchSpan span(true);
     const hipError_t e = mx_unpack<T>(w, k, dense, k, st);
     if (e != hipSuccess) return e;
+    span.last();
     if (swiglu)
       return gemm_swiglu<T>(plan.g, x, (int)ldx, dense, k, rows, w.n / 2, k, reinterpret_cast<T*>(y),
                             (int)ldy, st);
@@ -600,6 +603,8 @@ hipError_t mx_matmul(const MxPlan& plan, const T* x, long ldx, int rows, const M
   a.w = w, a.m = rows, a.k = k, a.swiglu = swiglu, a.add = add, a.y = y, a.ldy = ldy;
   a.slices = plan.join ? reinterpret_cast<float*>(reinterpret_cast<char*>(scratch) + plan.stage)
                        : reinterpret_cast<float*>(y);
+  const bool joined = plan.join && plan.tile.slices > 1;
+  const LaunchSpan span(plan.staged || joined);
   if (plan.staged) {
     const int kp = w.groups * kMxGroup;
     const long total = (long)rows * kp;
@@ -614,7 +619,8 @@ hipError_t mx_matmul(const MxPlan& plan, const T* x, long ldx, int rows, const M
   } else {
     return hipErrorInvalidValue;
   }
-  return launch_linear<NP>(a, plan.tile, plan.join, st);
+  if (!joined) span.last();
+  return launch_linear<NP>(a, plan.tile, plan.join, span, st);
 }
 
 #define INST(T)                                                                                 \

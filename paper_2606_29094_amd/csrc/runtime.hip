@@ -11,6 +11,7 @@
 #include <cstdio>
 #include <cstring>
 #include <mutex>
+#include <new>
 #include <string>
 #include <utility>
 #include <vector>
@@ -97,7 +98,7 @@ dlm_status scratch_address(void** out) {
       if (a_ && b_) g_launch_timing = LaunchTiming{a_, b_};                       \
     }                                                                             \
     const hipError_t le_ = (expr);                                                \
-    const bool used_ = a_ && b_ && !g_launch_timing.start;                        \
+    const bool used_ = a_ && b_ && !g_launch_timing.start && !g_launch_timing.stop; \
     g_launch_timing = LaunchTiming{};                                             \
     if (used_) {                                                                  \
       pf_.pending.push_back({pf_.kind_of(name), a_, b_});                         \
@@ -702,14 +703,20 @@ dlm_status dlm_load_weights_mx(const dlm_config* cfg, const dlm_weights_mx* w, d
       if ((s = check_mx(q.w, q.n, q.k, what)) != DLM_OK) return s;
     }
   }
-  dlm_model* m = new dlm_model();
+  dlm_model* m = nullptr;
+  try {
+    m = new dlm_model();
+    m->mx.assign(w->layers, w->layers + cfg->n_layers);
+    for (const dlm_layer_mx& lw : m->mx)
+      m->layers.push_back({lw.attn_norm, nullptr, nullptr, lw.ffn_norm, nullptr, nullptr});
+  } catch (const std::bad_alloc&) {
+    delete m;
+    return fail(DLM_ESIZE, "out of host memory for %d layers", cfg->n_layers);
+  }
   m->cfg = *cfg;
   m->embed = w->embed;
   m->lm_head = w->lm_head;
   m->final_norm = w->final_norm;
-  m->mx.assign(w->layers, w->layers + cfg->n_layers);
-  for (const dlm_layer_mx& lw : m->mx)
-    m->layers.push_back({lw.attn_norm, nullptr, nullptr, lw.ffn_norm, nullptr, nullptr});
   m->es = cfg->dtype == DLM_BF16 ? 2 : 4;
   m->num_cu = device_cus();
   *out = m;
@@ -811,7 +818,14 @@ static dlm_status kv_cache_alloc(const dlm_model* m, bool mx, int32_t n_slots, i
   if (buf_bytes < need) return fail(DLM_ESIZE, "cache buffer %zu bytes < %zu", buf_bytes, need);
   if (reinterpret_cast<uintptr_t>(dev_buf) % 256 != 0)
     return fail(DLM_EINVAL, "cache buffer is not 256-byte aligned");
-  dlm_cache* k = new dlm_cache();
+  dlm_cache* k = nullptr;
+  try {
+    k = new dlm_cache();
+    k->slots.assign(n_slots, SlotState{});
+  } catch (const std::bad_alloc&) {
+    delete k;
+    return fail(DLM_ESIZE, "out of host memory for %d slots", n_slots);
+  }
   k->model = m;
   k->n_slots = n_slots;
   k->s_max = s_max;
@@ -819,7 +833,6 @@ static dlm_status kv_cache_alloc(const dlm_model* m, bool mx, int32_t n_slots, i
   k->region = region;
   k->mx = mx;
   k->scale_region = scale_region;
-  k->slots.assign(n_slots, SlotState{});
   *out = k;
   return DLM_OK;
 }

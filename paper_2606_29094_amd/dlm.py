@@ -400,15 +400,24 @@ def _flat(name, t, shape, dtype):
         raise ValueError(f"{name} is not contiguous")
 
 
-def _on(stream, *tensors):
-    """The stream argument of a call on these tensors, which have to be on the current device:
-    the given one, or that device's current stream."""
+def _on(stream, *tensors, cache=None):
+    """The stream argument of a call on these tensors (and on a cache in a tensor's memory),
+    which have to be on the current device: the given one, or that device's current stream."""
     import torch
     dev = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else -2
     for t in tensors:
         if t.get_device() != dev:
             raise ValueError(f"a tensor is on {t.device}, not on the current GPU")
+    if cache is not None and cache.device not in (None, dev):
+        raise ValueError(f"the cache is on cuda:{cache.device}, not on the current GPU")
     return stream if stream is not None else torch._C._cuda_getCurrentRawStream(dev)
+
+
+def _scratch(workspace):
+    """(address, bytes) of a workspace tensor."""
+    if not workspace.is_contiguous():
+        raise ValueError("workspace is not contiguous")
+    return workspace.data_ptr(), workspace.nbytes
 
 
 def mx_bytes(n: int, k: int):
@@ -466,7 +475,7 @@ def mx_linear(x, q: DlmMx, y, epilogue: int = DLM_MX_STORE, workspace=None, stre
     if workspace is None:
         st, ws, size = _on(stream, x, y, *q._keep), None, 0
     else:
-        st, ws, size = _on(stream, x, y, workspace, *q._keep), workspace.data_ptr(), workspace.nbytes
+        st, (ws, size) = _on(stream, x, y, workspace, *q._keep), _scratch(workspace)
     check(lib().dlm_mx_linear(_dtype_id(dt), x.data_ptr(), ldx, m, ctypes.byref(q), epilogue,
                               y.data_ptr(), ldy, ws, size, st))
 
@@ -485,44 +494,50 @@ def kv_cache_alloc_mx(model, n_slots: int, max_seq_len: int, dev_buf=None, buf_b
     check(lib().dlm_kv_cache_alloc_mx(model, n_slots, max_seq_len, _ptr(dev_buf), buf_bytes,
                                       ctypes.byref(req), ctypes.byref(h)))
     h.config = model.config
+    h.device = dev_buf.get_device() if hasattr(dev_buf, "get_device") else None
     return (h if dev_buf is not None else None), req.value
 
 
 def _heads(cache):
     """(query width, key/value width, rotary pairs, torch dtype) of a 4-bit cache's model."""
     import torch
-    c = cache.config
+    c = getattr(cache, "config", None)
+    if c is None:
+        raise ValueError("not a cache of kv_cache_alloc_mx")
     return (c.n_q_heads * c.head_dim, c.n_kv_heads * c.head_dim, c.head_dim // 2,
             torch.bfloat16 if c.dtype == DLM_BF16 else torch.float32)
 
 
 def make_kv_rows(rows):
     """[(slot, seq_len, pos0, n_rows)] as the argument of the mx_kv calls."""
-    arr = (DlmKvRows * len(rows))(*[DlmKvRows(*r) for r in rows])
-    arr.total = sum(r[3] for r in rows)        # N, read by every call on these requests
-    return arr
+    return (DlmKvRows * len(rows))(*[DlmKvRows(*r) for r in rows])
+
+
+def _total(rows) -> int:
+    """N: the sum of n_rows, of the array as it is now."""
+    return sum((c_int32 * (4 * len(rows))).from_buffer(rows)[3::4])
 
 
 def mx_kv_append(cache, layer: int, rows, qkv, rot, q_out, stream=None):
     """qkv fp32 [splits, N, (n_q_heads + 2 n_kv_heads) head_dim] or without splits, rot fp32
     [N, head_dim / 2, 2], q_out [N, n_q_heads head_dim] in the model dtype. rows: make_kv_rows."""
     import torch
-    n, (qd, kd, pairs, dt) = rows.total, _heads(cache)
+    n, (qd, kd, pairs, dt) = _total(rows), _heads(cache)
     splits = qkv.shape[0] if qkv.dim() == 3 else 1
     _flat("qkv", qkv, (splits, n, qd + 2 * kd) if qkv.dim() == 3 else (n, qd + 2 * kd), torch.float32)
     _flat("rot", rot, (n, pairs, 2), torch.float32)
     _flat("q_out", q_out, (n, qd), dt)
-    st = _on(stream, qkv, rot, q_out)
+    st = _on(stream, qkv, rot, q_out, cache=cache)
     check(lib().dlm_mx_kv_append(cache, layer, len(rows), rows, qkv.data_ptr(), splits,
                                  rot.data_ptr(), q_out.data_ptr(), st))
 
 
 def mx_kv_read(cache, layer: int, rows, k_out, v_out, stream=None):
     """The stored keys and values of the rows' positions, [N, n_kv_heads head_dim]."""
-    n, (_, kd, _, dt) = rows.total, _heads(cache)
+    n, (_, kd, _, dt) = _total(rows), _heads(cache)
     _flat("k_out", k_out, (n, kd), dt)
     _flat("v_out", v_out, (n, kd), dt)
-    st = _on(stream, k_out, v_out)
+    st = _on(stream, k_out, v_out, cache=cache)
     check(lib().dlm_mx_kv_read(cache, layer, len(rows), rows, k_out.data_ptr(), v_out.data_ptr(), st))
 
 
@@ -535,13 +550,13 @@ def mx_kv_attention_workspace(cache, rows) -> int:
 def mx_kv_attention(cache, layer: int, rows, q, out, workspace=None, stream=None):
     """out = attention of q over the 4-bit cache; both [N, n_q_heads head_dim]; workspace: at
     least mx_kv_attention_workspace bytes, or None where that is 0."""
-    n, (qd, _, _, dt) = rows.total, _heads(cache)
+    n, (qd, _, _, dt) = _total(rows), _heads(cache)
     _flat("q", q, (n, qd), dt)
     _flat("out", out, (n, qd), dt)
     if workspace is None:
-        st, ws, size = _on(stream, q, out), None, 0
+        st, ws, size = _on(stream, q, out, cache=cache), None, 0
     else:
-        st, ws, size = _on(stream, q, out, workspace), workspace.data_ptr(), workspace.nbytes
+        st, (ws, size) = _on(stream, q, out, workspace, cache=cache), _scratch(workspace)
     check(lib().dlm_mx_kv_attention(cache, layer, len(rows), rows, q.data_ptr(), out.data_ptr(), ws, size, st))
 
 
