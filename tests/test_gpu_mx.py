@@ -200,6 +200,54 @@ def test_linear_non_finite(gpu):
         assert torch.equal(y.sign()[want.isinf()].double(), want.sign()[want.isinf()])
 
 
+@pytest.mark.parametrize("m", [2, 40])
+def test_linear_largest_inputs(gpu, m):
+    """fp32 inputs up to the type's largest value times weights of a half and one: each output
+    is one product, whose terms (the input in parts, times a power of two) add up exactly."""
+    w = torch.zeros(33, 64)
+    w[torch.arange(33), torch.arange(33)] = torch.where(torch.arange(33) % 2 == 0, 0.5, 1.0)
+    q, v = _packed(gpu, 33, 64, w=w)
+    assert torch.equal(v, w.double())
+    top = torch.finfo(torch.float32).max
+    x = torch.empty(m, 64).uniform_(0.99 * top, top, generator=torch.Generator().manual_seed(1))
+    x[0, :3], x[1, ::2] = top, -x[1, ::2]
+    y = torch.empty(m, 33, device=gpu)
+    ws = torch.empty(dlm.mx_linear_workspace(F32, m, q), dtype=torch.uint8, device=gpu)
+    dlm.mx_linear(x.to(gpu), q, y, workspace=ws)
+    assert torch.equal(y.cpu().double(), x.double() @ v.T)
+
+
+def test_binding_checks_of_device_calls(gpu):
+    """Requests changed after make_kv_rows, workspaces with holes or too short, a cache of
+    another device."""
+    c = Cache(gpu, 2, 1, 64, BF16, 2, 100)
+    rows = dlm.make_kv_rows([(0, 90, 0, 3), (1, 20, 0, 2)])
+    q, o = (torch.zeros(5, 128, dtype=BF16, device=gpu) for _ in range(2))
+    c.fill(0, 90, seed=1)
+    c.fill(1, 20, seed=2)
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device=gpu)
+    dlm.mx_kv_attention(c.handle, 0, rows, q, o, ws)
+    rows[1].n_rows = 4
+    with pytest.raises(ValueError):
+        dlm.mx_kv_attention(c.handle, 0, rows, q, o, ws)
+    rows[1].n_rows = 2
+    with pytest.raises(ValueError):
+        dlm.mx_kv_attention(c.handle, 0, rows, q, o, ws[::2])
+    c.handle.device = torch.cuda.device_count()
+    with pytest.raises(ValueError):
+        dlm.mx_kv_attention(c.handle, 0, rows, q, o, ws)
+    w, _ = _packed(gpu, 40, 96)
+    x, y = torch.zeros(3, 96, device=gpu), torch.zeros(3, 40, device=gpu)
+    need = dlm.mx_linear_workspace(F32, 3, w)
+    assert need > 1
+    for bad in (None, ws[:need - 1], ws[8:]):
+        with pytest.raises(dlm.DlmError):
+            dlm.mx_linear(x, w, y, workspace=bad)
+    with pytest.raises(ValueError):
+        dlm.mx_linear(x, w, y, workspace=torch.empty(1, dtype=torch.uint8, device=gpu).expand(need))
+    c.close()
+
+
 def test_linear_large_offsets(gpu):
     """Rows of the output more than 2^31 bytes behind the first."""
     q, w = _packed(gpu, 32, 64)
@@ -456,4 +504,43 @@ def test_other_stream_and_graph(gpu):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip((o, y, c.buf), want[s - 10])), i
         assert all(torch.equal(a, b) for a, b in zip(eager(12), want[2]))
+    c.close()
+
+
+def test_two_streams_at_once(gpu):
+    """Products and attention of two streams at once, each with its own outputs and workspaces,
+    give what they give alone."""
+    hq, hkv, dh, n = 8, 2, 128, 40
+    c = Cache(gpu, hq, hkv, dh, BF16, 2, 1500)
+    w, _ = _packed(gpu, 600, hq * dh, seed=3)
+    sets = []
+    for i, length in enumerate((1500, 1111)):
+        c.fill(i, length, seed=i)
+        rows = dlm.make_kv_rows([(i, length, 0, n)])
+        sets.append(dict(rows=rows, q=_randn(n, hq * dh, seed=i, dtype=BF16).to(gpu),
+                         o=torch.empty(n, hq * dh, dtype=BF16, device=gpu), y=torch.empty(n, 600, device=gpu),
+                         ws=torch.empty(max(256, dlm.mx_kv_attention_workspace(c.handle, rows)),
+                                        dtype=torch.uint8, device=gpu),
+                         ws2=torch.empty(max(256, dlm.mx_linear_workspace(BF16, n, w)),
+                                         dtype=torch.uint8, device=gpu)))
+
+    def run(s):
+        dlm.mx_kv_attention(c.handle, 0, s["rows"], s["q"], s["o"], s["ws"])
+        dlm.mx_linear(s["o"], w, s["y"], workspace=s["ws2"])
+
+    want = []
+    for s in sets:
+        run(s)
+        torch.cuda.synchronize()
+        want.append((s["o"].clone(), s["y"].clone()))
+        s["o"].zero_(), s["y"].zero_()
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sets]
+    for _ in range(5):
+        for s, st in zip(sets, streams):
+            with torch.cuda.stream(st):
+                run(s)
+    torch.cuda.synchronize()
+    for s, (o, y) in zip(sets, want):
+        assert torch.equal(s["o"], o) and torch.equal(s["y"], y)
     c.close()

@@ -197,3 +197,27 @@ def test_packed_step_without_allocation(gpu):
     for k in outs[0]:
         if k in ("n", "block_conf", "block_tok"):
             assert np.array_equal(outs[0][k], outs[1][k]), k
+
+
+@pytest.mark.parametrize("name", ["tiny", "gqa"])
+def test_packed_step_profile(gpu, name):
+    """The profiler times every class of a packed model's step once a layer; a projection of
+    several kernels (staging, product, joined slices) is one entry."""
+    cfg = MODELS[name]
+    t = sdev.model_tensors(cfg)
+    model = engine.DeviceModel(_shape(cfg), t, 10.0, packed=True)
+    reqs = _requests(cfg, SPECS, 32)
+    eng = engine.Engine(model, 3, 164, "dual", packed_kv=True)
+    for r in reqs:
+        eng.admit(r, cfg.mask_id)
+    eng.step(reqs)
+    dlm.profile_enable(model.handle, True)
+    for _ in range(2):
+        eng.step([r for r in reqs if not r.done])
+    dlm.profile_enable(model.handle, False)
+    prof = dlm.profile_read(model.handle)
+    for kind in ("gemm_qkv", "rope_kv_write", "attention", "gemm_o", "gemm_gate_up_swiglu", "gemm_down"):
+        calls, ms, seen = prof[kind]
+        assert calls == seen == 2 * cfg.n_layers, kind
+        assert 0 < ms < 1000, kind
+    eng.close()
