@@ -211,7 +211,7 @@ struct MxPlan {
 };
 // x_aligned, y_aligned: the buffer and its rows start at multiples of 16 bytes (rows of x at
 // most kMxTileK elements apart). join: K slices are added by the product; otherwise (DLM_MX_STORE alone)
-// y takes tile.slices of them, [slices, rows, n], for a consumer that adds them.
+// y takes tile.slices (g.splits) of them, [slices, rows, n], for a consumer that adds them.
 MxPlan mx_plan(int elem, int rows, int n, int k, bool swiglu, bool x_aligned, bool y_aligned, bool join,
                int num_cu);
 // epilogue: dlm_mx_epilogue

@@ -566,7 +566,9 @@ MxPlan mx_plan(int elem, int rows, int n, int k, bool swiglu, bool x_aligned, bo
   if (elem == 2 && x_aligned && y_aligned && rows >= kMxGemmRows && n >= kMxGemmCols && k % 8 == 0 &&
       (!swiglu || n % 32 == 0)) {
     p.gemm = true;
-    p.g = gemm_plan(elem, rows, n, k, false, num_cu, !swiglu, true, !swiglu);
+    // (without the join, K slices as those of a dense projection)
+    p.g = join ? gemm_plan(elem, rows, n, k, false, num_cu, !swiglu, true, !swiglu)
+               : gemm_plan(elem, rows, n, k, true, num_cu);
     p.scratch = (size_t)n * k * elem;
     return p;
   }

@@ -233,7 +233,7 @@ Layout layout(const dlm_model* m, int n, int n_req) {
     L.q_o = mx_plan(es_i, n, c.d_model, qd, false, true, true, false, m->num_cu);
     L.q_gu = mx_plan(es_i, n, 2 * c.d_ffn, c.d_model, true, true, true, true, m->num_cu);
     L.q_down = mx_plan(es_i, n, c.d_model, c.d_ffn, false, true, true, false, m->num_cu);
-    auto slices = [](const MxPlan& p) { return p.gemm ? 1 : p.tile.slices; };
+    auto slices = [](const MxPlan& p) { return p.gemm ? p.g.splits : p.tile.slices; };
     L.s_qkv = slices(L.q_qkv), L.s_o = slices(L.q_o), L.s_down = slices(L.q_down);
   }
   L.tiles = lm_head_tiles(L.g_lm, c.vocab);

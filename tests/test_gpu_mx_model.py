@@ -81,8 +81,7 @@ def test_packed_model_against_the_oracle(gpu, name, mode):
 @pytest.mark.parametrize("name", list(MODELS))
 def test_packed_model_is_the_dense_model_of_its_values(gpu, name):
     """Logits of a recompute step next to those of a model that holds the packed values: the
-    products differ in the order of their fp32 sums only. Rows above and below the row
-    count from which matrices are unpacked for the GEMM kernels."""
+    products differ in the order of their fp32 sums only."""
     cfg = MODELS[name]
     t = sdev.model_tensors(cfg)
     packed = engine.DeviceModel(_shape(cfg), t, 10.0, packed=True)
