@@ -465,10 +465,8 @@ hipError_t launch_linear(MxLinear a, const MxTile& tl, bool join, const LaunchSp
   DLM_LAUNCH((mx_linear_kernel<NF_, W_, NP>), grid, dim3(W_ * 64), 0, st, a)
     MX_FEW(1, 8);
     MX_FEW(2, 8);
-    if constexpr (NP == 1) {
-      MX_FEW(4, 8);
-      MX_FEW(4, 4);
-    }
+    MX_FEW(4, 8);
+    if constexpr (NP == 1) MX_FEW(4, 4);
 #undef MX_FEW
   } else {
 #define MX_TILE(KIND_, WN_, MT_, NF_, NS_)                                                         \
@@ -504,7 +502,8 @@ hipError_t launch_linear(MxLinear a, const MxTile& tl, bool join, const LaunchSp
 //    leave CUs idle) + x, once for each column tile and K slice, at 9 TB/s out of the
 //    L2s. So one row takes one column fragment a block and no slices (4096 x 4096 5.3,
 //    two fragments 6.6), and 16 rows over a long K take four in slices (4096 x 12288:
-//    four slices 13.6, one fragment, whole 18.4).
+//    four slices 13.6, one fragment, whole 18.4; the three planes of fp32 x 20.7, two
+//    fragments a block 25).
 //  * tiles (mx_tile_kernel): 4 + for each chunk of a slice 0.5, 0.84 or 1.7 (blocks of 32 x
 //    128, 64 x 128 and 128 x 256), or 0.43, 0.55 or 1.7 for each block that a CU runs.
 //    24576 x 4096: 32 rows 19.8 in the first, 128 rows 45, 38 and 63, 256 rows 82, 57
@@ -532,11 +531,11 @@ MxTile mx_tile(int elem, int rows, int n, int k, int groups, bool swiglu, bool j
   for (int s = 1; s <= (rows <= 4096 ? 8 : 1); s *= 2) {
     if ((rows <= 256 || wide) && s <= walks) {   // (small matrices: also for more than 16 rows)
       const int m_tiles = ceil_div(rows, 16);
-      for (int nf = swiglu ? 2 : 1; nf <= (planes > 1 ? 2 : 4); nf *= 2) {
+      for (int nf = swiglu ? 2 : 1; nf <= 4; nf *= 2) {
         const int n_tiles = ceil_div(n_out, cols * nf);
         const double blocks = (double)n_tiles * m_tiles * s;
         const double idle = std::max(1.0, 0.875 * num_cu / blocks);
-        const int waves = nf == 4 && blocks > num_cu ? 4 : 8;
+        const int waves = nf == 4 && planes == 1 && blocks > num_cu ? 4 : 8;
         take({kMxFew, nf, s, waves}, walks, 3.5 + mb * m_tiles * idle / 4.5 + x_mb * n_tiles / 9.0);
       }
     }
