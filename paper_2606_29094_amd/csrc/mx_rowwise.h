@@ -115,7 +115,8 @@ __global__ __launch_bounds__(256) void mx_unpack_kernel(MxView w, int k, T* __re
 // four consecutive elements of the head's first half and the same four of the
 // second, which are its rotary partners. Eight lanes hold a group of 32 of each
 // half and find its largest magnitude with three lane exchanges. Bound by memory:
-// it reads the product's fp32 slices once.
+// it reads the product's fp32 slices once (10240 rows of 32 heads, one slice: 138 us,
+// 4.6 TB/s; 32 rows, two slices: 3.6 us, the launch and two dependent loads).
 //
 // Every product of the rotation is rounded by itself (no fused multiply-add): the
 // stored codes then follow from the inputs by plain fp32 operations, and a value on
@@ -177,6 +178,7 @@ __global__ __launch_bounds__(256) void mx_append_kernel(StepPlan p, const float*
 }
 
 // The stored values: a lane writes 16 bytes of them, so that a wave's stores are whole lines.
+// Bound by memory (10240 rows of 32 heads: 49 us, 4.3 TB/s).
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void mx_read_kernel(StepPlan p, int hkv, MxKv kv,
                                                       T* __restrict__ k, T* __restrict__ v) {
