@@ -419,8 +419,8 @@ dlm_status dlm_mx_kv_read(const dlm_cache* c, int32_t layer, int32_t n_req, cons
  * n_kv_heads); q and out [N, n_q_heads head_dim] in the model dtype (out may not
  * overlap q). What the cache holds from seq_len on has no effect; rows of a
  * request with seq_len 0 become zeros. fp32 softmax; the weights enter the second
- * product as bf16 in bf16 models (at most 2^-9 off each) and as three bf16 terms
- * (24 bits) in fp32 ones. pos0 is not used, and a slot may be listed more than
+ * product as the sum of two bf16 terms in bf16 models (off by at most 2^-16 each) and of
+ * three (24 bits) in fp32 ones. pos0 is not used, and a slot may be listed more than
  * once. Workspace: as in dlm_mx_linear, for the same requests. */
 dlm_status dlm_mx_kv_attention_workspace(const dlm_cache* c, int32_t n_req, const dlm_kv_rows* rows,
                                          size_t* out_bytes);

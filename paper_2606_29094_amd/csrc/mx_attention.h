@@ -23,14 +23,15 @@ struct MxAttn {
 };
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 // V's part of LDS: kVRow bytes a key, 16-byte slot s (columns 8 s ..) of a key at v_slot.
 // head_dim 128: the 32-byte blocks of a row and the halves of a block change places with
 // the key, so that the eight rows that half a wave reads at one block, and the four keys
-// that 16 lanes write, are in distinct banks (10240 rows of 32 heads over 1280 keys 239 ->
-// 233 us against rows 288 bytes apart). head_dim 64: rows 160 bytes apart, whose
-// addresses are one base and constants (blocks exchanged: 16 requests of 64 rows over
-// 2000 keys 23.5 us against 22.9).
+// that 16 lanes write, are in distinct banks. head_dim 64: rows 160 bytes apart, whose
+// addresses are one base and constants. (With the weights in one term: rows 288 bytes
+// apart at head_dim 128, 10240 rows of 32 heads over 1280 keys 239 us against 233; blocks
+// exchanged at head_dim 64, 16 requests of 64 rows over 2000 keys 23.5 against 22.9.)
 template <int DH>
 constexpr int kVRow = DH == 128 ? 256 : DH * 2 + 32;
 template <int DH>
@@ -83,21 +84,48 @@ __device__ __forceinline__ Rescale softmax_tile(const f32x4 (&s)[4], float c, fl
 #pragma unroll
   for (int n = 0; n < 4; ++n)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float w = __builtin_amdgcn_exp2f(s[n][i] * c - mc);
-      l += w;
+    for (int i = 0; i < 4; i += 2) {
       const int e = 4 * (n & 1) + i;
-      if constexpr (NP == 1) {
-        p[n >> 1][0][e] = (bf16)w;
+      const f32x2 w = {__builtin_amdgcn_exp2f(s[n][i] * c - mc), __builtin_amdgcn_exp2f(s[n][i + 1] * c - mc)};
+      l += w[0];
+      l += w[1];
+      if constexpr (NP == 2) {             // (one conversion instruction for a pair's terms)
+        const bf16x2 hi = __builtin_convertvector(w, bf16x2);
+        const bf16x2 lo = __builtin_convertvector(w - __builtin_convertvector(hi, f32x2), bf16x2);
+        p[n >> 1][0][e] = hi[0], p[n >> 1][0][e + 1] = hi[1];
+        p[n >> 1][1][e] = lo[0], p[n >> 1][1][e + 1] = lo[1];
       } else {
-        bf16 hi, mid, lo;
-        split3(w, hi, mid, lo);
-        p[n >> 1][0][e] = hi;
-        p[n >> 1][1][e] = mid;
-        p[n >> 1][2][e] = lo;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          bf16 hi, mid, lo;
+          split3(w[u], hi, mid, lo);
+          p[n >> 1][0][e + u] = hi;
+          p[n >> 1][1][e + u] = mid;
+          p[n >> 1][2][e + u] = lo;
+        }
       }
     }
   return r;
+}
+
+// O^T += V^T P^T of a 64-key tile. The terms of a weight go into the same sums: two column
+// blocks are taken together, so that an MFMA does not wait for the one right before it.
+template <int DH, int QT, int PN>
+__device__ __forceinline__ void add_values(const char* rows, int lane, const bf16x8 (&p)[QT][2][PN],
+                                           f32x4 (&o)[DH / 16][QT]) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int d = 0; d < DH / 16; d += 2) {
+      const bf16x8 v[2] = {v_columns<DH>(rows + 32 * h * kVRow<DH>, 16 * d, lane),
+                           v_columns<DH>(rows + 32 * h * kVRow<DH>, 16 * d + 16, lane)};
+#pragma unroll
+      for (int w = PN - 1; w >= 0; --w)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int t = 0; t < QT; ++t) o[d + u][t] = mfma16_bf16(v[u], p[t][h][w], o[d + u][t]);
+    }
 }
 
 // Few query rows: one block = 16 QT items of one key/value head, wave w
@@ -109,14 +137,15 @@ __device__ __forceinline__ Rescale softmax_tile(const f32x4 (&s)[4], float c, fl
 // the B operand of O^T = V^T P^T as they stand. V is unpacked into the wave's part of
 // LDS key by key (its scales belong to keys) and read back transposed. The next tile's
 // codes are requested before the current one's are used. Bound by the chain of a wave's
-// tiles (32 rows of 32 heads: 517 keys 11 us, three tiles a wave; 4256 keys in four splits
-// 17).
-// NP bf16 terms for each query element and weight: 1 for bf16 queries (a weight is then
-// off by at most 2^-9 of itself, the rounding the output gets too), 3 for fp32 ones.
+// tiles and the join of the waves (32 rows of 32 heads: eight requests over 1280 keys 22.3
+// us, five tiles a wave; one over 4256 keys in eight splits 19.3).
+// bf16 queries: one term for an element, two for a weight (off by 2^-16 of itself at most,
+// far below the output's rounding; one term, off by 2^-8, put an error of its own size beside
+// that rounding). fp32 queries: three terms for each, which hold all 24 bits.
 template <typename T, int DH, int QT, int W>
 __global__ __launch_bounds__(W * 64, 2) void mx_attn_kernel(StepPlan p, const T* __restrict__ q,
                                                          MxAttn a, T* __restrict__ out) {
-  constexpr int NP = sizeof(T) == 2 ? 1 : 3;
+  constexpr int NP = sizeof(T) == 2 ? 1 : 3, PN = sizeof(T) == 2 ? 2 : 3;   // of a query, a weight
   constexpr int GROUPS = DH / kMxGroup;
   constexpr int KS = DH / 32;               // MFMA steps over dh
   constexpr int PER = DH / 4;               // elements of a key in a lane: 32 or 16
@@ -240,10 +269,10 @@ __global__ __launch_bounds__(W * 64, 2) void mx_attn_kernel(StepPlan p, const T*
 #pragma unroll
             for (int t = 0; t < QT; ++t) s[t][n][i] = -INFINITY;
     }
-    bf16x8 pf[QT][2][NP];
+    bf16x8 pf[QT][2][PN];
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
-      const Rescale f = softmax_tile<NP>(s[t], a.c, m[t], l[t], pf[t]);
+      const Rescale f = softmax_tile<PN>(s[t], a.c, m[t], l[t], pf[t]);
       if (f.any)
 #pragma unroll
         for (int d = 0; d < DT; ++d) o[d][t] *= f.by;
@@ -252,16 +281,7 @@ __global__ __launch_bounds__(W * 64, 2) void mx_attn_kernel(StepPlan p, const T*
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int d = 0; d < DT; ++d) {
-        const bf16x8 vf = v_columns<DH>(vrows + 32 * h * kVRow<DH>, 16 * d, lane);
-#pragma unroll
-        for (int t = 0; t < QT; ++t)
-#pragma unroll
-          for (int w = NP - 1; w >= 0; --w) o[d][t] = mfma16_bf16(vf, pf[t][h][w], o[d][t]);
-      }
+    add_values<DH, QT, PN>(vrows, lane, pf, o);
     // and its reads, before the next tile's stores
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
@@ -320,7 +340,7 @@ __global__ __launch_bounds__(W * 64, 2) void mx_attn_kernel(StepPlan p, const T*
 // S^T deals the keys (row 32 h + 16 b + 4 a + i holds key 32 h + 8 a + 4 b + i), their
 // 16-byte slots at s ^ (row & mask), so that the rows a fragment reads come from
 // distinct banks. Bound by the three pipes in turn (10240 rows of 32 heads over 1280 keys
-// 235 us, 0.91 PFLOP/s: vector units 52 % busy, LDS 50, matrix cores 38).
+// 293 us, 0.73 PFLOP/s; with the weights in one term 239).
 template <int DH, int QT, int NW>
 __global__ __launch_bounds__(NW * 64, 2) void mx_attn_shared_kernel(StepPlan p, const bf16* __restrict__ q,
                                                                  MxAttn a, bf16* __restrict__ out) {
@@ -429,22 +449,15 @@ __global__ __launch_bounds__(NW * 64, 2) void mx_attn_shared_kernel(StepPlan p, 
 #pragma unroll
             for (int t = 0; t < QT; ++t) s[t][n][i] = -INFINITY;
     }
-    bf16x8 pf[QT][2][1];
+    bf16x8 pf[QT][2][2];                 // weights in two terms, as above
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
-      const Rescale f = softmax_tile<1>(s[t], a.c, m[t], l[t], pf[t]);
+      const Rescale f = softmax_tile<2>(s[t], a.c, m[t], l[t], pf[t]);
       if (f.any)
 #pragma unroll
         for (int d = 0; d < DT; ++d) o[d][t] *= f.by;
     }
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int d = 0; d < DT; ++d) {
-        const bf16x8 vf = v_columns<DH>(st + KBYTES + 32 * h * kVRow<DH>, 16 * d, lane);
-#pragma unroll
-        for (int t = 0; t < QT; ++t) o[d][t] = mfma16_bf16(vf, pf[t][h][0], o[d][t]);
-      }
+    add_values<DH, QT, 2>(st + KBYTES, lane, pf, o);
   }
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
@@ -550,37 +563,41 @@ size_t mx_attention_scratch(int rows, int hq, int dh, int splits) {
 }
 
 // Kernel and key splits. Times in us on MI355X (256 CUs), head_dim 128: 6.5, and for each
-// 64-key tile that a block walks 0.58, 1.07 or 1.65 (32 items whose four waves split the
-// keys, 64 and 128 items that share them) while every CU has one block, or 0.48, 0.84 or
-// 1.34 for each block that a CU runs where it has more; head_dim 64 takes 0.7 and 0.55 of
-// these. Splits add the joining kernel, 3.5, and their partials' way at 3 TB/s.
-// So 32 rows over 1280 keys of 8 requests, 32 heads, take blocks of 32 (18.6; of 64: 28.3),
-// 28/4 heads, 64 requests of 64 rows over 1024 keys blocks of 128 (95; 64: 105, 32: 130),
-// and one request of 32 rows over 4256 keys, 32 heads, eight splits (20.3; whole 25.5).
+// 64-key tile that a block walks 0.555, 1.3 or 2.03 (32 items whose four waves split the
+// keys, 64 and 128 items that share them) while every CU has one block, or 0.48, 1.04 or
+// 1.62 for each block that a CU runs where it has more; a block's start and end (the join of
+// its waves) count as 9, 1 and 1.5 tiles; head_dim 64 takes 0.67 and 0.6 of these, and 0.55 of
+// the tiles for start and end. Splits add the joining kernel, 3.5, and their partials' way at
+// 3 TB/s.
+// So 32 rows over 1280 keys of 8 requests, 32 heads, take blocks of 32 (22.3; of 64: 33.7),
+// 28/4 heads, 16 requests of 64 rows over 1024 keys blocks of 64 (40.4; 128: 41.5, 32: 47.6),
+// 64 of them blocks of 128 (113; 64: 125, 32: 146), and one request of 32 rows over 4256 keys,
+// 32 heads, eight splits (19.3; four 22.5).
 // fp32 queries have the first kernel alone, with 16 items.
 MxAttnPlan mx_attention_plan(const StepPlan& p, int hq, int hkv, int dh, size_t elem,
                              size_t scratch_bytes, int num_cu) {
-  struct Kind { int kind, items, waves; double one, more; };
-  static const Kind kinds[] = {{kMxAttnFew, 32, 4, 0.58, 0.48},
-                               {kMxAttnShared64, 64, 1, 1.07, 0.84},
-                               {kMxAttnShared128, 128, 1, 1.65, 1.34}};
+  struct Kind { int kind, items, waves; double one, more, ends; };
+  static const Kind kinds[] = {{kMxAttnFew, 32, 4, 0.555, 0.48, 9.0},
+                               {kMxAttnShared64, 64, 1, 1.3, 1.04, 1.0},
+                               {kMxAttnShared128, 128, 1, 2.03, 1.62, 1.5}};
   const int gh = hq / hkv;
-  const double one = dh == 64 ? 0.7 : 1.0, more = dh == 64 ? 0.55 : 1.0;
+  const double one = dh == 64 ? 0.67 : 1.0, more = dh == 64 ? 0.6 : 1.0, ends = dh == 64 ? 0.55 : 1.0;
   MxAttnPlan best;
   double best_t = 1e30;
   for (const Kind& k : kinds) {
     if (elem != 2 && k.kind != kMxAttnFew) break;
     const int items = elem == 2 ? k.items : 16;
     for (int s = 1; s <= kMxSplits; s *= 2) {
-      long blocks = 0, work = 0;
-      int longest = 0;
+      long blocks = 0;
+      double work = 0.0, longest = 0.0;
       for (int r = 0; r < p.n_req; ++r) {
         const long b = (long)hkv * ceil_div(p.r[r].nrows * gh, items) * s;
         int tiles = ceil_div(ceil_div(p.r[r].seq_len, 64), s);
         tiles = ceil_div(tiles, k.waves) * k.waves;
         blocks += b;
-        work += b * tiles;
-        if (b) longest = std::max(longest, tiles);
+        const double walk = tiles + k.ends * ends;
+        work += b * walk;
+        if (b) longest = std::max(longest, walk);
       }
       if (s > 1 && (blocks > num_cu || mx_attention_scratch(p.n_rows, hq, dh, s) > scratch_bytes)) break;
       const double fill = (double)blocks / num_cu;   // blocks of a CU; few of them come whole
