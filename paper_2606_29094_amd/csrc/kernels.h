@@ -224,6 +224,7 @@ struct MxLinear {
   long ldx, plane;
   MxView w;
   int m, k;                // k: elements of x a row holds (a multiple of 8)
+  int tail;                // codes of the last group that belong to the matrix (0: all)
   void* y;
   long ldy;
   float* slices;           // [slice][m][n] partial sums, where K is sliced
