@@ -380,7 +380,8 @@ dlm_status dlm_load_weights_mx(const dlm_config* cfg, const dlm_weights_mx* w, d
  * may have one. Layout: per layer the codes of the keys
  * [slot][kv_head][pos][head_dim / 2], the codes of the values, the scales of the
  * keys [slot][kv_head][pos][head_dim / 32] and the scales of the values, each
- * part rounded up to 256 bytes, slots rounded up to 64 positions. */
+ * part rounded up to 256 bytes, slots rounded up to 64 positions; scale bytes of
+ * attended positions are those that packing writes (2 .. 252, 255). */
 dlm_status dlm_kv_cache_alloc_mx(const dlm_model* m, int32_t n_slots, int32_t max_seq_len,
                                  void* dev_buf, size_t buf_bytes, size_t* required_bytes,
                                  dlm_cache** out);

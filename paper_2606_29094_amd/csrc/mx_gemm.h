@@ -51,6 +51,28 @@ __device__ __forceinline__ u32x4 keep_codes(u32x4 c, int keep) {
   return c;
 }
 
+// Infinite weights meet the first term of an fp32 x alone, whose product is the right
+// infinity; the others would be 0 * inf, or an infinity of the other sign. Whether a scale
+// byte makes any code infinite, and eight weights with the infinite ones zero.
+__device__ __forceinline__ bool mx_may_be_infinite(uint32_t e) { return e - 253u < 2u; }
+__device__ __forceinline__ bf16x8 finite_or_zero(const bf16x8& w) {
+  u32x4 v = __builtin_bit_cast(u32x4, w);
+#pragma unroll
+  for (int d = 0; d < 4; ++d) {
+    if ((v[d] & 0x7fffu) == 0x7f80u) v[d] &= 0xffff0000u;
+    if ((v[d] & 0x7fff0000u) == 0x7f800000u) v[d] &= 0xffffu;
+  }
+  return __builtin_bit_cast(bf16x8, v);
+}
+
+// The same of a group's codes: 4 and 6 under byte 253, and 2 and 3 under 254.
+__device__ __forceinline__ u32x4 finite_or_zero(u32x4 c, uint32_t e) {
+#pragma unroll
+  for (int d = 0; d < 4; ++d)
+    c[d] &= ~(15u * (c[d] >> 2 & (e == 254u ? ~0u : c[d] >> 1) & 0x11111111u));
+  return c;
+}
+
 __device__ __forceinline__ float silu_mul(float g, float u) { return g / (1.f + __expf(-g)) * u; }
 
 // Up to 16 rows. One block: 16 NF columns, W waves that take the 512-wide k ranges
@@ -106,6 +128,14 @@ __global__ __launch_bounds__(W * 64) void mx_linear_kernel(MxLinear a) {
                           : u32x4{0u, 0u, 0u, 0u};
       scales[f] = *reinterpret_cast<const u32x4*>(ws[f] + 16 * s);
     }
+    bool infinite = false;   // (of any lane: a lane looks at its own groups)
+    if constexpr (NP > 1) {
+#pragma unroll
+      for (int f = 0; f < NF; ++f)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) infinite |= mx_may_be_infinite((scales[f][c] >> (8 * g)) & 255u);
+      infinite = __any(infinite);
+    }
     bf16x8 xv[2][XJ][NP];
     auto xload = [&](int i) {   // x of steps XJ i .. of the walk
 #pragma unroll
@@ -144,9 +174,14 @@ __global__ __launch_bounds__(W * 64) void mx_linear_kernel(MxLinear a) {
           b[f] = mx_bf16x8(codes[c][f][j], mx_scale(e));
         }
 #pragma unroll
-        for (int p = 0; p < NP; ++p)
+        for (int p = 0; p < NP; ++p) {
+          if (NP > 1 && p == 1 && infinite) {
+#pragma unroll
+            for (int f = 0; f < NF; ++f) b[f] = finite_or_zero(b[f]);
+          }
 #pragma unroll
           for (int f = 0; f < NF; ++f) acc[f] = mfma16_bf16(xv[i & 1][u][p], b[f], acc[f]);
+        }
       }
     }
   };
@@ -228,9 +263,10 @@ __global__ __launch_bounds__(W * 64) void mx_linear_kernel(MxLinear a) {
 __device__ const uint4 kZeros[1] = {};   // what x holds behind k
 
 // TAIL: k is not a multiple of 32 (an instance of its own: the test of each chunk for the
-// codes behind k costs 1 to 5 %, 256 rows of 4096 x 4096 18.9 us against 17.9).
+// codes behind k costs 1 to 5 %, 256 rows of 4096 x 4096 18.9 us against 17.9). The second
+// launch bound keeps four blocks of the smallest tile on a CU.
 template <int WN, int MT, int NF, int NS, bool PLANES, bool TAIL>
-__global__ __launch_bounds__(WN * 64) void mx_tile_kernel(MxLinear a, int n_tiles, int m_tiles) {
+__global__ __launch_bounds__(WN * 64, MT == 2 ? 4 : 1) void mx_tile_kernel(MxLinear a, int n_tiles, int m_tiles) {
   typedef typename std::conditional<PLANES, float, bf16>::type T;
   constexpr int BM = 16 * MT, STAGE = BM * 256;
   constexpr int XL = STAGE / 1024 / WN;    // direct loads of a wave for a stage
@@ -310,7 +346,7 @@ __global__ __launch_bounds__(WN * 64) void mx_tile_kernel(MxLinear a, int n_tile
     for (int f = 0; f < NF; ++f)
       scales[b][f] = *reinterpret_cast<const u32x4*>(sb + (f >= H ? up_scales : 0) + ws[f]);
   };
-  auto compute = [&](int b, int sb, int i, int c4) {
+  auto compute = [&](int b, int sb, int i, int c4, bool infinite) {
     const int s = walk(i), c = 4 * (PLANES ? s % walks : s) + c4;
     const int left = a.w.groups - 4 * c;   // groups of the chunk
     const uint32_t keep = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
@@ -319,6 +355,13 @@ __global__ __launch_bounds__(WN * 64) void mx_tile_kernel(MxLinear a, int n_tile
     if (TAIL && c == (a.w.groups - 1) / 4 && 4 * c + g == a.w.groups - 1) {
 #pragma unroll
       for (int f = 0; f < NF; ++f) codes[b][f] = keep_codes(codes[b][f], a.tail);
+    }
+    if (PLANES && infinite) {
+#pragma unroll
+      for (int f = 0; f < NF; ++f) {
+        const uint32_t e = (scales[sb][f][c4] >> (8 * g)) & 255u;
+        if (mx_may_be_infinite(e)) codes[b][f] = finite_or_zero(codes[b][f], e);
+      }
     }
 #pragma unroll
     for (int f = 0; f < NF; ++f) {
@@ -370,15 +413,23 @@ __global__ __launch_bounds__(WN * 64) void mx_tile_kernel(MxLinear a, int n_tile
   }
   auto turn = [&](int i, auto parity) {
     constexpr int P = decltype(parity)::value;
+    bool infinite = false;   // whether a weight of this walk meets zeros that it would make NaN
 #pragma unroll
     for (int c4 = 0; c4 < 4; ++c4) {
       wait_vmcnt<(NS - 2) * LOADS>();      // the chunk is here, later ones may be in flight,
       __builtin_amdgcn_s_barrier();        // and every wave is done with the one before
       constexpr int D = NS - 1;
       load((c4 + D) % NS, i + (c4 + D) / 4, (c4 + D) % 4);
+      if (PLANES && c4 == 0 && walk(i) >= walks) {   // the second and third plane
+#pragma unroll
+        for (int f = 0; f < NF; ++f)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) infinite |= mx_may_be_infinite((scales[P][f][c] >> (8 * g)) & 255u);
+        infinite = __any(infinite);
+      }
       if (c4 == 0) load_scales(1 - P, i + 1);
       __builtin_amdgcn_sched_barrier(0);
-      compute(c4 % NS, P, i, c4);
+      compute(c4 % NS, P, i, c4, infinite);
       __builtin_amdgcn_sched_barrier(0);
     }
   };

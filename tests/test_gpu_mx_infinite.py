@@ -39,3 +39,35 @@ def test_linear_ignores_infinite_codes_behind_k(gpu, m, n, k, dtype):
     got, xx = _linear(gpu, x, codes, scales, n, k), x.double()
     assert bool(got.isfinite().all())
     assert bool(((got - xx @ w.T).abs() <= ref.product_bound(xx, w, dtype)).all())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("m,n,k", [(1, 48, 64), (5, 48, 512), (16, 96, 1024), (33, 96, 64), (70, 2048, 4096),
+                                   (300, 96, 224), (600, 4096, 512)])
+def test_linear_infinite_weights(gpu, m, n, k, dtype):
+    """An infinite weight makes its column's outputs infinite, of the sign of its input, whatever
+    the input's type; other weights of the same groups stay what they are."""
+    codes, scales = ref.pack(_randn(n, k, seed=k))
+    at = torch.arange(n) % (k // 32)                       # of each row, one group
+    nib = torch.randint(0, 3, (n, 32), generator=torch.Generator().manual_seed(1))
+    odd = torch.arange(n) % 2 == 1                         # of each second row, one code
+    which = torch.arange(n) * 7 % 32
+    nib[odd, which[odd]] = (6 + 8 * (torch.arange(n) // 2 % 2))[odd]
+    nib[torch.arange(n) % 8 == 3, 0] = 12 + torch.arange(n)[torch.arange(n) % 8 == 3] // 8 % 4
+    packed = (nib[:, 0::2] + 16 * nib[:, 1::2]).to(torch.uint8)
+    for r in range(n):
+        codes[r, 16 * at[r]:16 * at[r] + 16] = packed[r]
+        scales[r, at[r]] = 253 + r // 4 % 2
+    w = ref.values(codes, scales, k)
+    w = torch.where(w.abs() >= 2.0 ** 128, torch.sign(w) * float("inf"), w)
+    x = _randn(m, k, seed=2, std=2.0 ** -60).to(dtype)
+    got, xx = _linear(gpu, x, codes, scales, n, k), x.double()
+    want = torch.empty(m, n, dtype=torch.float64)
+    for r in range(n):                                     # (several infinities: inf or NaN)
+        want[:, r] = (xx * w[r]).sum(1)
+    assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got.isinf(), want.isinf())
+    assert torch.equal(torch.sign(got)[want.isinf()], torch.sign(want)[want.isinf()])
+    fin = want.isfinite()
+    assert fin.any() and want.isinf().any()
+    bound = ref.product_bound(xx, torch.where(w.isfinite(), w, torch.zeros_like(w)), dtype)
+    assert bool(((got - want).abs() <= bound)[fin].all())
