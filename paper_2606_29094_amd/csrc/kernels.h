@@ -209,11 +209,11 @@ struct MxPlan {
   MxTile tile{};
   size_t stage = 0, scratch = 0;
 };
-// x_aligned, y_aligned: the buffer and its rows start at multiples of 16 bytes (rows of x at
-// most kMxTileK elements apart). join: K slices are added by the product; otherwise (DLM_MX_STORE alone)
+// x_aligned, y_aligned: the buffer and its rows start at multiples of 16 bytes (rows of x, ldx
+// elements apart, at most kMxTileK). join: K slices are added by the product; otherwise (DLM_MX_STORE alone)
 // y takes tile.slices (g.splits) of them, [slices, rows, n], for a consumer that adds them.
-MxPlan mx_plan(int elem, int rows, int n, int k, bool swiglu, bool x_aligned, bool y_aligned, bool join,
-               int num_cu);
+MxPlan mx_plan(int elem, int rows, int n, int k, long ldx, bool swiglu, bool x_aligned, bool y_aligned,
+               bool join, int num_cu);
 // epilogue: dlm_mx_epilogue
 template <typename T>
 hipError_t mx_matmul(const MxPlan& plan, const T* x, long ldx, int rows, const MxView& w, int k,

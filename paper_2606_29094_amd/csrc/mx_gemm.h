@@ -636,10 +636,12 @@ MxTile mx_tile(int elem, int rows, int n, int k, int groups, bool swiglu, bool j
 // 9 / 25, 41 x 2608 at 3636 14 / 55.)
 constexpr int kMxGemmRows = 2048, kMxGemmCols = 1024;
 
-MxPlan mx_plan(int elem, int rows, int n, int k, bool swiglu, bool x_aligned, bool y_aligned, bool join,
-               int num_cu) {
+MxPlan mx_plan(int elem, int rows, int n, int k, long ldx, bool swiglu, bool x_aligned, bool y_aligned,
+               bool join, int num_cu) {
   MxPlan p;
-  if (elem == 2 && x_aligned && y_aligned && rows >= kMxGemmRows && n >= kMxGemmCols && k % 8 == 0 &&
+  // (the GEMM kernels address their operands by 32-bit element offsets)
+  const bool near = std::max((double)rows * ldx, (double)n * k) < 4294967296.0;
+  if (elem == 2 && near && x_aligned && y_aligned && rows >= kMxGemmRows && n >= kMxGemmCols && k % 8 == 0 &&
       (!swiglu || n % 32 == 0)) {
     p.gemm = true;
     // (without the join, K slices as those of a dense projection)

@@ -229,10 +229,10 @@ Layout layout(const dlm_model* m, int n, int n_req) {
   L.s_down = L.g_down.splits;
   if (!m->mx.empty()) {
     // (the rotation and the residual norms add K slices as they read them)
-    L.q_qkv = mx_plan(es_i, n, qkv_dim, c.d_model, false, true, true, false, m->num_cu);
-    L.q_o = mx_plan(es_i, n, c.d_model, qd, false, true, true, false, m->num_cu);
-    L.q_gu = mx_plan(es_i, n, 2 * c.d_ffn, c.d_model, true, true, true, true, m->num_cu);
-    L.q_down = mx_plan(es_i, n, c.d_model, c.d_ffn, false, true, true, false, m->num_cu);
+    L.q_qkv = mx_plan(es_i, n, qkv_dim, c.d_model, c.d_model, false, true, true, false, m->num_cu);
+    L.q_o = mx_plan(es_i, n, c.d_model, qd, qd, false, true, true, false, m->num_cu);
+    L.q_gu = mx_plan(es_i, n, 2 * c.d_ffn, c.d_model, c.d_model, true, true, true, true, m->num_cu);
+    L.q_down = mx_plan(es_i, n, c.d_model, c.d_ffn, c.d_ffn, false, true, true, false, m->num_cu);
     auto slices = [](const MxPlan& p) { return p.gemm ? p.g.splits : p.tile.slices; };
     L.s_qkv = slices(L.q_qkv), L.s_o = slices(L.q_o), L.s_down = slices(L.q_down);
   }
@@ -1153,8 +1153,8 @@ dlm_status dlm_mx_linear_workspace(int32_t dtype, int32_t m_rows, const dlm_mx* 
   // whatever the addresses and the row strides of x and y turn out to be
   size_t need = 0;
   for (int al = 0; al < 4; ++al)
-    need = std::max(need, mx_plan(dtype == DLM_BF16 ? 2 : 4, m_rows, w->n, w->k, epilogue == DLM_MX_SWIGLU,
-                                  al & 1, al & 2, true, device_cus()).scratch);
+    need = std::max(need, mx_plan(dtype == DLM_BF16 ? 2 : 4, m_rows, w->n, w->k, w->k,
+                                  epilogue == DLM_MX_SWIGLU, al & 1, al & 2, true, device_cus()).scratch);
   *out_bytes = need;
   return DLM_OK;
 }
@@ -1174,7 +1174,7 @@ dlm_status dlm_mx_linear(int32_t dtype, const void* x, int64_t ldx, int32_t m_ro
   const int es = dtype == DLM_BF16 ? 2 : 4;
   const bool x_al = aligned16(x) && ldx * es % 16 == 0 && w->k * (long)es % 16 == 0 && ldx <= kMxTileK;
   const bool y_al = aligned16(y) && ldy % 8 == 0 && ldy < INT32_MAX;
-  const MxPlan plan = mx_plan(es, m_rows, w->n, w->k, swiglu, x_al, y_al, true, device_cus());
+  const MxPlan plan = mx_plan(es, m_rows, w->n, w->k, (long)ldx, swiglu, x_al, y_al, true, device_cus());
   if (plan.scratch) {
     if (!workspace) return fail(DLM_EINVAL, "workspace is NULL");
     if (reinterpret_cast<uintptr_t>(workspace) % 256 != 0)
