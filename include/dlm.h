@@ -478,6 +478,26 @@ dlm_status dlm_debug_attention_plan(int32_t n_q_heads, int32_t n_kv_heads, int32
                                     size_t scratch_bytes, int32_t num_cu, int32_t* kernel,
                                     int32_t* splits);
 
+/* Test hooks for the planners of the 4-bit calls (host only), on num_cu CUs.
+ * dlm_debug_mx_linear_plan: how m_rows rows of dtype, ldx elements apart, are multiplied
+ * with a packed [n, k] matrix. aligned: bit 0 where x and its rows start at multiples
+ * of 16 bytes, bit 1 where y and its rows do. join 0 (DLM_MX_STORE only): K slices are left
+ * to the kernel that reads y, as in a packed model's step; else they are joined.
+ * out = way (0: straight from the codes, 16 rows a block; 1 to 3: in tiles of 32 x 128,
+ * 64 x 128 and 128 x 256; 4: unpacked, for the GEMM kernels), K slices, and whether x is copied
+ * first (1 or 0). dlm_debug_mx_attention_plan: the kernel (0: blocks of 32 (row, head) items,
+ * 16 for fp32, whose waves split the keys; 1 and 2: of 64 and 128 that share them) and the
+ * key splits for n_req requests of rows[r] rows over seq_len[r] keys (0 or more each),
+ * with scratch_bytes of scratch. DLM_EINVAL as in the calls themselves, for NULL arrays and
+ * outputs, no rows in the product, a negative count, or num_cu below 1. */
+dlm_status dlm_debug_mx_linear_plan(int32_t dtype, int32_t m_rows, int32_t n, int32_t k, int64_t ldx,
+                                    int32_t epilogue, int32_t aligned, int32_t join, int32_t num_cu,
+                                    int32_t out[3]);
+dlm_status dlm_debug_mx_attention_plan(int32_t dtype, int32_t n_q_heads, int32_t n_kv_heads,
+                                       int32_t head_dim, int32_t n_req, const int32_t* rows,
+                                       const int32_t* seq_len, size_t scratch_bytes, int32_t num_cu,
+                                       int32_t* kernel, int32_t* splits);
+
 /* Kernel timing. While enabled, every kernel the library enqueues for this
  * model (or, when only_class is not NULL, every kernel of that class; see also
  * dlm_profile_sample) is timed by a pair of HIP events carried in the kernel's

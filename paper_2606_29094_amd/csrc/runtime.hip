@@ -1192,6 +1192,54 @@ dlm_status dlm_mx_linear(int32_t dtype, const void* x, int64_t ldx, int32_t m_ro
   return DLM_OK;
 }
 
+dlm_status dlm_debug_mx_linear_plan(int32_t dtype, int32_t m_rows, int32_t n, int32_t k, int64_t ldx,
+                                    int32_t epilogue, int32_t aligned, int32_t join, int32_t num_cu,
+                                    int32_t out[3]) {
+  g_err.clear();
+  uint8_t unused[16] __attribute__((aligned(16)));   // (buffers for the check; not looked at)
+  const dlm_mx w{unused, unused, n, k};
+  dlm_status s = check_linear(dtype, m_rows, &w, epilogue);
+  if (s != DLM_OK) return s;
+  if (!out) return fail(DLM_EINVAL, "out is NULL");
+  if (m_rows < 1 || ldx < k || num_cu < 1 || (!join && epilogue != DLM_MX_STORE))
+    return fail(DLM_EINVAL, "%d rows, row stride %lld, %d CUs, join %d", m_rows, (long long)ldx, num_cu, join);
+  const MxPlan p = mx_plan(dtype == DLM_BF16 ? 2 : 4, m_rows, n, k, (long)ldx, epilogue == DLM_MX_SWIGLU,
+                           aligned & 1, aligned & 2, join != 0, num_cu);
+  out[0] = p.gemm ? 4 : p.tile.kind;
+  out[1] = p.gemm ? p.g.splits : p.tile.slices;
+  out[2] = p.staged;
+  return DLM_OK;
+}
+
+dlm_status dlm_debug_mx_attention_plan(int32_t dtype, int32_t n_q_heads, int32_t n_kv_heads,
+                                       int32_t head_dim, int32_t n_req, const int32_t* rows,
+                                       const int32_t* seq_len, size_t scratch_bytes, int32_t num_cu,
+                                       int32_t* kernel, int32_t* splits) {
+  g_err.clear();
+  dlm_status s = check_dtype(dtype);
+  if (s != DLM_OK) return s;
+  if (!rows || !seq_len || !kernel || !splits) return fail(DLM_EINVAL, "NULL array or output");
+  if (n_req < 1 || n_req > kMaxReq) return fail(DLM_EINVAL, "n_req %d outside [1, %d]", n_req, kMaxReq);
+  if (n_q_heads < 1 || n_kv_heads < 1 || n_q_heads % n_kv_heads != 0 || num_cu < 1 ||
+      (head_dim != 64 && head_dim != 128))
+    return fail(DLM_EINVAL, "heads %d / %d of %d on %d CUs", n_q_heads, n_kv_heads, head_dim, num_cu);
+  StepPlan p{};
+  p.n_req = n_req;
+  for (int r = 0; r < n_req; ++r) {
+    if (rows[r] < 0 || rows[r] > DLM_MAX_SEQ || seq_len[r] < 0 || seq_len[r] > DLM_MAX_SEQ)
+      return fail(DLM_EINVAL, "request %d: %d rows over %d keys", r, rows[r], seq_len[r]);
+    p.r[r].row0 = p.n_rows;
+    p.r[r].nrows = rows[r];
+    p.r[r].seq_len = seq_len[r];
+    p.n_rows += rows[r];
+  }
+  const MxAttnPlan ap = mx_attention_plan(p, n_q_heads, n_kv_heads, head_dim, dtype == DLM_BF16 ? 2 : 4,
+                                          scratch_bytes, num_cu);
+  *kernel = ap.kind;
+  *splits = ap.splits;
+  return DLM_OK;
+}
+
 dlm_status dlm_mx_kv_append(dlm_cache* c, int32_t layer, int32_t n_req, const dlm_kv_rows* rows,
                             const float* qkv, int32_t splits, const float* rot, void* q_out,
                             void* stream) {

@@ -35,7 +35,8 @@ EXPORTS = ["dlm_load_weights", "dlm_model_destroy", "dlm_workspace_bytes",
            "dlm_profile_sample", "dlm_ceiling_mfma", "dlm_ceiling_copy", "dlm_last_error",
            "dlm_mx_bytes", "dlm_mx_pack", "dlm_mx_unpack", "dlm_mx_linear_workspace",
            "dlm_mx_linear", "dlm_load_weights_mx", "dlm_kv_cache_alloc_mx", "dlm_mx_kv_append",
-           "dlm_mx_kv_read", "dlm_mx_kv_attention_workspace", "dlm_mx_kv_attention"]
+           "dlm_mx_kv_read", "dlm_mx_kv_attention_workspace", "dlm_mx_kv_attention",
+           "dlm_debug_mx_linear_plan", "dlm_debug_mx_attention_plan"]
 
 
 class DlmConfig(ctypes.Structure):
@@ -180,6 +181,11 @@ def lib():
                                                     POINTER(c_size_t)]
         L.dlm_mx_kv_attention.argtypes = [c_void_p, c_int32, c_int32, POINTER(DlmKvRows),
                                           c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
+        L.dlm_debug_mx_linear_plan.argtypes = [c_int32, c_int32, c_int32, c_int32, c_int64, c_int32,
+                                               c_int32, c_int32, c_int32, POINTER(c_int32)]
+        L.dlm_debug_mx_attention_plan.argtypes = [c_int32, c_int32, c_int32, c_int32, c_int32,
+                                                  POINTER(c_int32), POINTER(c_int32), c_size_t,
+                                                  c_int32, POINTER(c_int32), POINTER(c_int32)]
         L.dlm_last_error.argtypes = []
         L.dlm_last_error.restype = ctypes.c_char_p
         for name in ["dlm_load_weights", "dlm_workspace_bytes", "dlm_kv_cache_alloc",
@@ -191,7 +197,8 @@ def lib():
                      "dlm_profile_read", "dlm_profile_sample", "dlm_mx_bytes", "dlm_mx_pack",
                      "dlm_mx_unpack", "dlm_mx_linear_workspace", "dlm_mx_linear",
                      "dlm_load_weights_mx", "dlm_kv_cache_alloc_mx", "dlm_mx_kv_append",
-                     "dlm_mx_kv_read", "dlm_mx_kv_attention_workspace", "dlm_mx_kv_attention"]:
+                     "dlm_mx_kv_read", "dlm_mx_kv_attention_workspace", "dlm_mx_kv_attention",
+                     "dlm_debug_mx_linear_plan", "dlm_debug_mx_attention_plan"]:
             getattr(L, name).restype = c_int32
         _lib = L
     return _lib
@@ -558,6 +565,27 @@ def mx_kv_attention(cache, layer: int, rows, q, out, workspace=None, stream=None
     else:
         st, (ws, size) = _on(stream, q, out, workspace, cache=cache), _scratch(workspace)
     check(lib().dlm_mx_kv_attention(cache, layer, len(rows), rows, q.data_ptr(), out.data_ptr(), ws, size, st))
+
+
+def debug_mx_linear_plan(dtype, m_rows: int, n: int, k: int, epilogue: int = DLM_MX_STORE,
+                         ldx: int = 0, aligned: int = 3, join: bool = True, num_cu: int = 256):
+    """(way, K slices, whether x is copied first) of a product with a packed matrix
+    (dlm_debug_mx_linear_plan); ldx 0: contiguous rows."""
+    out = (c_int32 * 3)()
+    check(lib().dlm_debug_mx_linear_plan(_dtype_id(dtype), m_rows, n, k, ldx or k, epilogue, aligned,
+                                         1 if join else 0, num_cu, out))
+    return out[0], out[1], bool(out[2])
+
+
+def debug_mx_attention_plan(dtype, hq: int, hkv: int, dh: int, rows, lens,
+                            scratch_bytes: int = 1 << 62, num_cu: int = 256):
+    """(kernel, key splits) of the attention over a 4-bit cache (dlm_debug_mx_attention_plan)."""
+    arr = lambda v: (c_int32 * len(v))(*v)
+    kernel, splits = c_int32(), c_int32()
+    check(lib().dlm_debug_mx_attention_plan(_dtype_id(dtype), hq, hkv, dh, len(rows), arr(rows), arr(lens),
+                                            scratch_bytes, num_cu, ctypes.byref(kernel),
+                                            ctypes.byref(splits)))
+    return kernel.value, splits.value
 
 
 def profile_enable(model, on: bool, only_class: str | None = None):
