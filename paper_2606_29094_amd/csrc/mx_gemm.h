@@ -628,21 +628,26 @@ MxTile mx_tile(int elem, int rows, int n, int k, int groups, bool swiglu, bool j
   return best;
 }
 
-// From this many rows on a bf16 matrix is unpacked once and goes through the GEMM kernels.
-// Straight from the codes / unpacked (the unpacking included), us: 24576 x 4096 at 1024
-// rows 183 / 222, at 2048 357 / 351, at 4096 736 / 631; 4096 x 12288 112 / 121, 179 / 193
-// and 370 / 332. (fp32 stays with the codes: three bf16 products take half of an fp32
-// one, 24576 x 4096 at 1024 rows 496. Narrow matrices stay too: 512 x 688 at 3815 rows
-// 9 / 25, 41 x 2608 at 3636 14 / 55.)
+// From this many rows on a bf16 matrix is unpacked once and goes through the GEMM kernels, where
+// it holds kMxGemmValues or more and k is a multiple of 64, as the fast ones of those take it.
+// Straight from the codes / unpacked (the unpacking included), us, at 2048, 3000 and 4096
+// rows: 24576 x 4096 SwiGLU 361 / 354, 548 / 514, 752 / 645; 4096 x 12288 176 / 187, 343 /
+// 297, 365 / 307; 4608 x 3584 87 / 79, 107 / 95, 160 / 121. Other k: 4096 x 4088 71 / 114,
+// 133 / 174, 139 / 195; 24576 x 3608 SwiGLU 366 / 518, 540 / 771, 741 / 1029. Smaller
+// matrices: 2048 x 2048 25 / 30, 34 / 48, 39 / 52; 1088 x 1024 15 / 19, 16 / 19, 21 / 26.
+// (At 1024 rows 24576 x 4096 182 / 217, 12288 x 4096 110 / 105. fp32 stays with the codes: three bf16 products take
+// half of an fp32 one, 24576 x 4096 at 1024 rows 503. Narrow matrices stay too: 41 x 2608 at
+// 3636 rows 14 / 55.)
 constexpr int kMxGemmRows = 2048, kMxGemmCols = 1024;
+constexpr long kMxGemmValues = 1L << 23;
 
 MxPlan mx_plan(int elem, int rows, int n, int k, long ldx, bool swiglu, bool x_aligned, bool y_aligned,
                bool join, int num_cu) {
   MxPlan p;
   // (the GEMM kernels address their operands by 32-bit element offsets)
   const bool near = std::max((double)rows * ldx, (double)n * k) < 4294967296.0;
-  if (elem == 2 && near && x_aligned && y_aligned && rows >= kMxGemmRows && n >= kMxGemmCols && k % 8 == 0 &&
-      (!swiglu || n % 32 == 0)) {
+  if (elem == 2 && near && x_aligned && y_aligned && rows >= kMxGemmRows && n >= kMxGemmCols && k % 64 == 0 &&
+      (long)n * k >= kMxGemmValues && (!swiglu || n % 32 == 0)) {
     p.gemm = true;
     // (without the join, K slices as those of a dense projection)
     p.g = join ? gemm_plan(elem, rows, n, k, false, num_cu, !swiglu, true, !swiglu)

@@ -33,6 +33,19 @@ def test_operands_of_32_bits_are_unpacked_others_not():
     assert plan(2048, 4096, 4096, ldx=1 << 21) != UNPACKED
 
 
+def test_unpacked_where_the_gemm_kernels_are_faster():
+    """Both sides of each line, at the sizes that were measured."""
+    for n, k, epilogue in [(24576, 4096, SWIGLU), (4096, 12288, ADD), (4608, 3584, STORE), (4096, 4096, STORE)]:
+        for m in (3000, 4096):
+            assert dlm.debug_mx_linear_plan(BF16, m, n, k, epilogue)[0] == UNPACKED
+            # k no multiple of 64: those kernels stage such operands through registers
+            for odd in (k - 8, k - 32, k + 8):
+                assert dlm.debug_mx_linear_plan(BF16, m, n, odd, epilogue)[0] != UNPACKED
+    for m in (2048, 4096):                  # small matrices
+        for n, k in [(2048, 2048), (1088, 1024), (1040, 1032), (512, 18944)]:
+            assert dlm.debug_mx_linear_plan(BF16, m, n, k)[0] != UNPACKED
+
+
 def test_buffers_that_vector_accesses_cannot_take():
     for aligned in (0, 2):                  # rows of x: copied first, straight from the codes
         way, _, staged = dlm.debug_mx_linear_plan(BF16, 4096, 4096, 4096, aligned=aligned)
