@@ -464,13 +464,14 @@ __global__ __launch_bounds__(WN * 64, MT == 2 ? 4 : 1) void mx_tile_kernel(MxLin
     const int n = n0 + 16 * (a.swiglu ? f % H : f) + col;
     o[f] = n < n_end ? out + (m0 + 4 * g) * ldo + n + (a.swiglu && f >= H ? n_end : 0) : nullptr;
   }
-  if (a.add && !sliced) {    // all of the old values before the first store
+  if (a.add && !sliced && n0 < n_end) {   // all of the old values before the first store
     // In the large tiles no load is conditional, so that they go out together: 3369 x 4187
     // outputs of 382 inputs 65 us against 93. In the small ones the registers that this
     // takes would cost a block a CU: 300 rows of 3584 x 18944 71 us against 65.
     const float* p[NF];
 #pragma unroll
-    for (int f = 0; f < NF; ++f) p[f] = out + min(n0 + 16 * f + col, n_end - 1);
+    for (int f = 0; f < NF; ++f)   // (behind the last column: the wave's own first one, not used)
+      p[f] = out + (n0 + 16 * f + col < n_end ? n0 + 16 * f + col : n0);
 #pragma unroll
     for (int t = 0; t < MT; ++t)
 #pragma unroll
