@@ -217,17 +217,15 @@ Layout layout(const dlm_model* m, int n, int n_req) {
   const int qkv_dim = (c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim;
   const int qd = c.n_q_heads * c.head_dim;
   const int es_i = (int)m->es;
-  L.g_qkv = projection_plan(es_i, n, qkv_dim, c.d_model, m->num_cu);
-  L.g_o = projection_plan(es_i, n, c.d_model, qd, m->num_cu);
-  L.g_gu = gate_up_plan(es_i, n, c.d_ffn, c.d_model, m->num_cu);
-  L.g_down = projection_plan(es_i, n, c.d_model, c.d_ffn, m->num_cu);
-  L.m_max = std::min(n, n_req * kMaxBlock);
-  L.g_lm = lm_head_plan(es_i, L.m_max, c.vocab, c.d_model, m->num_cu);
-  L.g_logits = L.g_lm;
-  L.s_qkv = L.g_qkv.splits;
-  L.s_o = L.g_o.splits;
-  L.s_down = L.g_down.splits;
-  if (!m->mx.empty()) {
+  if (m->mx.empty()) {
+    L.g_qkv = projection_plan(es_i, n, qkv_dim, c.d_model, m->num_cu);
+    L.g_o = projection_plan(es_i, n, c.d_model, qd, m->num_cu);
+    L.g_gu = gate_up_plan(es_i, n, c.d_ffn, c.d_model, m->num_cu);
+    L.g_down = projection_plan(es_i, n, c.d_model, c.d_ffn, m->num_cu);
+    L.s_qkv = L.g_qkv.splits;
+    L.s_o = L.g_o.splits;
+    L.s_down = L.g_down.splits;
+  } else {
     // (the rotation and the residual norms add K slices as they read them)
     L.q_qkv = mx_plan(es_i, n, qkv_dim, c.d_model, c.d_model, false, true, true, false, m->num_cu);
     L.q_o = mx_plan(es_i, n, c.d_model, qd, qd, false, true, true, false, m->num_cu);
@@ -236,6 +234,9 @@ Layout layout(const dlm_model* m, int n, int n_req) {
     auto slices = [](const MxPlan& p) { return p.gemm ? p.g.splits : p.tile.slices; };
     L.s_qkv = slices(L.q_qkv), L.s_o = slices(L.q_o), L.s_down = slices(L.q_down);
   }
+  L.m_max = std::min(n, n_req * kMaxBlock);
+  L.g_lm = lm_head_plan(es_i, L.m_max, c.vocab, c.d_model, m->num_cu);
+  L.g_logits = L.g_lm;
   L.tiles = lm_head_tiles(L.g_lm, c.vocab);
   const size_t es = m->es;
   size_t off = 0;
