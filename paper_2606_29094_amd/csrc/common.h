@@ -76,21 +76,6 @@ extern thread_local LaunchTiming g_launch_timing;
     }                                                                                          \
   } while (0)
 
-// For a call of several kernels: the first one carries the hook's start event, and the one
-// launched after last() its stop event, so the time between them is the whole call's.
-struct LaunchSpan {
-  LaunchTiming all;
-  explicit LaunchSpan(bool several) {
-    if (several && g_launch_timing.start) {
-      all = g_launch_timing;
-      g_launch_timing.stop = nullptr;
-    }
-  }
-  void last() const {
-    if (all.stop) g_launch_timing = LaunchTiming{nullptr, all.stop};
-  }
-};
-
 // XCDs the dispatcher spreads a launch's blocks over (block i to XCD i mod 8);
 // each has its own L2
 constexpr int kXcds = 8;

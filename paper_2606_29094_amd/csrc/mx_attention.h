@@ -4,8 +4,8 @@
 #include <algorithm>
 #include <cmath>
 
-#include "kernels.h"
 #include "mx_common.h"
+#include "mx_kernels.h"
 
 namespace dlm {
 

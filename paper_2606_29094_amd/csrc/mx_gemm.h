@@ -7,8 +7,8 @@
 #include <type_traits>
 
 #include "../../include/dlm.h"
-#include "kernels.h"
 #include "mx_common.h"
+#include "mx_kernels.h"
 
 namespace dlm {
 

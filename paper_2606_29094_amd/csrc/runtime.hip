@@ -20,6 +20,7 @@
 #include "common.h"
 #include "kernels.h"
 #include "mx_common.h"
+#include "mx_kernels.h"
 
 using namespace dlm;
 
