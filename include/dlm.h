@@ -504,8 +504,9 @@ dlm_status dlm_debug_mx_attention_plan(int32_t dtype, int32_t n_q_heads, int32_t
  * own dispatch (start and end of the kernel; no extra commands on the
  * stream). dlm_profile_read waits for those events, adds their elapsed times
  * per kernel class into out[0 .. *n_out) (at most cap entries, in first-seen
- * order) and clears them. A class that enqueues several kernels has its first
- * one timed. The profiler state is per model and not thread-safe. */
+ * order) and clears them. A class that enqueues several kernels (projections of a
+ * packed model, attention over a 4-bit cache) is timed from its first one's start to its
+ * last one's end. The profiler state is per model and not thread-safe. */
 typedef struct dlm_profile_entry {
   char name[32];          /* kernel class, e.g. "gemm_gate_up_swiglu"                  */
   int32_t calls;          /* launches timed                                             */

@@ -75,7 +75,7 @@ __device__ __forceinline__ u32x4 finite_or_zero(u32x4 c, uint32_t e) {
 
 __device__ __forceinline__ float silu_mul(float g, float u) { return g / (1.f + __expf(-g)) * u; }
 
-// Up to 16 rows. One block: 16 NF columns, W waves that take the 512-wide k ranges
+// Few rows. One block: 16 of them and 16 NF columns, W waves that take the 512-wide k ranges
 // ("walks") of the block's K slice in turn and add their partial sums in LDS, in
 // wave order. In a chunk of 128 k lane l reads the 32 codes of group l / 16 of weight
 // row l % 16 as one 16-byte load; four register swaps between the 16-lane groups turn
@@ -83,7 +83,7 @@ __device__ __forceinline__ float silu_mul(float g, float u) { return g / (1.f + 
 // 64 consecutive bytes of each x row). A walk's codes and scales (one 16-byte load for
 // its 16 groups) are all requested before the first is used. The weights are read once,
 // by the one block row that needs them; x comes from the caches, once for every 16 NF
-// columns. (One row: 4096 x 4096 5.2 us, 24576 x 4096 18.3, 2.9 TB/s.)
+// columns. (One row: 4096 x 4096 4.9 us, 24576 x 4096 17.6, 3.0 TB/s.)
 constexpr int kWalk = 512;
 
 template <int NF, int W, int NP>
@@ -252,8 +252,8 @@ __global__ __launch_bounds__(W * 64) void mx_linear_kernel(MxLinear a) {
 // own columns' codes from memory into registers NS - 1 chunks ahead, and their scales
 // for four chunks (a walk) at a time one walk ahead, and unpacks them there (once for 16 MT
 // rows), so the weights need no LDS. Bound by the chain of a chunk where a CU has one block
-// of few rows, by the matrix cores beyond (37888 x 3584 SwiGLU, 1000 rows 250 us, 1.09
-// PFLOP/s).
+// of few rows, beyond by the matrix cores and by LDS, which each wave reads all rows from
+// (37888 x 3584 SwiGLU, 1000 rows 248 us, 1.09 PFLOP/s).
 // Row r of a stage is 256 bytes, its 16-byte slot s stored at s ^ (r & 15): the 16 rows
 // that a fragment reads at one slot come from distinct banks.
 // Blocks 8 apart in the launch run on one XCD: each XCD takes an eighth of the tiles, the row
@@ -576,16 +576,17 @@ hipError_t launch_linear(MxLinear a, const MxTile& tl, bool join, const LaunchSp
 
 // Way of a product. Times in us on MI355X (256 CUs), weights from HBM; what is modelled
 // is what decides between the ways:
-//  * up to 16 rows (mx_linear_kernel): 3.5 + the weights at 4.5 TB/s (less while blocks
+//  * blocks of 16 rows (mx_linear_kernel): 3.5 + the weights at 4.5 TB/s (less while blocks
 //    leave CUs idle) + x, once for each column tile and K slice, at 9 TB/s out of the
-//    L2s. So one row takes one column fragment a block and no slices (4096 x 4096 5.3,
-//    two fragments 6.6), and 16 rows over a long K take four in slices (4096 x 12288:
-//    four slices 13.6, one fragment, whole 18.4; the three planes of fp32 x 20.7, two
-//    fragments a block 25).
+//    L2s. So one row takes one column fragment a block and no slices (4096 x 4096 4.9,
+//    two fragments 6.3), 32 rows two (9.1; tiles in four slices 11.5), and 10 rows of fp32
+//    x over 4096 x 12288 four in four slices (20.3; two in two slices 24.6, tiles 30).
+//    The model is off by up to a tenth: 16 rows of 4096 x 4096 get two slices (8.8; whole
+//    7.9), one row of 24576 x 4096 four fragments (17.6; two 16.2).
 //  * tiles (mx_tile_kernel): 4 + for each chunk of a slice 0.5, 0.84 or 1.7 (blocks of 32 x
 //    128, 64 x 128 and 128 x 256), or 0.43, 0.55 or 1.7 for each block that a CU runs.
-//    24576 x 4096: 32 rows 19.8 in the first, 128 rows 45, 38 and 63, 256 rows 82, 57
-//    and 55; 37888 x 3584, 256 rows: 296 large blocks on 256 CUs 98, second 77.
+//    24576 x 4096: 32 rows 19.9 in the first, 128 rows 46, 38.5 and 54, 256 rows 84, 58
+//    and 57; 37888 x 3584, 256 rows: 296 large blocks on 256 CUs 101, second 81.
 //  * slices cost 2 + 0.8 a MB of them (mx_join_kernel and the stores), or, left to the
 //    kernel that reads the output anyway, 0.5 + 0.3 a MB.
 MxTile mx_tile(int elem, int rows, int n, int k, int groups, bool swiglu, bool join, int num_cu) {
@@ -636,9 +637,9 @@ MxTile mx_tile(int elem, int rows, int n, int k, int groups, bool swiglu, bool j
 // 297, 365 / 307; 4608 x 3584 87 / 79, 107 / 95, 160 / 121. Other k: 4096 x 4088 71 / 114,
 // 133 / 174, 139 / 195; 24576 x 3608 SwiGLU 366 / 518, 540 / 771, 741 / 1029. Smaller
 // matrices: 2048 x 2048 25 / 30, 34 / 48, 39 / 52; 1088 x 1024 15 / 19, 16 / 19, 21 / 26.
-// (At 1024 rows 24576 x 4096 182 / 217, 12288 x 4096 110 / 105. fp32 stays with the codes: three bf16 products take
-// half of an fp32 one, 24576 x 4096 at 1024 rows 503. Narrow matrices stay too: 41 x 2608 at
-// 3636 rows 14 / 55.)
+// (At 1024 rows 24576 x 4096 182 / 217, 12288 x 4096 110 / 105. fp32 stays with the codes:
+// three bf16 products take half of an fp32 one, 24576 x 4096 at 1024 rows 503. Narrow
+// matrices stay too: 41 x 2608 at 3636 rows 14 / 55.)
 constexpr int kMxGemmRows = 2048, kMxGemmCols = 1024;
 constexpr long kMxGemmValues = 1L << 23;
 
