@@ -33,8 +33,9 @@ hipError_t mx_unpack(const MxView& w, int k, T* out, long ldo, hipStream_t st);
 // ([rows, n / 2], rows [0, n / 2) of w the gate).
 // A product's way: straight from the codes with K in `slices` (kMxFew: 16 rows x 16 nf
 // columns a block of `waves` waves; tiles of 32 x 128, 64 x 128 and 128 x 256), or (gemm) over
-// the matrix unpacked to the scratch and the GEMM kernels of its type. scratch: bytes, 256-byte aligned. staged: x is first copied into the
-// scratch's first `stage` bytes (fp32 x, or rows that 16-byte loads cannot read).
+// the matrix unpacked to the scratch and the GEMM kernels of its type. scratch: bytes,
+// 256-byte aligned. staged: x is first copied into the scratch's first `stage` bytes (fp32 x,
+// or rows that 16-byte loads cannot read).
 enum { kMxFew, kMxTile32, kMxTile64, kMxTile128 };
 constexpr int kMxTileK = 1 << 24;   // the tiles take rows (and row strides) of up to that many elements
 struct MxTile { int kind, nf, slices, waves; };
