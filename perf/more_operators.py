@@ -1,0 +1,272 @@
+"""The operators on 8-bit integers: packing rows, the norm that feeds them, and products.
+
+An 8-bit matrix is rows of signed bytes (behind k zeros up to a multiple of 128) and one
+fp32 scale for each row: a value is its code times its row's scale. Rows of a weight matrix
+are output channels, rows of an activation are tokens. A row's scale is its largest
+magnitude / 127 (2^-126 at least), its codes the values times 127 / that magnitude, at the
+nearest integer. Each case is one call (a pack, a norm: the call and the read-back of what
+it stored) at the layer shapes of the repository's models, or of generic ones.
+"""
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+ROW = 128                              # codes of a row are padded to a multiple of this
+EPS = 1e-5
+DTYPE = {"bf16": torch.bfloat16, "f32": torch.float32}
+SIZE = {"bf16": 2, "f32": 4}
+MAX_PRODUCT = 4096 * 37888 * 3584      # rows x outputs x inputs of the largest product
+MAX_VALUES = 37888 * 3584              # of the largest pack
+MAX_NORM = 10240 * 4096 * 12           # rows x width x bytes read of the largest norm
+
+
+def _linear(name, rows, n, k, epilogue="store", dtype="bf16"):
+    return {"name": name, "kind": "linear", "rows": rows, "n": n, "k": k, "epilogue": epilogue,
+            "dtype": dtype}
+
+
+def _pack(name, rows, k, dtype="bf16", pad=0):
+    return {"name": name, "kind": "pack", "rows": rows, "k": k, "dtype": dtype, "pad": pad}
+
+
+def _norm(name, rows, k, slices=1, dtype="f32", out="bf16", pad=0):
+    return {"name": name, "kind": "norm", "rows": rows, "k": k, "slices": slices, "dtype": dtype,
+            "out": out, "pad": pad}
+
+
+def listed():
+    return [
+        # output projection of a single row: the smallest call, latency
+        _linear("linear-o-1", 1, 4096, 4096, dtype="f32"),
+        # gate/up of one request's block of 32: weights streamed once
+        _linear("linear-gate-up-32", 32, 24576, 4096, "swiglu"),
+        # down projection of one request's block of 64 into the residual stream
+        _linear("linear-down-64", 64, 3584, 18944, "add", "f32"),
+        # sizes that fit no tile
+        _linear("linear-odd", 137, 689, 1031, dtype="f32"),
+        # down projection of a recompute step into the residual stream
+        _linear("linear-down-1000", 1000, 3584, 18944, "add", "f32"),
+        # gate/up of the default benchmark's batch of 64: bound by the matrix cores
+        _linear("linear-gate-up-4096", 4096, 37888, 3584, "swiglu"),
+        # residual and norm of a single row, from a branch in bf16
+        _norm("norm-1", 1, 4096, dtype="bf16"),
+        # of a no-cache step of 512 rows whose product comes in two K slices
+        _norm("norm-512", 512, 4096, 2),
+        # of a batch of 8 recomputed whole
+        _norm("norm-10240", 10240, 4096),
+        # the attention's output of one request's block of 32
+        _pack("pack-32", 32, 4096),
+        # the gated activations of the default benchmark's batch
+        _pack("pack-act-4096", 4096, 18944),
+        # a gate/up matrix held in fp32, packed while a model is loaded
+        _pack("pack-gate-up-fp32", 37888, 3584, "f32"),
+    ]
+
+
+def draw(rng):
+    log = lambda lo, hi: int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+    kind = rng.choice(["linear", "linear", "linear", "norm", "norm", "pack"])
+    if kind == "linear":
+        n, k = rng.choice([(4096, 4096), (12288, 4096), (24576, 4096), (4096, 12288), (4608, 3584),
+                           (3584, 18944), (37888, 3584), (1376, 256), (256, 688),
+                           (log(1, 20000), log(1, 20000)), (log(1, 20000), 16 * log(1, 1250)),
+                           (log(1, 600), log(1000, 100000))])
+        epilogue = rng.choice(["store", "store", "add", "swiglu"])
+        dtype = "f32" if epilogue == "add" else rng.choice(["bf16", "f32"])
+        c = _linear("", log(1, 4096), n, k, epilogue, dtype)
+        c["n"] += c["n"] % 2 if epilogue == "swiglu" else 0
+        # (an odd shape of the plain form is a slower library product than a round one)
+        while c["rows"] * c["n"] * c["k"] > MAX_PRODUCT // (1 if k % 64 == 0 else 4):
+            c["rows"] = (c["rows"] + 1) // 2
+    elif kind == "norm":
+        c = _norm("", log(1, 10240), rng.choice([4096, 3584, 4096, 3584, 256, log(1, 20000), 4 * log(1, 5000)]),
+                  rng.choice([0, 1, 1, 2, 4]), rng.choice(["f32", "f32", "bf16"]),
+                  rng.choice(["bf16", "bf16", "f32"]), rng.choice([0, 0, 0, 4, 3]))
+        while c["rows"] * c["k"] * (8 + c["slices"] * SIZE[c["dtype"]]) > MAX_NORM:
+            c["rows"] = (c["rows"] + 1) // 2
+    else:
+        c = _pack("", log(1, 40000), rng.choice([4096, 3584, 18944, 12288, 256, log(1, 40000), 8 * log(1, 4000)]),
+                  rng.choice(["bf16", "bf16", "f32"]), rng.choice([0, 0, 0, 8, 3]))
+        while c["rows"] * c["k"] * SIZE[c["dtype"]] > MAX_VALUES * 4:
+            c["rows"] = (c["rows"] + 1) // 2
+    del c["name"]
+    return c
+
+
+# ------------------------------------------------------------------ shapes
+def _padded(k):
+    return -(-k // ROW) * ROW
+
+
+def work(case):
+    m, k = case["rows"], case["k"]
+    packed = lambda rows: rows * (k + 4)
+    if case["kind"] == "linear":
+        n, es = case["n"], SIZE[case["dtype"]]
+        out = {"store": n * es, "add": 8 * n, "swiglu": n // 2 * es}[case["epilogue"]]
+        return {"bytes": packed(n) + packed(m) + m * out, "flops": 2 * m * n * k}
+    if case["kind"] == "pack":                 # read; pack; the values read back
+        return {"bytes": 2 * m * k * SIZE[case["dtype"]] + 2 * packed(m), "flops": 4 * m * k}
+    # residual read and written, slices read, gains; codes written; the values read back
+    return {"bytes": m * k * (8 + case["slices"] * SIZE[case["dtype"]] + SIZE[case["out"]]) + 4 * k +
+            2 * packed(m), "flops": m * k * (7 + case["slices"])}
+
+
+# ------------------------------------------------------------- plain form
+def _encode(x):
+    """codes (int8) and scales (fp32) of the rows of x, decided in 64 bits (values next to the
+    border of two codes)."""
+    x = x.double()
+    amax = x.abs().amax(-1)
+    scale = (amax / 127).clamp_min(2.0 ** -126)
+    code = torch.round(x * (127 / amax).clamp_max(2.0 ** 126)[:, None])
+    bad = ~torch.isfinite(amax)
+    code = torch.where(bad[:, None], torch.zeros_like(code), code)
+    return code.to(torch.int8), torch.where(bad, torch.full_like(scale, math.nan), scale).float()
+
+
+def _values(codes, scales):
+    return codes.float() * scales[:, None]
+
+
+# ------------------------------------------------------------------ inputs
+def _normal(gen, *shape, std=1.0):
+    return torch.randn(*shape, generator=gen, device="cuda").mul_(std)
+
+
+def _tokens(gen, rows, k):
+    """Normed activations: a few channels are much larger than the others."""
+    x = _normal(gen, rows, k)
+    wide = torch.rand(k, generator=gen, device="cuda") < 0.003
+    return x.mul_(torch.where(wide, 12.0, 1.0))
+
+
+def _packed(codes, scales):
+    """The same in the layout that a program keeps: rows padded with zeros."""
+    n, k = codes.shape
+    full = torch.zeros(n, _padded(k), dtype=torch.int8, device="cuda")
+    full[:, :k] = codes
+    return full, scales.contiguous()
+
+
+def _empty(rows, k):
+    from paper_2606_29094_amd import dlm
+    codes = torch.empty(rows, _padded(k), dtype=torch.int8, device="cuda")
+    scales = torch.empty(rows, dtype=torch.float32, device="cuda")
+    return dlm.make_q8(codes, scales, rows, k)
+
+
+def prepare(case, seed):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    s = {"case": case}
+    m, k = case["rows"], case["k"]
+    if case["kind"] == "linear":
+        n, dt = case["n"], DTYPE[case["dtype"]]
+        s["wc"], s["ws"] = _packed(*_encode(_normal(gen, n, k, std=0.02)))
+        x = _tokens(gen, m, k)
+        if case["epilogue"] == "add":          # a gated activation
+            x = x.mul_(_normal(gen, m, k))
+        s["xc"], s["xs"] = _packed(*_encode(x))
+        if case["epilogue"] == "add":
+            s["h"] = _normal(gen, m, n)
+        if own:
+            from paper_2606_29094_amd import dlm
+            s["x"] = dlm.make_q8(s["xc"], s["xs"], m, k)
+            s["w"] = dlm.make_q8(s["wc"], s["ws"], n, k)
+            s["y"] = torch.empty(m, n // 2 if case["epilogue"] == "swiglu" else n, dtype=dt, device="cuda")
+            s["epilogue"] = dlm.Q8_EPILOGUES[case["epilogue"]]
+            s["space"] = torch.empty(max(1, dlm.q8_linear_workspace(m, s["w"], s["epilogue"])),
+                                     dtype=torch.uint8, device="cuda")
+        return s
+    if case["kind"] == "pack":
+        dt, x = DTYPE[case["dtype"]], _tokens(gen, m, k + case["pad"])
+        s["x"] = x.to(dt)[:, :k]
+        if own:
+            s["q"] = _empty(m, k)
+            s["out"] = torch.empty(m, k, dtype=dt, device="cuda")
+        return s
+    s["h"] = _tokens(gen, m, k + case["pad"])[:, :k]
+    s["gain"] = 1 + _normal(gen, k, std=0.1)
+    s["add"] = _normal(gen, case["slices"], m, k, std=0.5).to(DTYPE[case["dtype"]]) if case["slices"] else None
+    if own:
+        s["q"] = _empty(m, k)
+        s["sum"] = torch.empty(m, k, dtype=torch.float32, device="cuda")
+        s["out"] = torch.empty(m, k, dtype=DTYPE[case["out"]], device="cuda")
+    return s
+
+
+# -------------------------------------------------------------------- runs
+def run(s):
+    case = s["case"]
+    return {"linear": _run_linear, "pack": _run_pack, "norm": _run_norm}[case["kind"]](s, case)
+
+
+def _run_linear(s, case):
+    if own:
+        from paper_2606_29094_amd import dlm
+        dlm.q8_linear(s["x"], s["w"], s["y"], s["epilogue"], s["space"], residual=s.get("h"))
+        return s["y"]
+    y = _values(s["xc"], s["xs"]) @ _values(s["wc"], s["ws"]).T
+    if case["epilogue"] == "add":
+        return s["h"] + y
+    if case["epilogue"] == "swiglu":
+        gate, up = y.chunk(2, -1)
+        y = gate / (1 + torch.exp(-gate)) * up
+    return y.to(DTYPE[case["dtype"]])
+
+
+def _run_pack(s, case):
+    if own:
+        from paper_2606_29094_amd import dlm
+        dlm.q8_pack(s["x"], s["q"])
+        dlm.q8_unpack(s["q"], s["out"])
+        return s["out"]
+    return _values(*_encode(s["x"])).to(s["x"].dtype)
+
+
+def _run_norm(s, case):
+    if own:
+        from paper_2606_29094_amd import dlm
+        dlm.q8_norm(s["h"], s["gain"], EPS, s["q"], add=s["add"], h_out=s["sum"])
+        dlm.q8_unpack(s["q"], s["out"])
+        return {"h": s["sum"], "x": s["out"]}
+    h = s["h"]
+    for a in s["add"] if s["add"] is not None else ():       # slices in order
+        h = h + a.float()
+    mean = h.double().square().mean(-1, keepdim=True) + float(np.float32(EPS))
+    x = h.double() / mean.sqrt() * s["gain"].double()
+    return {"h": h.contiguous(), "x": _values(*_encode(x)).to(DTYPE[case["out"]])}
+
+
+# ------------------------------------------------------------------- exact
+def _exact_round(x):
+    """The rows of x (64 bits) at the nearest of 255 evenly spaced values."""
+    step = x.abs().amax(-1, keepdim=True) / 127
+    return torch.where(step > 0, torch.round(x / step.clamp_min(1e-300)) * step, torch.zeros_like(x))
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    if case["kind"] == "pack":
+        return _exact_round(s["x"].double())
+    if case["kind"] == "norm":
+        h = s["h"].double()
+        if s["add"] is not None:
+            h = h + s["add"].double().sum(0)
+        x = h / torch.sqrt((h * h).mean(-1, keepdim=True) + EPS) * s["gain"].double()
+        return {"h": h, "x": _exact_round(x)}
+    # 1024 products of two codes sum to less than 2^24: whole numbers in 32 bits
+    m, n = case["rows"], case["n"]
+    y = torch.zeros(m, n, dtype=torch.float64, device="cuda")
+    for at in range(0, s["xc"].shape[1], 1024):
+        y += s["xc"][:, at:at + 1024].float() @ s["wc"][:, at:at + 1024].float().T
+    y *= s["xs"].double()[:, None]
+    y *= s["ws"].double()[None]
+    if case["epilogue"] == "add":
+        return s["h"].double() + y
+    if case["epilogue"] == "swiglu":
+        return torch.nn.functional.silu(y[:, :n // 2]) * y[:, n // 2:]
+    return y
