@@ -156,7 +156,7 @@ def _empty(rows, k):
     from paper_2606_29094_amd import dlm
     codes = torch.empty(rows, _padded(k), dtype=torch.int8, device="cuda")
     scales = torch.empty(rows, dtype=torch.float32, device="cuda")
-    return dlm.make_q8(codes, scales, rows, k)
+    return dlm.make_qint(codes, scales, rows, k)
 
 
 def prepare(case, seed):
@@ -174,11 +174,11 @@ def prepare(case, seed):
             s["h"] = _normal(gen, m, n)
         if own:
             from paper_2606_29094_amd import dlm
-            s["x"] = dlm.make_q8(s["xc"], s["xs"], m, k)
-            s["w"] = dlm.make_q8(s["wc"], s["ws"], n, k)
+            s["x"] = dlm.make_qint(s["xc"], s["xs"], m, k)
+            s["w"] = dlm.make_qint(s["wc"], s["ws"], n, k)
             s["y"] = torch.empty(m, n // 2 if case["epilogue"] == "swiglu" else n, dtype=dt, device="cuda")
-            s["epilogue"] = dlm.Q8_EPILOGUES[case["epilogue"]]
-            s["space"] = torch.empty(max(1, dlm.q8_linear_workspace(m, s["w"], s["epilogue"])),
+            s["epilogue"] = dlm.QINT_EPILOGUES[case["epilogue"]]
+            s["space"] = torch.empty(max(1, dlm.qint_linear_workspace(m, s["w"], s["epilogue"])),
                                      dtype=torch.uint8, device="cuda")
         return s
     if case["kind"] == "pack":
@@ -207,7 +207,7 @@ def run(s):
 def _run_linear(s, case):
     if own:
         from paper_2606_29094_amd import dlm
-        dlm.q8_linear(s["x"], s["w"], s["y"], s["epilogue"], s["space"], residual=s.get("h"))
+        dlm.qint_linear(s["x"], s["w"], s["y"], s["epilogue"], s["space"], residual=s.get("h"))
         return s["y"]
     y = _values(s["xc"], s["xs"]) @ _values(s["wc"], s["ws"]).T
     if case["epilogue"] == "add":
@@ -221,8 +221,8 @@ def _run_linear(s, case):
 def _run_pack(s, case):
     if own:
         from paper_2606_29094_amd import dlm
-        dlm.q8_pack(s["x"], s["q"])
-        dlm.q8_unpack(s["q"], s["out"])
+        dlm.qint_pack(s["x"], s["q"])
+        dlm.qint_unpack(s["q"], s["out"])
         return s["out"]
     return _values(*_encode(s["x"])).to(s["x"].dtype)
 
@@ -230,8 +230,8 @@ def _run_pack(s, case):
 def _run_norm(s, case):
     if own:
         from paper_2606_29094_amd import dlm
-        dlm.q8_norm(s["h"], s["gain"], EPS, s["q"], add=s["add"], h_out=s["sum"])
-        dlm.q8_unpack(s["q"], s["out"])
+        dlm.qint_norm(s["h"], s["gain"], EPS, s["q"], add=s["add"], h_out=s["sum"])
+        dlm.qint_unpack(s["q"], s["out"])
         return {"h": s["sum"], "x": s["out"]}
     h = s["h"]
     for a in s["add"] if s["add"] is not None else ():       # slices in order
