@@ -429,6 +429,67 @@ dlm_status dlm_mx_kv_attention(const dlm_cache* c, int32_t layer, int32_t n_req,
                                const dlm_kv_rows* rows, const void* q, void* out, void* workspace,
                                size_t ws_bytes, void* stream);
 
+/* ---- 8-bit integers: activations and weights in 8 bits ----
+ *
+ * Format. A matrix [n, k] holds a signed byte (its code) for every value and one fp32
+ * scale for every row (a token of an activation, an output channel of a weight matrix): the value
+ * is code * scale. Packing takes A = the row's largest magnitude, the scale max(A / 127, 2^-126)
+ * rounded to fp32, and for each x the integer nearest to x min(127 / A, 2^126) (ties to the even
+ * one; decided in 64 bits, so either neighbour where x lies within 2^-40 of a step of the middle).
+ * A row that holds an infinity or a NaN gets the scale NaN and zero codes.
+ * Products of two such matrices are sums of whole numbers in 32 bits, exact and independent of
+ * their order: k is DLM_QINT_MAX_K at most (DLM_EUNSUPPORTED beyond, in every call). */
+enum { DLM_QINT_ROW = 128, DLM_QINT_MAX_K = 131071 };
+
+/* An 8-bit matrix [n, k] in device memory: codes [n, K] with K = k rounded up to a multiple of
+ * DLM_QINT_ROW, 16-byte aligned, the codes behind k zero (the library writes them so; a caller that
+ * fills codes itself does too); scales [n]. n may be 0 where the matrix is an activation. */
+typedef struct dlm_qint {
+  int8_t* codes;
+  float* scales;
+  int32_t n, k;
+} dlm_qint;
+
+/* Bytes of the two buffers of an [n, k] matrix. */
+dlm_status dlm_qint_bytes(int32_t n, int32_t k, size_t* codes_bytes, size_t* scales_bytes);
+
+/* Pack the rows of x [n, k] (dtype: dlm_dtype; rows ldx elements apart, any alignment) into out's
+ * buffers. n and k are out's. */
+dlm_status dlm_qint_pack(int32_t dtype, const void* x, int64_t ldx, const dlm_qint* out, void* stream);
+
+/* The values of an 8-bit matrix: out [n, k] in dtype, rows ldo elements apart. */
+dlm_status dlm_qint_unpack(const dlm_qint* x, int32_t dtype, void* out, int64_t ldo, void* stream);
+
+/* Residual update and RMS norm, packed:
+ *   h'  = h + add[0] + .. + add[splits - 1]       fp32, slices in order
+ *   out = pack(h' / sqrt(mean(h'^2) + eps) * gain)
+ * h [n, k] fp32 (rows ldh elements apart), add [splits, n, k] in dtype (slices add_stride, rows
+ * ldadd elements apart; splits may be 0, add is then not used), gain [k] fp32. h' is stored to h_out [n, k]
+ * (rows ldo apart; h itself with ldo = ldh, or NULL to store nothing; otherwise no overlap with h
+ * or add). The statistic and the codes are computed in 64 bits. eps is positive and finite. n and k are
+ * out's; any alignment. */
+dlm_status dlm_qint_norm(const float* h, int64_t ldh, float* h_out, int64_t ldo, int32_t dtype,
+                       const void* add, int32_t splits, int64_t add_stride, int64_t ldadd,
+                       const float* gain, float eps, const dlm_qint* out, void* stream);
+
+/* Product of two 8-bit matrices, p[m][n] = (sum_k x[m][k] w[n][k]) sx[m] sw[n]: the exact sum of
+ * the codes' products, its conversion to fp32 and both scalings rounded to fp32 each. x's k is w's.
+ * Epilogues (dtype is the output's):
+ *   DLM_QINT_STORE   y [x.n, w.n] = p
+ *   DLM_QINT_ADD     y [x.n, w.n] fp32 = residual + p (dtype DLM_F32; residual [x.n, w.n] fp32, rows
+ *                  ldr elements apart, may be y itself with ldr = ldy)
+ *   DLM_QINT_SWIGLU  y [x.n, w.n / 2] = silu(p[:, f]) * p[:, w.n / 2 + f] (rows [0, n / 2) of w are
+ *                  the gate weights; n even)
+ * y's rows are ldy elements apart; y must not overlap x or w. residual is not used by the others.
+ * w holds 2^33 bytes of codes at most. Workspace: as in dlm_mx_linear, for the same m_rows (x.n),
+ * w and epilogue. A row's result depends on that row alone, bit for bit. */
+typedef enum { DLM_QINT_STORE = 0, DLM_QINT_ADD = 1, DLM_QINT_SWIGLU = 2 } dlm_qint_epilogue;
+dlm_status dlm_qint_linear_workspace(int32_t m_rows, const dlm_qint* w, int32_t epilogue,
+                                   size_t* out_bytes);
+dlm_status dlm_qint_linear(const dlm_qint* x, const dlm_qint* w, int32_t epilogue, const float* residual,
+                         int64_t ldr, int32_t dtype, void* y, int64_t ldy, void* workspace,
+                         size_t ws_bytes, void* stream);
+
 /* Test hooks for the bf16 GEMM kernel (the contraction of every projection of
  * the step: QKV, output, gate/up and down). dlm_debug_gemm_info: the output
  * tile (bm x bn) of tile configuration cfg and, in *subs, the sub-tile splits

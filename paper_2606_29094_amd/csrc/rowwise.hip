@@ -744,3 +744,7 @@ INST(float)
 
 // 4-bit matrices and caches
 #include "mx_rowwise.h"
+
+// 8-bit integers
+#include "qint_rowwise.h"
+#include "qint_gemm.h"

@@ -21,6 +21,7 @@
 #include "kernels.h"
 #include "mx_common.h"
 #include "mx_kernels.h"
+#include "qint_kernels.h"
 
 using namespace dlm;
 
@@ -641,6 +642,35 @@ dlm_status make_kv_plan(const dlm_cache* c, int32_t layer, int32_t n_req, const 
       return fail(DLM_ESIZE, "more than %d rows", DLM_MAX_REQ * DLM_MAX_SEQ);
   }
   p->n_rows = (int)total;
+  return DLM_OK;
+}
+
+// ---- 8-bit integers ----
+// A matrix of the given width (k < 0: any), with buffers the kernels can read. rows0: no rows will do.
+dlm_status check_qint(const dlm_qint* q, int k, bool rows0, const char* what) {
+  if (!q) return fail(DLM_EINVAL, "%s: 8-bit matrix pointer is NULL", what);
+  if (q->n < (rows0 ? 0 : 1) || q->k < 1) return fail(DLM_EINVAL, "%s: 8-bit matrix of %d x %d", what, q->n, q->k);
+  if (k >= 0 && q->k != k) return fail(DLM_EINVAL, "%s: 8-bit matrix is %d wide, expected %d", what, q->k, k);
+  if (q->k > DLM_QINT_MAX_K)
+    return fail(DLM_EUNSUPPORTED, "%s: 8-bit matrix is %d wide; %d at most", what, q->k, (int)DLM_QINT_MAX_K);
+  if (q->n == 0) return DLM_OK;
+  if (!q->codes || !q->scales) return fail(DLM_EINVAL, "%s: 8-bit matrix pointer is NULL", what);
+  if (!aligned16(q->codes) || reinterpret_cast<uintptr_t>(q->scales) % 4 != 0)
+    return fail(DLM_EINVAL, "%s: codes are not 16-byte aligned, or scales not 4-byte aligned", what);
+  return DLM_OK;
+}
+QintView qint_view(const dlm_qint& q) { return {q.codes, q.scales, q.n, q.k}; }
+
+dlm_status check_qint_linear(int32_t m_rows, const dlm_qint* w, int32_t epilogue) {
+  dlm_status s = check_qint(w, -1, false, "w");
+  if (s != DLM_OK) return s;
+  if ((size_t)w->n * qint_row(w->k) > (size_t)1 << 33)
+    return fail(DLM_EUNSUPPORTED, "w: 8-bit matrix of %d x %d: more than 2^33 bytes", w->n, w->k);
+  if (m_rows < 0 || m_rows > DLM_MAX_REQ * DLM_MAX_SEQ)
+    return fail(DLM_EINVAL, "%d rows outside [0, %d]", m_rows, DLM_MAX_REQ * DLM_MAX_SEQ);
+  if (epilogue < DLM_QINT_STORE || epilogue > DLM_QINT_SWIGLU) return fail(DLM_EINVAL, "epilogue %d", epilogue);
+  if (epilogue == DLM_QINT_SWIGLU && w->n % 2 != 0)
+    return fail(DLM_EINVAL, "odd number of rows %d for the SwiGLU epilogue", w->n);
   return DLM_OK;
 }
 
@@ -1333,6 +1363,115 @@ dlm_status dlm_mx_kv_attention(const dlm_cache* c, int32_t layer, int32_t n_req,
     HIPCHECK(mx_attention<float>(p, reinterpret_cast<const float*>(q), c->mx_layer(layer), cf.n_q_heads,
                                  cf.n_kv_heads, cf.head_dim, reinterpret_cast<float*>(out), plan, scratch,
                                  st));
+  return DLM_OK;
+}
+
+// ---- operators on 8-bit integers ----
+
+dlm_status dlm_qint_bytes(int32_t n, int32_t k, size_t* codes_bytes, size_t* scales_bytes) {
+  g_err.clear();
+  if (n < 0 || k < 1) return fail(DLM_EINVAL, "8-bit matrix of %d x %d", n, k);
+  if (k > DLM_QINT_MAX_K) return fail(DLM_EUNSUPPORTED, "8-bit matrix is %d wide; %d at most", k, (int)DLM_QINT_MAX_K);
+  if (codes_bytes) *codes_bytes = (size_t)n * qint_row(k);
+  if (scales_bytes) *scales_bytes = (size_t)n * sizeof(float);
+  return DLM_OK;
+}
+
+dlm_status dlm_qint_pack(int32_t dtype, const void* x, int64_t ldx, const dlm_qint* out, void* stream) {
+  g_err.clear();
+  dlm_status s = check_dtype(dtype);
+  if (s != DLM_OK || (s = check_qint(out, -1, true, "out")) != DLM_OK) return s;
+  if (out->n == 0) return DLM_OK;
+  if (!x) return fail(DLM_EINVAL, "x is NULL");
+  if (ldx < out->k) return fail(DLM_EINVAL, "row stride %lld < %d", (long long)ldx, out->k);
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  if (dtype == DLM_BF16)
+    HIPCHECK(qint_pack<bf16>(reinterpret_cast<const bf16*>(x), ldx, qint_view(*out), st));
+  else
+    HIPCHECK(qint_pack<float>(reinterpret_cast<const float*>(x), ldx, qint_view(*out), st));
+  return DLM_OK;
+}
+
+dlm_status dlm_qint_unpack(const dlm_qint* x, int32_t dtype, void* out, int64_t ldo, void* stream) {
+  g_err.clear();
+  dlm_status s = check_dtype(dtype);
+  if (s != DLM_OK || (s = check_qint(x, -1, true, "x")) != DLM_OK) return s;
+  if (x->n == 0) return DLM_OK;
+  if (!out) return fail(DLM_EINVAL, "out is NULL");
+  if (ldo < x->k) return fail(DLM_EINVAL, "row stride %lld < %d", (long long)ldo, x->k);
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  if (dtype == DLM_BF16)
+    HIPCHECK(qint_unpack<bf16>(qint_view(*x), reinterpret_cast<bf16*>(out), ldo, st));
+  else
+    HIPCHECK(qint_unpack<float>(qint_view(*x), reinterpret_cast<float*>(out), ldo, st));
+  return DLM_OK;
+}
+
+dlm_status dlm_qint_norm(const float* h, int64_t ldh, float* h_out, int64_t ldo, int32_t dtype,
+                       const void* add, int32_t splits, int64_t add_stride, int64_t ldadd,
+                       const float* gain, float eps, const dlm_qint* out, void* stream) {
+  g_err.clear();
+  dlm_status s = check_dtype(dtype);
+  if (s != DLM_OK || (s = check_qint(out, -1, true, "out")) != DLM_OK) return s;
+  if (splits < 0) return fail(DLM_EINVAL, "splits %d < 0", splits);
+  if (!(eps > 0.f) || !std::isfinite(eps)) return fail(DLM_EINVAL, "eps %g is not positive and finite", eps);
+  if (out->n == 0) return DLM_OK;
+  if (!h || !gain || (splits > 0 && !add)) return fail(DLM_EINVAL, "NULL buffer");
+  if (ldh < out->k || (h_out && ldo < out->k) || (splits > 0 && ldadd < out->k))
+    return fail(DLM_EINVAL, "row strides %lld, %lld, %lld: %d at least", (long long)ldh, (long long)ldo,
+                (long long)ldadd, out->k);
+  if (splits > 1 && add_stride < 0) return fail(DLM_EINVAL, "slice stride %lld < 0", (long long)add_stride);
+  if (h_out == h && ldo != ldh)
+    return fail(DLM_EINVAL, "h in place with row strides %lld and %lld", (long long)ldh, (long long)ldo);
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  if (dtype == DLM_BF16) {
+    const QintNorm<bf16> a{h, ldh, h_out, ldo, reinterpret_cast<const bf16*>(add), splits, add_stride, ldadd, gain, eps};
+    HIPCHECK(qint_norm<bf16>(a, qint_view(*out), st));
+  } else {
+    const QintNorm<float> a{h, ldh, h_out, ldo, reinterpret_cast<const float*>(add), splits, add_stride, ldadd, gain, eps};
+    HIPCHECK(qint_norm<float>(a, qint_view(*out), st));
+  }
+  return DLM_OK;
+}
+
+dlm_status dlm_qint_linear_workspace(int32_t m_rows, const dlm_qint* w, int32_t epilogue,
+                                   size_t* out_bytes) {
+  g_err.clear();
+  dlm_status s = check_qint_linear(m_rows, w, epilogue);
+  if (s != DLM_OK) return s;
+  if (!out_bytes) return fail(DLM_EINVAL, "out_bytes is NULL");
+  *out_bytes = qint_plan(m_rows, w->n, w->k, epilogue == DLM_QINT_SWIGLU, device_cus()).scratch;
+  return DLM_OK;
+}
+
+dlm_status dlm_qint_linear(const dlm_qint* x, const dlm_qint* w, int32_t epilogue, const float* residual,
+                         int64_t ldr, int32_t dtype, void* y, int64_t ldy, void* workspace,
+                         size_t ws_bytes, void* stream) {
+  g_err.clear();
+  dlm_status s = check_dtype(dtype);
+  if (s != DLM_OK || (s = check_qint(x, -1, true, "x")) != DLM_OK ||
+      (s = check_qint_linear(x->n, w, epilogue)) != DLM_OK)
+    return s;
+  if (x->k != w->k) return fail(DLM_EINVAL, "x is %d wide, w %d", x->k, w->k);
+  if (epilogue == DLM_QINT_ADD && dtype != DLM_F32) return fail(DLM_EINVAL, "sums with a residual are fp32");
+  if (x->n == 0) return DLM_OK;
+  if (!y || (epilogue == DLM_QINT_ADD && !residual)) return fail(DLM_EINVAL, "NULL buffer");
+  const int n_out = epilogue == DLM_QINT_SWIGLU ? w->n / 2 : w->n;
+  if (ldy < n_out || (epilogue == DLM_QINT_ADD && ldr < n_out))
+    return fail(DLM_EINVAL, "row strides %lld, %lld too small for %d outputs", (long long)ldy, (long long)ldr, n_out);
+  if (epilogue == DLM_QINT_ADD && residual == y && ldr != ldy)
+    return fail(DLM_EINVAL, "residual in place with row strides %lld and %lld", (long long)ldr, (long long)ldy);
+  const QintPlan plan = qint_plan(x->n, w->n, w->k, epilogue == DLM_QINT_SWIGLU, device_cus());
+  if (plan.scratch) {
+    if (!workspace) return fail(DLM_EINVAL, "workspace is NULL");
+    if (reinterpret_cast<uintptr_t>(workspace) % 256 != 0)
+      return fail(DLM_EINVAL, "workspace is not 256-byte aligned");
+    if (ws_bytes < plan.scratch)
+      return fail(DLM_ESIZE, "workspace of %zu bytes; needs %zu", ws_bytes, plan.scratch);
+  }
+  QintOut o{};
+  o.y = y, o.ldy = ldy, o.res = residual, o.ldr = ldr, o.mode = epilogue, o.wide = dtype == DLM_F32;
+  HIPCHECK(qint_matmul(plan, qint_view(*x), qint_view(*w), o, workspace, reinterpret_cast<hipStream_t>(stream)));
   return DLM_OK;
 }
 

@@ -24,6 +24,9 @@ DLM_REQ_REFRESH = 1
 DLM_MX_GROUP = 32
 DLM_MX_STORE, DLM_MX_ADD, DLM_MX_SWIGLU = 0, 1, 2
 MX_EPILOGUES = {"store": DLM_MX_STORE, "add": DLM_MX_ADD, "swiglu": DLM_MX_SWIGLU}
+DLM_QINT_ROW, DLM_QINT_MAX_K = 128, 131071
+DLM_QINT_STORE, DLM_QINT_ADD, DLM_QINT_SWIGLU = 0, 1, 2
+QINT_EPILOGUES = {"store": DLM_QINT_STORE, "add": DLM_QINT_ADD, "swiglu": DLM_QINT_SWIGLU}
 MODES = {"none": DLM_CACHE_NONE, "prefix": DLM_CACHE_PREFIX, "dual": DLM_CACHE_DUAL}
 
 EXPORTS = ["dlm_load_weights", "dlm_model_destroy", "dlm_workspace_bytes",
@@ -36,7 +39,9 @@ EXPORTS = ["dlm_load_weights", "dlm_model_destroy", "dlm_workspace_bytes",
            "dlm_mx_bytes", "dlm_mx_pack", "dlm_mx_unpack", "dlm_mx_linear_workspace",
            "dlm_mx_linear", "dlm_load_weights_mx", "dlm_kv_cache_alloc_mx", "dlm_mx_kv_append",
            "dlm_mx_kv_read", "dlm_mx_kv_attention_workspace", "dlm_mx_kv_attention",
-           "dlm_debug_mx_linear_plan", "dlm_debug_mx_attention_plan"]
+           "dlm_debug_mx_linear_plan", "dlm_debug_mx_attention_plan",
+           "dlm_qint_bytes", "dlm_qint_pack", "dlm_qint_unpack", "dlm_qint_norm",
+           "dlm_qint_linear_workspace", "dlm_qint_linear"]
 
 
 class DlmConfig(ctypes.Structure):
@@ -69,6 +74,11 @@ class DlmLayerMx(ctypes.Structure):
 class DlmWeightsMx(ctypes.Structure):
     _fields_ = [("embed", c_void_p), ("lm_head", c_void_p), ("final_norm", c_void_p),
                 ("layers", POINTER(DlmLayerMx))]
+
+
+class DlmQint(ctypes.Structure):
+    _keep = ()              # the tensors of make_qint
+    _fields_ = [("codes", c_void_p), ("scales", c_void_p), ("n", c_int32), ("k", c_int32)]
 
 
 class DlmKvRows(ctypes.Structure):
@@ -186,6 +196,14 @@ def lib():
         L.dlm_debug_mx_attention_plan.argtypes = [c_int32, c_int32, c_int32, c_int32, c_int32,
                                                   POINTER(c_int32), POINTER(c_int32), c_size_t,
                                                   c_int32, POINTER(c_int32), POINTER(c_int32)]
+        L.dlm_qint_bytes.argtypes = [c_int32, c_int32, POINTER(c_size_t), POINTER(c_size_t)]
+        L.dlm_qint_pack.argtypes = [c_int32, c_void_p, c_int64, POINTER(DlmQint), c_void_p]
+        L.dlm_qint_unpack.argtypes = [POINTER(DlmQint), c_int32, c_void_p, c_int64, c_void_p]
+        L.dlm_qint_norm.argtypes = [c_void_p, c_int64, c_void_p, c_int64, c_int32, c_void_p, c_int32,
+                                  c_int64, c_int64, c_void_p, c_float, POINTER(DlmQint), c_void_p]
+        L.dlm_qint_linear_workspace.argtypes = [c_int32, POINTER(DlmQint), c_int32, POINTER(c_size_t)]
+        L.dlm_qint_linear.argtypes = [POINTER(DlmQint), POINTER(DlmQint), c_int32, c_void_p, c_int64,
+                                    c_int32, c_void_p, c_int64, c_void_p, c_size_t, c_void_p]
         L.dlm_last_error.argtypes = []
         L.dlm_last_error.restype = ctypes.c_char_p
         for name in ["dlm_load_weights", "dlm_workspace_bytes", "dlm_kv_cache_alloc",
@@ -198,7 +216,9 @@ def lib():
                      "dlm_mx_unpack", "dlm_mx_linear_workspace", "dlm_mx_linear",
                      "dlm_load_weights_mx", "dlm_kv_cache_alloc_mx", "dlm_mx_kv_append",
                      "dlm_mx_kv_read", "dlm_mx_kv_attention_workspace", "dlm_mx_kv_attention",
-                     "dlm_debug_mx_linear_plan", "dlm_debug_mx_attention_plan"]:
+                     "dlm_debug_mx_linear_plan", "dlm_debug_mx_attention_plan",
+                     "dlm_qint_bytes", "dlm_qint_pack", "dlm_qint_unpack", "dlm_qint_norm",
+                     "dlm_qint_linear_workspace", "dlm_qint_linear"]:
             getattr(L, name).restype = c_int32
         _lib = L
     return _lib
@@ -586,6 +606,95 @@ def debug_mx_attention_plan(dtype, hq: int, hkv: int, dh: int, rows, lens,
                                             scratch_bytes, num_cu, ctypes.byref(kernel),
                                             ctypes.byref(splits)))
     return kernel.value, splits.value
+
+
+# ------------------------------------------------- 8-bit integers
+def qint_bytes(n: int, k: int):
+    """(bytes of the codes, bytes of the scales) of an 8-bit [n, k] matrix."""
+    c, s = c_size_t(), c_size_t()
+    check(lib().dlm_qint_bytes(n, k, ctypes.byref(c), ctypes.byref(s)))
+    return c.value, s.value
+
+
+def make_qint(codes, scales, n: int, k: int) -> DlmQint:
+    """An 8-bit [n, k] matrix over a contiguous int8 device tensor (rows of k rounded up to a
+    multiple of 128 codes, zero behind k) and a contiguous fp32 one (a scale for each row)."""
+    import torch
+    for name, t, dt, need in zip(("codes", "scales"), (codes, scales), (torch.int8, torch.float32),
+                                 qint_bytes(n, k)):
+        if t.dtype != dt or not t.is_contiguous() or not t.is_cuda:
+            raise ValueError(f"{name}: contiguous {dt} device tensor expected")
+        if t.nbytes < need:
+            raise ValueError(f"{name} holds {t.nbytes} bytes; a {n} x {k} matrix needs {need}")
+    if codes.device != scales.device:
+        raise ValueError(f"codes on {codes.device}, scales on {scales.device}")
+    q = DlmQint(codes.data_ptr(), scales.data_ptr(), n, k)
+    q._keep = (codes, scales)
+    return q
+
+
+def qint_pack(x, q: DlmQint, stream=None):
+    """Pack the rows of x [n, k] (bf16 or fp32, contiguous rows) into q's buffers."""
+    ld = _rows_of("x", x, (q.n, q.k))
+    check(lib().dlm_qint_pack(_dtype_id(x.dtype), x.data_ptr(), ld, ctypes.byref(q),
+                            _on(stream, x, *q._keep)))
+
+
+def qint_unpack(q: DlmQint, out, stream=None):
+    """The values of q, in out's dtype."""
+    ld = _rows_of("out", out, (q.n, q.k))
+    check(lib().dlm_qint_unpack(ctypes.byref(q), _dtype_id(out.dtype), out.data_ptr(), ld,
+                              _on(stream, out, *q._keep)))
+
+
+def qint_norm(h, gain, eps: float, q: DlmQint, add=None, h_out=None, stream=None):
+    """h' = h + add (fp32 [n, k]; add [n, k] or slices [splits, n, k], bf16 or fp32), stored to
+    h_out or, where there is an add and no h_out, to h; its RMS norm times gain, packed into q."""
+    import torch
+    shape = (q.n, q.k)
+    ldh = _rows_of("h", h, shape, torch.float32)
+    _flat("gain", gain, (q.k,), torch.float32)
+    splits, stride, ldadd, dt = 0, 0, 0, DLM_F32
+    if add is not None:
+        dt = _dtype_id(add.dtype)
+        slices = add if add.dim() == 3 else add[None]
+        splits = slices.shape[0]
+        if splits:
+            ldadd = _rows_of("add", slices[0], shape)
+            stride = slices.stride(0) if splits > 1 else 0
+        if h_out is None:
+            h_out = h
+    ldo = _rows_of("h_out", h_out, shape, torch.float32) if h_out is not None else 0
+    st = _on(stream, *(t for t in (h, gain, add, h_out) if t is not None), *q._keep)
+    check(lib().dlm_qint_norm(h.data_ptr(), ldh, None if h_out is None else h_out.data_ptr(), ldo, dt,
+                            add.data_ptr() if splits else None, splits, stride, ldadd,
+                            gain.data_ptr(), eps, ctypes.byref(q), st))
+
+
+def qint_linear_workspace(m_rows: int, w: DlmQint, epilogue: int = DLM_QINT_STORE) -> int:
+    out = c_size_t()
+    check(lib().dlm_qint_linear_workspace(m_rows, ctypes.byref(w), epilogue, ctypes.byref(out)))
+    return out.value
+
+
+def qint_linear(x: DlmQint, w: DlmQint, y, epilogue: int = DLM_QINT_STORE, workspace=None, residual=None,
+              stream=None):
+    """y = x @ w.T (in y's dtype), residual + x @ w.T (fp32; residual may be y), or silu(gate) *
+    up in y's dtype; workspace: at least qint_linear_workspace bytes, or None where that is 0."""
+    import torch
+    n_out = w.n // 2 if epilogue == DLM_QINT_SWIGLU else w.n
+    ldy, tensors = _rows_of("y", y, (x.n, n_out)), [y, *x._keep, *w._keep]
+    r, ldr, ws, size = None, 0, None, 0
+    if epilogue == DLM_QINT_ADD:
+        if residual is None:
+            raise ValueError("the add epilogue takes a residual")
+        r, ldr = residual.data_ptr(), _rows_of("residual", residual, (x.n, n_out), torch.float32)
+        tensors.append(residual)
+    if workspace is not None:
+        ws, size = _scratch(workspace)
+        tensors.append(workspace)
+    check(lib().dlm_qint_linear(ctypes.byref(x), ctypes.byref(w), epilogue, r, ldr,
+                              _dtype_id(y.dtype), y.data_ptr(), ldy, ws, size, _on(stream, *tensors)))
 
 
 def profile_enable(model, on: bool, only_class: str | None = None):
