@@ -358,6 +358,10 @@ double few_rows_base_us(int M, int N, int s, bool gate_up) {
                  0.03 * std::max(0.0, mb * s - 32.0));
 }
 
+// A kernel of its own that adds the slices, beyond what their reader is charged above: its launch
+// and, as no other kernel would, the first slice's reads and the result's stores.
+double join_us(int M, int N) { return 1.6 + (double)M * N * 4e-6 / 5.0; }
+
 // A tile of kFewRowTiles with its dimensions.
 struct FewRowDims {
   int cfg, bm, bn, stages, subs, occ;
@@ -404,8 +408,15 @@ int last_round_subs(int subs, long rem, long slots) {
 }  // namespace
 
 GemmPlan gemm_plan(int es, int M, int N, int K, bool splittable, int num_cu, bool allow_mf32,
-                   bool allow_tail, bool allow_odd, int few_rows, bool allow_small) {
+                   bool allow_tail, bool allow_odd, int few_rows, bool allow_small, bool join,
+                   double* us) {
   GemmPlan best{-1, 1, 0};
+  // (a join takes slices of any number of k-tiles, so every power of two will do)
+  const int max_s = join ? 32 : 8;
+  auto slices = [&](int s) {
+    if (!splittable || K / s < 512) return false;
+    return join ? ceil_div(K / 64, ceil_div(K / 64, s)) == s : (K / 64) % s == 0;
+  };
   if (M <= 0 || N <= 0) return best;
   if (es != 2 || K % 64 != 0) {
     const int bm = M <= 32 ? 32 : (M <= 64 ? 64 : 128);
@@ -431,8 +442,9 @@ GemmPlan gemm_plan(int es, int M, int N, int K, bool splittable, int num_cu, boo
   }
   double best_t = 1e30;
   if (M <= few_rows) {
-    double base[9];
-    for (int sp = 1; sp <= 8; sp *= 2) base[sp] = few_rows_base_us(M, N, sp, !splittable);
+    double base[33];
+    for (int sp = 1; sp <= max_s; sp *= 2)
+      base[sp] = few_rows_base_us(M, N, sp, !splittable) + (join && sp > 1 ? join_us(M, N) : 0.0);
     const bool pow2 = (K & (K - 1)) == 0 && K >= 2048;
     const double stream0 = (double)N * K * 2e-6 / 7.11, inv_cu = 1.0 / num_cu;
     const FewRowDims* const tiles = few_row_dims();
@@ -445,8 +457,8 @@ GemmPlan gemm_plan(int es, int M, int N, int K, bool splittable, int num_cu, boo
       const double stream = stream0 * f;
       const double us_kt = c.us_kt * f * (1.0 - 0.27 * (1.0 - (double)M / ((double)n_m * c.bm)));
       const long n_tiles = (long)n_m * ceil_div(N, c.bn);
-      for (int s = 1; s <= 8; s *= 2) {
-        if (s > 1 && (!splittable || c.cfg == 22 || (K / 64) % s != 0 || K / s < 512)) continue;
+      for (int s = 1; s <= max_s; s *= 2) {
+        if (s > 1 && (c.cfg == 22 || !slices(s))) continue;
         const double scale = s > 1 ? 1.01 : 1.0;
         if (base[s] + stream * scale >= best_t) break;   // (more slices only add to the base)
         const long units = n_tiles * s, full = units / num_cu, rem = units - full * num_cu;
@@ -460,7 +472,7 @@ GemmPlan gemm_plan(int es, int M, int N, int K, bool splittable, int num_cu, boo
           rounds += sub == 4 ? 0.55 : sub == 2 ? 0.75 : rem ? 1.0 : 0.0;
           if (n_m >= 5 && full >= 2) rounds *= 1.06;
         }
-        const double walk = (K / 64 / s) * rounds * us_kt *
+        const double walk = ceil_div(K / 64, s) * rounds * us_kt *
                             (1.0 - 0.093 * (1.0 - std::min(1.0, units * inv_cu)));
         if (base[s] + walk * scale >= best_t) continue;
         const double t = base[s] + std::sqrt(walk * walk + stream * stream) * scale;
@@ -479,7 +491,7 @@ GemmPlan gemm_plan(int es, int M, int N, int K, bool splittable, int num_cu, boo
     int bm, bn, th;
     gemm_dl_tile(c.cfg, &bm, &bn, &th);
     for (int s = 1; s <= 8; s *= 2) {
-      if (s > 1 && (c.unsplit_only || !splittable || (K / 64) % s != 0 || K / s < 512)) continue;
+      if (s > 1 && (c.unsplit_only || !slices(s))) continue;
       if (K / 64 / s < c.min_kt) continue;
       const long units = (long)ceil_div(M, bm) * ceil_div(N, bn) * s;
       const long slots = (long)num_cu * c.occ;
@@ -494,12 +506,14 @@ GemmPlan gemm_plan(int es, int M, int N, int K, bool splittable, int num_cu, boo
         rounds += c.occ > 1 ? std::max(0.7, fill) : 1.0;
       double t = rounds * round_us(c, (double)(K / s) / 64.0);
       if (s > 1) t += (double)M * N * 4.0 * (s - 1) / 5.0e12 * 1e6;   // the consumer's reads
+      if (s > 1 && join) t += join_us(M, N);
       if (t < best_t * 0.999) {
         best_t = t;
         best = GemmPlan{c.cfg, s, 0, sub, sub ? (int)rem : 0};
       }
     }
   }
+  if (us) *us = best_t;
   // weights larger than the last-level cache (256 MB Infinity Cache) stream
   // from HBM once per row tile in plain order: use the grouped XCD order
   int bm, bn, th;

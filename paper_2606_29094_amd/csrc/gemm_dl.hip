@@ -14,6 +14,11 @@
 // v_mfma_f32_32x32x16_bf16 (MF = 32); the 16x16 epilogues are the same as the
 // register-staged kernel's, the 32x32 ones (plain, residual-add and SwiGLU
 // stores) follow the 32x32 accumulator layout.
+//
+// Operands in 8-bit integers (qint_gemm.h) take the same tiles: a row of 128 bytes then holds
+// 128 values, a 16-byte fragment 16 of them, and v_mfma_i32_16x16x64_i8 takes as many cycles
+// over it as the bf16 instruction. Their rows are passed as half as many 2-byte elements; what
+// multiplies (and what it accumulates in) follows from the epilogue (MulOf).
 #include <type_traits>
 
 #include "common.h"
@@ -21,6 +26,21 @@
 #include "kernels.h"
 
 namespace dlm {
+
+// The matrix instruction of a tile: a fragment of 16 bytes a lane each, accumulators of 16x16
+// (and 32x32) tiles. An epilogue for other operands than bf16 names its own as Epi::Mul.
+struct MulBf16 {
+  typedef f32x4 Acc16;
+  typedef f32x16 Acc32;
+  __device__ __forceinline__ static Acc16 mma16(const u32x4& a, const u32x4& b, const Acc16& c) {
+    return mfma16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c);
+  }
+  __device__ __forceinline__ static Acc32 mma32(const u32x4& a, const u32x4& b, const Acc32& c) {
+    return mfma32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c);
+  }
+};
+template <class Epi, class = void> struct MulOf { typedef MulBf16 type; };
+template <class Epi> struct MulOf<Epi, std::void_t<typename Epi::Mul>> { typedef typename Epi::Mul type; };
 
 // One BM x BN output tile at rows m0.., columns n0.., K range [kbeg, kend),
 // with the block's LDS at smem. tn and tz (column tile, K slice) are passed
@@ -31,6 +51,7 @@ __device__ __forceinline__ void dl_tile(char* smem, const bf16* __restrict__ A, 
                                         const bf16* __restrict__ B, int ldb, int M, int N,
                                         int m0, int n0, int tn, int tz, int kbeg, int kend,
                                         int rot, const Epi& epi) {
+  typedef typename MulOf<Epi>::type Mul;
   static_assert(RB == 64 || RB == 128, "k-tile row bytes");
   static_assert(SA >= 2 && SA <= 4 && SB >= SA && SB <= 4, "A and B stages");
   static_assert(MF == 16 || MF == 32, "MFMA tile");
@@ -126,7 +147,7 @@ __device__ __forceinline__ void dl_tile(char* smem, const bf16* __restrict__ A, 
   };
 
   // accumulators: 16x16 tiles (4 values per lane) or 32x32 tiles (16 per lane)
-  typedef typename std::conditional<MF == 32, f32x16, f32x4>::type Acc;
+  typedef typename std::conditional<MF == 32, typename Mul::Acc32, typename Mul::Acc16>::type Acc;
   Acc acc[FM][FN];
 #pragma unroll
   for (int a = 0; a < FM; ++a)
@@ -176,8 +197,7 @@ __device__ __forceinline__ void dl_tile(char* smem, const bf16* __restrict__ A, 
           for (int fm = 0; fm < FM; ++fm)
 #pragma unroll
             for (int fn = 0; fn < FN; ++fn)
-              acc[fm][fn] = mfma32_bf16(__builtin_bit_cast(bf16x8, af[0][fm]),
-                                        __builtin_bit_cast(bf16x8, bq[0][fn]), acc[fm][fn]);
+              acc[fm][fn] = Mul::mma32(af[0][fm], bq[0][fn], acc[fm][fn]);
         }
         return;
       }
@@ -189,8 +209,7 @@ __device__ __forceinline__ void dl_tile(char* smem, const bf16* __restrict__ A, 
         for (int fm = 0; fm < FM; ++fm)
 #pragma unroll
           for (int fn = 0; fn < FN; ++fn)
-            acc[fm][fn] = mfma32_bf16(__builtin_bit_cast(bf16x8, af[st & 1][fm]),
-                                      __builtin_bit_cast(bf16x8, bq[st & 1][fn]), acc[fm][fn]);
+            acc[fm][fn] = Mul::mma32(af[st & 1][fm], bq[st & 1][fn], acc[fm][fn]);
       }
       // schedule (mask 0x100: LDS reads, 0x008: MFMA): the first step's reads,
       // then each step's MFMAs with the next step's reads spread among them
@@ -241,14 +260,12 @@ __device__ __forceinline__ void dl_tile(char* smem, const bf16* __restrict__ A, 
       for (int fm = 0; fm < FM; ++fm)
 #pragma unroll
         for (int fn = 0; fn < FN; ++fn)
-          acc[fm][fn] = mfma16_bf16(__builtin_bit_cast(bf16x8, af0[fm]),
-                                    __builtin_bit_cast(bf16x8, bf0[fn]), acc[fm][fn]);
+          acc[fm][fn] = Mul::mma16(af0[fm], bf0[fn], acc[fm][fn]);
 #pragma unroll
       for (int fm = 0; fm < FM; ++fm)
 #pragma unroll
         for (int fn = 0; fn < FN; ++fn)
-          acc[fm][fn] = mfma16_bf16(__builtin_bit_cast(bf16x8, af1[fm]),
-                                    __builtin_bit_cast(bf16x8, bf1[fn]), acc[fm][fn]);
+          acc[fm][fn] = Mul::mma16(af1[fm], bf1[fn], acc[fm][fn]);
       // scheduling groups (mask 0x100: LDS reads, 0x008: MFMA)
       constexpr int NR = FM + FN, NM = FM * FN;
       __builtin_amdgcn_sched_group_barrier(0x100, NR, 0);
@@ -273,8 +290,7 @@ __device__ __forceinline__ void dl_tile(char* smem, const bf16* __restrict__ A, 
         for (int fm = 0; fm < FM; ++fm)
 #pragma unroll
           for (int fn = 0; fn < FN; ++fn)
-            acc[fm][fn] = mfma16_bf16(__builtin_bit_cast(bf16x8, af[fm]),
-                                      __builtin_bit_cast(bf16x8, bfr[fn]), acc[fm][fn]);
+            acc[fm][fn] = Mul::mma16(af[fm], bfr[fn], acc[fm][fn]);
       }
     }
   };
@@ -355,6 +371,7 @@ __device__ __forceinline__ void dls_tile(char* smem, const bf16* __restrict__ A,
                                          const bf16* __restrict__ B, int ldb, int M, int N,
                                          int m0, int n0, int tn, int tz, int kbeg, int kend,
                                          const Epi& epi) {
+  typedef typename MulOf<Epi>::type Mul;
   static_assert(SA >= 2 && SB >= SA && SB <= 4, "stages");
   constexpr int RB = 128, BK = 64, CPR = 8, RPI = 8;
   constexpr int NW = WAVES_M * WAVES_N;
@@ -422,11 +439,12 @@ __device__ __forceinline__ void dls_tile(char* smem, const bf16* __restrict__ A,
                                          (lptr_t)(dst + inst_b(j) * 1024), 16, 0, 0);
   };
 
-  f32x4 acc[FM][FN];
+  typedef typename Mul::Acc16 Acc;
+  Acc acc[FM][FN];
 #pragma unroll
   for (int a = 0; a < FM; ++a)
 #pragma unroll
-    for (int b = 0; b < FN; ++b) acc[a][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int b = 0; b < FN; ++b) acc[a][b] = Acc{};
 
   // fragment rows: base + (lane & 15); group g's chunk 4 g + lane / 16 at slot chunk ^ (row & 7)
   const int co0 = ((lane >> 4) ^ swz(lane & 15)) << 4;
@@ -460,16 +478,14 @@ __device__ __forceinline__ void dls_tile(char* smem, const bf16* __restrict__ A,
     for (int fm = 0; fm < FM; ++fm)
 #pragma unroll
       for (int fn = 0; fn < FN; ++fn)
-        acc[fm][fn] = mfma16_bf16(__builtin_bit_cast(bf16x8, g0a[fm]),
-                                  __builtin_bit_cast(bf16x8, g0b[fn]), acc[fm][fn]);
+        acc[fm][fn] = Mul::mma16(g0a[fm], g0b[fn], acc[fm][fn]);
   };
   auto mma1 = [&]() {
 #pragma unroll
     for (int fm = 0; fm < FM; ++fm)
 #pragma unroll
       for (int fn = 0; fn < FN; ++fn)
-        acc[fm][fn] = mfma16_bf16(__builtin_bit_cast(bf16x8, g1a[fm]),
-                                  __builtin_bit_cast(bf16x8, g1b[fn]), acc[fm][fn]);
+        acc[fm][fn] = Mul::mma16(g1a[fm], g1b[fn], acc[fm][fn]);
   };
 
 #pragma unroll
@@ -617,7 +633,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void gemm_dl_kernel(
       logical(xcd_range(id, n_n * n_m * (int)gridDim.z), tz, tm, tn);
     }
   } else {
-    const int n_main = n_n * n_m * (K / k_per_split) - n_tail;
+    const int n_main = n_n * n_m * ceil_div(K, k_per_split) - n_tail;
     const int id = blockIdx.x;
     if (id < n_main) {
       logical(group_m > 0 ? xcd_range(id, n_main) : id, tz, tm, tn);
@@ -734,6 +750,10 @@ constexpr bool head_tile(int cfg) {
          cfg == 42;
 }
 
+// The configurations that are planned with for 8-bit integers (16x16 MFMA; 10 and 11 are the
+// head's alone).
+constexpr bool int8_tile(int cfg) { return cfg != 10 && cfg != 11 && cfg != 62 && cfg != 65; }
+
 int gemm_dl_tile(int cfg, int* bm, int* bn, int* threads) {
   switch (cfg) {
 #define X(id, BM_, BN_, WM_, WN_, SA_, S_, RB_, MF_, SP_) \
@@ -797,11 +817,14 @@ hipError_t gemm_dl_launch(int cfg, const bf16* A, int lda, const bf16* B, int ld
                           int K, int splits, int group_m, int sub, int n_tail, const Epi& epi,
                           hipStream_t st) {
   if (M <= 0 || N <= 0) return hipSuccess;
-  if (K % 64 != 0 || splits < 1 || (K / 64) % splits != 0) return hipErrorInvalidValue;
+  // (slices of bf16 sums are equal; whole numbers also come in slices whose last one is shorter)
+  constexpr bool equal = std::is_same<typename MulOf<Epi>::type, MulBf16>::value;
+  if (K % 64 != 0 || splits < 1 || (equal && (K / 64) % splits != 0)) return hipErrorInvalidValue;
+  const int kps = ceil_div(K / 64, splits) * 64;
+  if (ceil_div(K, kps) != splits) return hipErrorInvalidValue;
   // the kernel addresses operands with 32-bit element offsets
   if ((double)(M - 1) * lda + K >= 4294967296.0 || (double)(N - 1) * ldb + K >= 4294967296.0)
     return hipErrorInvalidValue;
-  const int kps = K / splits;
   if (sub == 0) n_tail = 0;
   if (n_tail < 0 || (sub != 0 && (!Epi::kTailSplit || !(gemm_dl_subs(cfg) & sub))))
     return hipErrorInvalidValue;
@@ -809,6 +832,7 @@ hipError_t gemm_dl_launch(int cfg, const bf16* A, int lda, const bf16* B, int ld
 #define X(id, BM_, BN_, WM_, WN_, SA_, S_, RB_, MF_, SP_)                                        \
   case id: {                                                                             \
     if constexpr ((MF_ == 32 && !Epi::kMf32) || (Epi::kHead && !head_tile(id)) ||        \
+                  (!equal && !int8_tile(id)) ||                                          \
                   (!Epi::kOddFragments && (BN_ / WN_ / MF_) % 2 != 0))                   \
       return hipErrorInvalidValue;                                                       \
     else {                                                                               \
@@ -883,3 +907,5 @@ template hipError_t gemm_dl_launch<EpiLMHead>(int, const bf16*, int, const bf16*
     int, int, int, int, int, const EpiLMHead&, hipStream_t);
 
 }  // namespace dlm
+
+#include "qint_gemm.h"

@@ -111,10 +111,13 @@ constexpr int kFewRows = 1024;
 // allow_small: fp32 launches whose 128-wide tiles would not fill the CUs may use
 // the 16x32-tile kernel (plan cfg kSmallF32; every epilogue that needs only its
 // own wave)
+// join: K slices are added by a kernel of their own (and may differ by a k-tile); us: the
+// modelled time of a bf16 plan
 constexpr int kSmallF32 = -2;
 GemmPlan gemm_plan(int elem_bytes, int M, int N, int K, bool splittable, int num_cu,
                    bool allow_mf32 = true, bool allow_tail = true, bool allow_odd = true,
-                   int few_rows = kFewRows, bool allow_small = true);
+                   int few_rows = kFewRows, bool allow_small = true, bool join = false,
+                   double* us = nullptr);
 // plan of the LM-head GEMM (M rows x V vocab entries)
 GemmPlan lm_head_plan(int elem_bytes, int M, int V, int K, int num_cu);
 template <typename T>

@@ -48,10 +48,12 @@ struct QintOut {
   int mode;
   bool wide;
 };
-// A product's way: blocks of 16 rows straight from memory (nf 16-column fragments, `waves` waves
-// that share K), K in `slices` over blocks that write their sums to scratch.
+// A product's way: (gemm) the GEMM tiles, or blocks of 16 rows and columns straight from memory.
+// slices > 1: as many K slices go to scratch and are added by a second kernel.
 struct QintPlan {
-  int nf = 1, waves = 8, slices = 1;
+  bool gemm = false;
+  GemmPlan g{};
+  int slices = 1;
   size_t scratch = 0;
 };
 QintPlan qint_plan(int rows, int n, int k, bool swiglu, int num_cu);

@@ -318,14 +318,15 @@ hipError_t qint_norm(const QintNorm<T>& a, const QintView& o, hipStream_t st) {
   const bool vec = vector_rows(a.h, a.ldh, o.k, 4) && vector_rows(a.g, 4, o.k, 4) &&
                    (!a.h_out || vector_rows(a.h_out, a.ldo, o.k, 4)) &&
                    (a.splits == 0 || (vector_rows(a.add, a.lda, o.k, 4) && a.stride % 4 == 0));
-  const int c = o.n < 512 && quads <= 1024 ? 1 : 4;
 #define NORM(S_, VEC_, C_, LOOP_)                                                                  \
   DLM_LAUNCH((qint_norm_kernel<T, S_, VEC_, C_, LOOP_>), dim3(blocks), dim3(qint_threads(quads, C_)), 0, \
              st, a, o)
+// Four vectors a thread; two where the slices' loads take as many registers again (4096 x 4096, two
+// slices: 52 us against 59, one slice 40.9 against 40.4; one vector 77 and 72).
 #define NORM_C(S_)                                                                                 \
   do {                                                                                             \
     if (quads > 4096) NORM(S_, true, 4, true);                                                     \
-    else if (c == 1) NORM(S_, true, 1, false);                                                     \
+    else if (a.splits > 1 && quads <= 2048) NORM(S_, true, 2, false);                              \
     else NORM(S_, true, 4, false);                                                                 \
   } while (0)
   if (!vec) {

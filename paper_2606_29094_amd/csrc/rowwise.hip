@@ -747,4 +747,3 @@ INST(float)
 
 // 8-bit integers
 #include "qint_rowwise.h"
-#include "qint_gemm.h"

@@ -650,25 +650,32 @@ def qint_unpack(q: DlmQint, out, stream=None):
 def qint_norm(h, gain, eps: float, q: DlmQint, add=None, h_out=None, stream=None):
     """h' = h + add (fp32 [n, k]; add [n, k] or slices [splits, n, k], bf16 or fp32), stored to
     h_out or, where there is an add and no h_out, to h; its RMS norm times gain, packed into q."""
-    import torch
+    f32 = gain.dtype
+    if str(f32) != "torch.float32":
+        raise ValueError(f"gain is {f32}, expected torch.float32")
     shape = (q.n, q.k)
-    ldh = _rows_of("h", h, shape, torch.float32)
-    _flat("gain", gain, (q.k,), torch.float32)
-    splits, stride, ldadd, dt = 0, 0, 0, DLM_F32
-    if add is not None:
-        dt = _dtype_id(add.dtype)
-        slices = add if add.dim() == 3 else add[None]
-        splits = slices.shape[0]
+    ldh = _rows_of("h", h, shape, f32)
+    _flat("gain", gain, (q.k,), f32)
+    splits, stride, ldadd, dt, part = 0, 0, 0, DLM_F32, None
+    if add is None:
+        tensors = [h, gain]
+    else:
+        dt, tensors = _dtype_id(add.dtype), [h, gain, add]
+        if add.dim() == 2:
+            splits, ldadd = 1, _rows_of("add", add, shape)
+        elif add.shape[0]:
+            splits, ldadd = add.shape[0], _rows_of("add", add[0], shape)
+            stride = add.stride(0) if splits > 1 else 0
         if splits:
-            ldadd = _rows_of("add", slices[0], shape)
-            stride = slices.stride(0) if splits > 1 else 0
+            part = add.data_ptr()
         if h_out is None:
             h_out = h
-    ldo = _rows_of("h_out", h_out, shape, torch.float32) if h_out is not None else 0
-    st = _on(stream, *(t for t in (h, gain, add, h_out) if t is not None), *q._keep)
-    check(lib().dlm_qint_norm(h.data_ptr(), ldh, None if h_out is None else h_out.data_ptr(), ldo, dt,
-                            add.data_ptr() if splits else None, splits, stride, ldadd,
-                            gain.data_ptr(), eps, ctypes.byref(q), st))
+    ldo, out = 0, None
+    if h_out is not None:
+        ldo, out = (ldh if h_out is h else _rows_of("h_out", h_out, shape, f32)), h_out.data_ptr()
+        tensors.append(h_out)
+    check(lib().dlm_qint_norm(h.data_ptr(), ldh, out, ldo, dt, part, splits, stride, ldadd,
+                              gain.data_ptr(), eps, ctypes.byref(q), _on(stream, *tensors, *q._keep)))
 
 
 def qint_linear_workspace(m_rows: int, w: DlmQint, epilogue: int = DLM_QINT_STORE) -> int:
@@ -681,14 +688,15 @@ def qint_linear(x: DlmQint, w: DlmQint, y, epilogue: int = DLM_QINT_STORE, works
               stream=None):
     """y = x @ w.T (in y's dtype), residual + x @ w.T (fp32; residual may be y), or silu(gate) *
     up in y's dtype; workspace: at least qint_linear_workspace bytes, or None where that is 0."""
-    import torch
     n_out = w.n // 2 if epilogue == DLM_QINT_SWIGLU else w.n
     ldy, tensors = _rows_of("y", y, (x.n, n_out)), [y, *x._keep, *w._keep]
     r, ldr, ws, size = None, 0, None, 0
     if epilogue == DLM_QINT_ADD:
         if residual is None:
             raise ValueError("the add epilogue takes a residual")
-        r, ldr = residual.data_ptr(), _rows_of("residual", residual, (x.n, n_out), torch.float32)
+        r, ldr = residual.data_ptr(), _rows_of("residual", residual, (x.n, n_out))
+        if _dtype_id(residual.dtype) != DLM_F32:
+            raise ValueError(f"residual is {residual.dtype}, expected torch.float32")
         tensors.append(residual)
     if workspace is not None:
         ws, size = _scratch(workspace)
