@@ -490,6 +490,27 @@ dlm_status dlm_qint_linear(const dlm_qint* x, const dlm_qint* w, int32_t epilogu
                          int64_t ldr, int32_t dtype, void* y, int64_t ldy, void* workspace,
                          size_t ws_bytes, void* stream);
 
+/* A model whose layer projections are in 8 bits (shapes as in dlm_layer_weights); embedding, LM
+ * head and norms as in dlm_weights, rms_eps positive. Every entry point takes such a model, with
+ * any cache: its steps pack each projection's input rows (the norms' outputs by dlm_qint_norm, the
+ * attention's and the gated activations, held in the model dtype, by dlm_qint_pack) and
+ * multiply by dlm_qint_linear, residuals added by its epilogue; all else is as in a step of
+ * other models. In a dlm_trace a_attn and a_ffn are then the packed rows' values, in the model
+ * dtype, and qkv is one slice. */
+typedef struct dlm_layer_qint {
+  const float* attn_norm;
+  dlm_qint w_qkv, w_o;
+  const float* ffn_norm;
+  dlm_qint w_gate_up, w_down;
+} dlm_layer_qint;
+typedef struct dlm_weights_qint {
+  const void* embed;
+  const void* lm_head;
+  const float* final_norm;
+  const dlm_layer_qint* layers; /* host array of n_layers entries, copied by load   */
+} dlm_weights_qint;
+dlm_status dlm_load_weights_qint(const dlm_config* cfg, const dlm_weights_qint* w, dlm_model** out);
+
 /* Test hooks for the bf16 GEMM kernel (the contraction of every projection of
  * the step: QKV, output, gate/up and down). dlm_debug_gemm_info: the output
  * tile (bm x bn) of tile configuration cfg and, in *subs, the sub-tile splits
@@ -558,6 +579,13 @@ dlm_status dlm_debug_mx_attention_plan(int32_t dtype, int32_t n_q_heads, int32_t
                                        int32_t head_dim, int32_t n_req, const int32_t* rows,
                                        const int32_t* seq_len, size_t scratch_bytes, int32_t num_cu,
                                        int32_t* kernel, int32_t* splits);
+
+/* Test hook for the planner of products of 8-bit matrices (host only), on num_cu CUs: out = tile
+ * configuration (-1: blocks of 16 rows straight from memory), K slices, sub-tiles per tile of the
+ * last round (0: whole), row tiles of a group (0: plain order). DLM_EINVAL as in dlm_qint_linear, for a
+ * NULL out, no rows or num_cu below 1. */
+dlm_status dlm_debug_qint_linear_plan(int32_t m_rows, int32_t n, int32_t k, int32_t epilogue,
+                                      int32_t num_cu, int32_t out[4]);
 
 /* Kernel timing. While enabled, every kernel the library enqueues for this
  * model (or, when only_class is not NULL, every kernel of that class; see also

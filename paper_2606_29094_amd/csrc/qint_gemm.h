@@ -398,16 +398,20 @@ __global__ __launch_bounds__(256) void qint_join_kernel(const int32_t* __restric
 // 18.6, 26.0 / 21.6.
 constexpr int kQintFewRows = 16;
 
+// Rows that the tiles can address (32-bit offsets of 2-byte units); more are taken in turn.
+static int qint_near_rows(int units) { return (int)std::min<long>(((1L << 32) / units - 1) & ~255L, 1 << 30); }
+
 QintPlan qint_plan(int rows, int n, int k, bool swiglu, int num_cu) {
   QintPlan p;
   if (rows <= 0) return p;
   const int units = qint_row(k) / 2, cols = swiglu ? ceil_div(n, 32) * 32 : n;   // 2-byte units of a row
+  const bool split = !swiglu && rows <= qint_near_rows(units);
   double us, best;
   p.gemm = true;
-  p.g = gemm_plan(2, rows, cols, units, !swiglu, num_cu, false, true, !swiglu, kFewRows, false, !swiglu, &best);
+  p.g = gemm_plan(2, rows, cols, units, split, num_cu, false, true, !swiglu, kFewRows, false, split, &best);
   if (swiglu && (long)rows * cols < 64 * 64 * (long)num_cu) {     // (the smallest tiles leave CUs idle)
-    const GemmPlan split = gemm_plan(2, rows, n, units, true, num_cu, false, true, true, kFewRows, false, true, &us);
-    if (split.splits > 1 && us < best) best = us, p.g = split;
+    const GemmPlan g = gemm_plan(2, rows, n, units, true, num_cu, false, true, true, kFewRows, false, true, &us);
+    if (g.splits > 1 && us < best) best = us, p.g = g;
   }
   // Several row tiles: in groups of 8, so that an XCD's blocks share weight columns as well as rows
   // (37888 x 3584 SwiGLU at 2048 rows 270 -> 249 us, at 4096 512 -> 496; 3584 x 18944 at 4096 240 ->
@@ -432,7 +436,20 @@ QintPlan qint_plan(int rows, int n, int k, bool swiglu, int num_cu) {
 hipError_t qint_matmul(const QintPlan& plan, const QintView& x, const QintView& w, QintOut o, void* scratch,
                        hipStream_t st) {
   if (x.n == 0) return hipSuccess;
-  const int row_bytes = qint_row(w.k);
+  const int row_bytes = qint_row(w.k), near = qint_near_rows(row_bytes / 2);
+  if (x.n > near) {
+    const LaunchSpan span(true);
+    for (int at = 0; at < x.n; at += near) {
+      const QintView part{x.codes + (long)at * row_bytes, x.scales + at, std::min(near, x.n - at), x.k};
+      QintOut op = o;
+      op.y = reinterpret_cast<char*>(o.y) + (long)at * o.ldy * (o.wide ? 4 : 2);
+      if (o.mode == DLM_QINT_ADD) op.res = o.res + (long)at * o.ldr;
+      if (at + near >= x.n) span.last();
+      const hipError_t e = qint_matmul(plan, part, w, op, scratch, st);
+      if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+  }
   o.m = x.n, o.n = w.n, o.f = w.n / 2, o.sx = x.scales, o.sw = w.scales;
   const bool swiglu = o.mode == DLM_QINT_SWIGLU;
   const int n_out = swiglu ? o.f : o.n, es = o.wide ? 4 : 2;

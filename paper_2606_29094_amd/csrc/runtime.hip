@@ -161,6 +161,7 @@ struct dlm_model {
   const float* final_norm;
   std::vector<dlm_layer_weights> layers;
   std::vector<dlm_layer_mx> mx;   // packed projections (dlm_load_weights_mx), or empty
+  std::vector<dlm_layer_qint> qint;   // projections in 8 bits (dlm_load_weights_qint), or empty
   int num_cu;
   size_t es;   // element size
 };
@@ -193,9 +194,10 @@ namespace {
 // Workspace layout of a step with n recomputed rows and n_req requests.
 struct Layout {
   size_t h, a, qkv, cs, q, ao, part, act, lm_rows, lm_count, req_off, req_cnt, u, pm, ps, pi,
-      conf, tok, mx, total;
+      conf, tok, mx, codes, scales, total;
   GemmPlan g_qkv, g_o, g_gu, g_down, g_lm, g_logits;
   MxPlan q_qkv, q_o, q_gu, q_down;   // of a model with packed projections
+  QintPlan i_qkv, i_o, i_gu, i_down; // of a model with projections in 8 bits
   int s_qkv, s_o, s_down, tiles, m_max;
 };
 
@@ -219,7 +221,13 @@ Layout layout(const dlm_model* m, int n, int n_req) {
   const int qkv_dim = (c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim;
   const int qd = c.n_q_heads * c.head_dim;
   const int es_i = (int)m->es;
-  if (m->mx.empty()) {
+  if (!m->qint.empty()) {
+    L.i_qkv = qint_plan(n, qkv_dim, c.d_model, false, m->num_cu);
+    L.i_o = qint_plan(n, c.d_model, qd, false, m->num_cu);
+    L.i_gu = qint_plan(n, 2 * c.d_ffn, c.d_model, true, m->num_cu);
+    L.i_down = qint_plan(n, c.d_model, c.d_ffn, false, m->num_cu);
+    L.s_qkv = 1;                                  // (products join their own K slices)
+  } else if (m->mx.empty()) {
     L.g_qkv = projection_plan(es_i, n, qkv_dim, c.d_model, m->num_cu);
     L.g_o = projection_plan(es_i, n, c.d_model, qd, m->num_cu);
     L.g_gu = gate_up_plan(es_i, n, c.d_ffn, c.d_model, m->num_cu);
@@ -265,7 +273,12 @@ Layout layout(const dlm_model* m, int n, int n_req) {
   L.pi = take((size_t)L.tiles * std::max(L.m_max, 1) * 4);
   L.conf = take((size_t)std::max(L.m_max, 1) * 4);
   L.tok = take((size_t)std::max(L.m_max, 1) * 4);
-  L.mx = take(std::max({L.q_qkv.scratch, L.q_o.scratch, L.q_gu.scratch, L.q_down.scratch}));
+  L.mx = take(std::max({L.q_qkv.scratch, L.q_o.scratch, L.q_gu.scratch, L.q_down.scratch, L.i_qkv.scratch,
+                        L.i_o.scratch, L.i_gu.scratch, L.i_down.scratch}));
+  if (!m->qint.empty()) {    // the packed inputs of one projection at a time
+    L.codes = take((size_t)n * qint_row(std::max({c.d_model, qd, c.d_ffn})));
+    L.scales = take((size_t)n * sizeof(float));
+  }
   L.total = off;
   return L;
 }
@@ -418,8 +431,21 @@ dlm_status run_forward(dlm_model* m, dlm_cache* c, const dlm_batch* b, const Ste
   const AttnPlan ap = attention_plan(p, hq, hkv, dh, sizeof(T), L.lm_rows - L.part, m->num_cu);
   const MxAttnPlan mx_ap =
       c->mx ? mx_attention_plan(p, hq, hkv, dh, sizeof(T), L.lm_rows - L.part, m->num_cu) : MxAttnPlan{};
-  const bool w4 = !m->mx.empty();
+  const bool w4 = !m->mx.empty(), w8 = !m->qint.empty();
   void* const mxs = ws + L.mx;
+  // 8-bit projections: their inputs packed row by row, and the products
+  const auto packed = [&](int k) {
+    return QintView{reinterpret_cast<int8_t*>(ws + L.codes), reinterpret_cast<float*>(ws + L.scales), n, k};
+  };
+  const auto norm8 = [&](const float* gain) {
+    return qint_norm<float>(QintNorm<float>{h, d, nullptr, 0, nullptr, 0, 0, 0, gain, cf.rms_eps}, packed(d), st);
+  };
+  const auto product8 = [&](const QintPlan& plan, const dlm_qint& w, int mode, void* y, int ldy, bool wide) {
+    QintOut o{};
+    o.y = y, o.ldy = ldy, o.res = mode == DLM_QINT_ADD ? reinterpret_cast<float*>(y) : nullptr, o.ldr = ldy;
+    o.mode = mode, o.wide = wide;
+    return qint_matmul(plan, packed(w.k), QintView{w.codes, w.scales, w.n, w.k}, o, mxs, st);
+  };
 
   LAUNCH(m, st, "embed_norm", embed_norm_rows<T>(p, reinterpret_cast<const T*>(m->embed), d, cf.vocab,
                          cf.mask_id, b->tokens, b->mask, m->layers[0].attn_norm, cf.rms_eps, dh,
@@ -428,15 +454,20 @@ dlm_status run_forward(dlm_model* m, dlm_cache* c, const dlm_batch* b, const Ste
   for (int l = 0; l < cf.n_layers; ++l) {
     const dlm_layer_weights& w = m->layers[l];
     const dlm_layer_mx* w4l = w4 ? &m->mx[l] : nullptr;
+    const dlm_layer_qint* w8l = w8 ? &m->qint[l] : nullptr;
     const MxKv kv4 = c->mx ? c->mx_layer(l) : MxKv{};
     T* kc = c->mx ? nullptr : reinterpret_cast<T*>(c->k_layer(l));
     T* vc = c->mx ? nullptr : reinterpret_cast<T*>(c->v_layer(l));
     const dlm_trace* t = tr && tr->layer == l ? tr : nullptr;
+    if (w8) LAUNCH(m, st, "rmsnorm", norm8(w.attn_norm));
     if (t) {
+      if (w8 && t->a_attn) HIPCHECK(qint_unpack<T>(packed(d), a, d, st));
       TRACE_COPY(t->h_in, h, (size_t)n * d * 4);
       TRACE_COPY(t->a_attn, a, (size_t)n * d * es);
     }
-    if (w4)
+    if (w8)
+      LAUNCH(m, st, "gemm_qkv", product8(L.i_qkv, w8l->w_qkv, DLM_QINT_STORE, qkv, qkv_dim, true));
+    else if (w4)
       LAUNCH(m, st, "gemm_qkv", mx_matmul<T>(L.q_qkv, a, d, n, mx_view(w4l->w_qkv), d, DLM_MX_STORE, qkv,
                                              qkv_dim, mxs, st));
     else
@@ -460,7 +491,11 @@ dlm_status run_forward(dlm_model* m, dlm_cache* c, const dlm_batch* b, const Ste
     }
     if (t) TRACE_COPY(t->attn_out, ao, (size_t)n * qd * es);
     // O projection; its residual update is fused into the FFN norm when K is split
-    if (L.s_o == 1) {
+    if (w8) {
+      LAUNCH(m, st, "pack_attention", qint_pack<T>(ao, qd, packed(qd), st));
+      LAUNCH(m, st, "gemm_o", product8(L.i_o, w8l->w_o, DLM_QINT_ADD, h, d, true));
+      LAUNCH(m, st, "rmsnorm", norm8(w.ffn_norm));
+    } else if (L.s_o == 1) {
       if (w4)
         LAUNCH(m, st, "gemm_o", mx_matmul<T>(L.q_o, ao, qd, n, mx_view(w4l->w_o), qd, DLM_MX_ADD, h, d,
                                              mxs, st));
@@ -479,10 +514,14 @@ dlm_status run_forward(dlm_model* m, dlm_cache* c, const dlm_batch* b, const Ste
                                                                 cf.rms_eps, a, st));
     }
     if (t) {
+      if (w8 && t->a_ffn) HIPCHECK(qint_unpack<T>(packed(d), a, d, st));
       TRACE_COPY(t->h_mid, h, (size_t)n * d * 4);
       TRACE_COPY(t->a_ffn, a, (size_t)n * d * es);
     }
-    if (w4)
+    if (w8)
+      LAUNCH(m, st, "gemm_gate_up_swiglu",
+             product8(L.i_gu, w8l->w_gate_up, DLM_QINT_SWIGLU, act, cf.d_ffn, sizeof(T) == 4));
+    else if (w4)
       LAUNCH(m, st, "gemm_gate_up_swiglu", mx_matmul<T>(L.q_gu, a, d, n, mx_view(w4l->w_gate_up), d,
                                                         DLM_MX_SWIGLU, act, cf.d_ffn, mxs, st));
     else
@@ -492,7 +531,10 @@ dlm_status run_forward(dlm_model* m, dlm_cache* c, const dlm_batch* b, const Ste
     // down projection; its residual update is fused into the next layer's norm
     const float* next_norm = l + 1 < cf.n_layers ? m->layers[l + 1].attn_norm : nullptr;
     T* next_a = l + 1 < cf.n_layers ? a : nullptr;
-    if (L.s_down == 1) {
+    if (w8) {
+      LAUNCH(m, st, "pack_act", qint_pack<T>(act, cf.d_ffn, packed(cf.d_ffn), st));
+      LAUNCH(m, st, "gemm_down", product8(L.i_down, w8l->w_down, DLM_QINT_ADD, h, d, true));
+    } else if (L.s_down == 1) {
       if (w4)
         LAUNCH(m, st, "gemm_down", mx_matmul<T>(L.q_down, act, cf.d_ffn, n, mx_view(w4l->w_down), cf.d_ffn,
                                                 DLM_MX_ADD, h, d, mxs, st));
@@ -740,6 +782,54 @@ dlm_status dlm_load_weights_mx(const dlm_config* cfg, const dlm_weights_mx* w, d
     m = new dlm_model();
     m->mx.assign(w->layers, w->layers + cfg->n_layers);
     for (const dlm_layer_mx& lw : m->mx)
+      m->layers.push_back({lw.attn_norm, nullptr, nullptr, lw.ffn_norm, nullptr, nullptr});
+  } catch (const std::bad_alloc&) {
+    delete m;
+    return fail(DLM_ESIZE, "out of host memory for %d layers", cfg->n_layers);
+  }
+  m->cfg = *cfg;
+  m->embed = w->embed;
+  m->lm_head = w->lm_head;
+  m->final_norm = w->final_norm;
+  m->es = cfg->dtype == DLM_BF16 ? 2 : 4;
+  m->num_cu = device_cus();
+  *out = m;
+  return DLM_OK;
+}
+
+dlm_status dlm_load_weights_qint(const dlm_config* cfg, const dlm_weights_qint* w, dlm_model** out) {
+  g_err.clear();
+  if (!out) return fail(DLM_EINVAL, "out is NULL");
+  *out = nullptr;
+  dlm_status s = check_config(cfg);
+  if (s != DLM_OK) return s;
+  if (!(cfg->rms_eps > 0.f) || !std::isfinite(cfg->rms_eps))
+    return fail(DLM_EINVAL, "rms_eps %g is not positive and finite", cfg->rms_eps);
+  if (!w || !w->embed || !w->lm_head || !w->final_norm || !w->layers)
+    return fail(DLM_EINVAL, "weights pointer is NULL");
+  const int qd = cfg->n_q_heads * cfg->head_dim, qkv_dim = qd + 2 * cfg->n_kv_heads * cfg->head_dim;
+  for (int l = 0; l < cfg->n_layers; ++l) {
+    const dlm_layer_qint& lw = w->layers[l];
+    char what[48];
+    if (!lw.attn_norm || !lw.ffn_norm) return fail(DLM_EINVAL, "layer %d: weight pointer is NULL", l);
+    const struct { const dlm_qint* w; int n, k, epilogue; const char* name; } parts[4] = {
+        {&lw.w_qkv, qkv_dim, cfg->d_model, DLM_QINT_STORE, "w_qkv"},
+        {&lw.w_o, cfg->d_model, qd, DLM_QINT_ADD, "w_o"},
+        {&lw.w_gate_up, 2 * cfg->d_ffn, cfg->d_model, DLM_QINT_SWIGLU, "w_gate_up"},
+        {&lw.w_down, cfg->d_model, cfg->d_ffn, DLM_QINT_ADD, "w_down"}};
+    for (const auto& q : parts) {
+      snprintf(what, sizeof what, "layer %d: %s", l, q.name);
+      if (q.w->n != q.n)
+        return fail(DLM_EINVAL, "%s: 8-bit matrix of %d rows, expected %d", what, q.w->n, q.n);
+      if ((s = check_qint(q.w, q.k, false, what)) != DLM_OK) return s;
+      if ((s = check_qint_linear(0, q.w, q.epilogue)) != DLM_OK) return s;
+    }
+  }
+  dlm_model* m = nullptr;
+  try {
+    m = new dlm_model();
+    m->qint.assign(w->layers, w->layers + cfg->n_layers);
+    for (const dlm_layer_qint& lw : m->qint)
       m->layers.push_back({lw.attn_norm, nullptr, nullptr, lw.ffn_norm, nullptr, nullptr});
   } catch (const std::bad_alloc&) {
     delete m;
@@ -1472,6 +1562,24 @@ dlm_status dlm_qint_linear(const dlm_qint* x, const dlm_qint* w, int32_t epilogu
   QintOut o{};
   o.y = y, o.ldy = ldy, o.res = residual, o.ldr = ldr, o.mode = epilogue, o.wide = dtype == DLM_F32;
   HIPCHECK(qint_matmul(plan, qint_view(*x), qint_view(*w), o, workspace, reinterpret_cast<hipStream_t>(stream)));
+  return DLM_OK;
+}
+
+dlm_status dlm_debug_qint_linear_plan(int32_t m_rows, int32_t n, int32_t k, int32_t epilogue,
+                                      int32_t num_cu, int32_t out[4]) {
+  g_err.clear();
+  int8_t unused[16] __attribute__((aligned(16)));   // (buffers for the check; not looked at)
+  float scale;
+  const dlm_qint w{unused, &scale, n, k};
+  dlm_status s = check_qint_linear(m_rows, &w, epilogue);
+  if (s != DLM_OK) return s;
+  if (!out) return fail(DLM_EINVAL, "out is NULL");
+  if (m_rows < 1 || num_cu < 1) return fail(DLM_EINVAL, "%d rows on %d CUs", m_rows, num_cu);
+  const QintPlan p = qint_plan(m_rows, n, k, epilogue == DLM_QINT_SWIGLU, num_cu);
+  out[0] = p.gemm ? p.g.cfg : -1;
+  out[1] = p.slices;
+  out[2] = p.gemm ? p.g.sub : 0;
+  out[3] = p.gemm ? p.g.group_m : 0;
   return DLM_OK;
 }
 

@@ -41,7 +41,8 @@ EXPORTS = ["dlm_load_weights", "dlm_model_destroy", "dlm_workspace_bytes",
            "dlm_mx_kv_read", "dlm_mx_kv_attention_workspace", "dlm_mx_kv_attention",
            "dlm_debug_mx_linear_plan", "dlm_debug_mx_attention_plan",
            "dlm_qint_bytes", "dlm_qint_pack", "dlm_qint_unpack", "dlm_qint_norm",
-           "dlm_qint_linear_workspace", "dlm_qint_linear"]
+           "dlm_qint_linear_workspace", "dlm_qint_linear", "dlm_load_weights_qint",
+           "dlm_debug_qint_linear_plan"]
 
 
 class DlmConfig(ctypes.Structure):
@@ -79,6 +80,16 @@ class DlmWeightsMx(ctypes.Structure):
 class DlmQint(ctypes.Structure):
     _keep = ()              # the tensors of make_qint
     _fields_ = [("codes", c_void_p), ("scales", c_void_p), ("n", c_int32), ("k", c_int32)]
+
+
+class DlmLayerQint(ctypes.Structure):
+    _fields_ = [("attn_norm", c_void_p), ("w_qkv", DlmQint), ("w_o", DlmQint),
+                ("ffn_norm", c_void_p), ("w_gate_up", DlmQint), ("w_down", DlmQint)]
+
+
+class DlmWeightsQint(ctypes.Structure):
+    _fields_ = [("embed", c_void_p), ("lm_head", c_void_p), ("final_norm", c_void_p),
+                ("layers", POINTER(DlmLayerQint))]
 
 
 class DlmKvRows(ctypes.Structure):
@@ -204,6 +215,9 @@ def lib():
         L.dlm_qint_linear_workspace.argtypes = [c_int32, POINTER(DlmQint), c_int32, POINTER(c_size_t)]
         L.dlm_qint_linear.argtypes = [POINTER(DlmQint), POINTER(DlmQint), c_int32, c_void_p, c_int64,
                                     c_int32, c_void_p, c_int64, c_void_p, c_size_t, c_void_p]
+        L.dlm_debug_qint_linear_plan.argtypes = [c_int32, c_int32, c_int32, c_int32, c_int32,
+                                                 POINTER(c_int32)]
+        L.dlm_load_weights_qint.argtypes = [POINTER(DlmConfig), POINTER(DlmWeightsQint), POINTER(c_void_p)]
         L.dlm_last_error.argtypes = []
         L.dlm_last_error.restype = ctypes.c_char_p
         for name in ["dlm_load_weights", "dlm_workspace_bytes", "dlm_kv_cache_alloc",
@@ -218,7 +232,8 @@ def lib():
                      "dlm_mx_kv_read", "dlm_mx_kv_attention_workspace", "dlm_mx_kv_attention",
                      "dlm_debug_mx_linear_plan", "dlm_debug_mx_attention_plan",
                      "dlm_qint_bytes", "dlm_qint_pack", "dlm_qint_unpack", "dlm_qint_norm",
-                     "dlm_qint_linear_workspace", "dlm_qint_linear"]:
+                     "dlm_qint_linear_workspace", "dlm_qint_linear", "dlm_load_weights_qint",
+                     "dlm_debug_qint_linear_plan"]:
             getattr(L, name).restype = c_int32
         _lib = L
     return _lib
@@ -703,6 +718,22 @@ def qint_linear(x: DlmQint, w: DlmQint, y, epilogue: int = DLM_QINT_STORE, works
         tensors.append(workspace)
     check(lib().dlm_qint_linear(ctypes.byref(x), ctypes.byref(w), epilogue, r, ldr,
                               _dtype_id(y.dtype), y.data_ptr(), ldy, ws, size, _on(stream, *tensors)))
+
+
+def load_weights_qint(cfg: DlmConfig, weights: DlmWeightsQint) -> c_void_p:
+    h = c_void_p()
+    check(lib().dlm_load_weights_qint(ctypes.byref(cfg), ctypes.byref(weights), ctypes.byref(h)))
+    h.config = cfg
+    return h
+
+
+def debug_qint_linear_plan(m_rows: int, n: int, k: int, epilogue: int = DLM_QINT_STORE,
+                           num_cu: int = 256):
+    """(tile configuration or -1, K slices, sub-tiles, row tiles of a group) of a product of
+    8-bit matrices (dlm_debug_qint_linear_plan)."""
+    out = (c_int32 * 4)()
+    check(lib().dlm_debug_qint_linear_plan(m_rows, n, k, epilogue, num_cu, out))
+    return tuple(out)
 
 
 def profile_enable(model, on: bool, only_class: str | None = None):

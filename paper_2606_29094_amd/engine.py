@@ -64,6 +64,20 @@ def pack_layer(layer: dict) -> dict:
     return out
 
 
+def pack_layer_qint(layer: dict) -> dict:
+    """A layer's weights with its projections in 8 bits (those that are not yet)."""
+    out = dict(layer)
+    for name in ("w_qkv", "w_o", "w_gate_up", "w_down"):
+        w = layer[name]
+        if isinstance(w, dlm.DlmQint):
+            continue
+        n, k = w.shape
+        codes = torch.empty(dlm.qint_bytes(n, k)[0], dtype=torch.int8, device=w.device)
+        out[name] = dlm.make_qint(codes, torch.empty(n, dtype=torch.float32, device=w.device), n, k)
+        dlm.qint_pack(w, out[name])
+    return out
+
+
 class DeviceModel:
     """Caller-owned device weights plus the library's model handle.
 
@@ -73,19 +87,28 @@ class DeviceModel:
 
     packed: the layers' projections are held in 4 bits (dlm_load_weights_mx).
     Each is then either a tensor, packed here and not kept, or a dlm.DlmMx that
-    is packed already. ``self.tensors`` holds the packed ones in their place."""
+    is packed already. ``self.tensors`` holds the packed ones in their place.
 
-    def __init__(self, shape: ModelShape, tensors: dict, inv_tau: float, packed: bool = False):
+    int8: the projections are held in 8 bits and multiplied with their inputs packed to 8 bits
+    (dlm_load_weights_qint); each is a tensor or a dlm.DlmQint."""
+
+    def __init__(self, shape: ModelShape, tensors: dict, inv_tau: float, packed: bool = False,
+                 int8: bool = False):
+        if packed and int8:
+            raise ValueError("projections in 4 bits or in 8 bits, not both")
         self.shape = shape
         self.packed = packed
+        self.int8 = int8
         self.inv_tau = float(inv_tau)
-        if packed:
-            tensors = dict(tensors, layers=[pack_layer(l) for l in tensors["layers"]])
+        if packed or int8:
+            pack = pack_layer_qint if int8 else pack_layer
+            tensors = dict(tensors, layers=[pack(l) for l in tensors["layers"]])
         self.tensors = tensors
-        if packed:
-            self._layer_arr = (dlm.DlmLayerMx * shape.n_layers)(*[
-                dlm.DlmLayerMx(l["attn_norm"].data_ptr(), l["w_qkv"], l["w_o"],
-                               l["ffn_norm"].data_ptr(), l["w_gate_up"], l["w_down"])
+        if packed or int8:
+            layer_type = dlm.DlmLayerQint if int8 else dlm.DlmLayerMx
+            self._layer_arr = (layer_type * shape.n_layers)(*[
+                layer_type(l["attn_norm"].data_ptr(), l["w_qkv"], l["w_o"],
+                           l["ffn_norm"].data_ptr(), l["w_gate_up"], l["w_down"])
                 for l in tensors["layers"]])
         else:
             self._layer_arr = (dlm.DlmLayerWeights * shape.n_layers)(*[
@@ -93,7 +116,7 @@ class DeviceModel:
                                     l["w_o"].data_ptr(), l["ffn_norm"].data_ptr(),
                                     l["w_gate_up"].data_ptr(), l["w_down"].data_ptr())
                 for l in tensors["layers"]])
-        self.weights = (dlm.DlmWeightsMx if packed else dlm.DlmWeights)(
+        self.weights = (dlm.DlmWeightsQint if int8 else dlm.DlmWeightsMx if packed else dlm.DlmWeights)(
             tensors["embed"].data_ptr(), tensors["lm_head"].data_ptr(),
             tensors["final_norm"].data_ptr(), self._layer_arr)
         mask_id = shape.vocab - 1 if shape.mask_id is None else shape.mask_id
@@ -101,7 +124,8 @@ class DeviceModel:
                                     shape.n_kv_heads, shape.head_dim, shape.d_ffn, shape.vocab,
                                     mask_id, shape.rms_eps, shape.rope_theta, self.inv_tau,
                                     dlm.DLM_BF16 if shape.dtype == "bf16" else dlm.DLM_F32)
-        load = dlm.load_weights_mx if packed else dlm.load_weights
+        load = (dlm.load_weights_qint if int8 else dlm.load_weights_mx if packed
+                else dlm.load_weights)
         self.handle = load(self.config, self.weights)
 
     def close(self):

@@ -131,3 +131,108 @@ def test_binding_refuses_host_tensors_and_shapes():
             dlm.qint_linear(q, w, y, epilogue, residual=res)
     with pytest.raises(ValueError):
         dlm.make_qint(torch.zeros(8, 128, dtype=torch.int8), f(8), 8, 64)
+
+
+# ------------------------------------------------------------------ workspace
+def test_workspace_is_checked():
+    """A product whose K is split: no workspace, an unaligned one, a small one."""
+    L, x, w = dlm.lib(), _q(40, 18944), _q(3584, 18944)
+    assert dlm.debug_qint_linear_plan(40, 3584, 18944)[1] > 1
+    need = dlm.qint_linear_workspace(40, w)
+    assert need == 40 * 3584 * 4 * dlm.debug_qint_linear_plan(40, 3584, 18944)[1]
+    b = ctypes.byref
+    call = lambda ws, size: L.dlm_qint_linear(b(x), b(w), 0, None, 0, 0, FAKE, 3584, ws, size, None)
+    assert call(None, need) == E and call(FAKE + 128, need) == E
+    assert call(FAKE, need - 1) == dlm.DLM_ESIZE
+    assert dlm.qint_linear_workspace(0, w) == 0
+
+
+def test_plans_are_sound():
+    """Plans over a wide range: slices that are not empty and that the scratch holds, tiles that
+    the epilogue can run; the hook refuses what the call does."""
+    import random
+    rng = random.Random(3)
+    size = lambda lo, hi: int(lo * (hi / lo) ** rng.random())
+    for _ in range(5000):
+        m, n, k, e = size(1, 600000) % 524288 + 1, 2 * size(1, 60000), size(1, ref.MAX_K), rng.randrange(3)
+        if n * ref.row_bytes(k) > 1 << 33:
+            continue
+        cfg, slices, sub, group = dlm.debug_qint_linear_plan(m, n, k, e, rng.choice([8, 80, 256, 304]))
+        tiles = ref.row_bytes(k) // 128
+        assert 1 <= slices <= max(1, tiles)
+        if cfg >= 0:
+            per = -(-tiles // slices)
+            assert -(-tiles // per) == slices                 # none of them empty
+            bm, bn, flags = dlm.debug_gemm_info(cfg)
+            assert sub == 0 or (flags & sub and slices * sub > 0)
+            assert slices > 1 or e != dlm.DLM_QINT_SWIGLU or not flags & 8
+            # the tiles' 32-bit offsets: rows beyond them are taken in turn, unsplit
+            assert slices == 1 or m * ref.row_bytes(k) // 2 < 1 << 32
+        else:
+            assert m <= 16
+    for bad in [(0, 8, 8, 0), (1, 0, 8, 0), (1, 8, 0, 0), (1, 7, 8, 2), (1, 8, 8, 3), (1 << 20, 8, 8, 0)]:
+        with pytest.raises(dlm.DlmError):
+            dlm.debug_qint_linear_plan(*bad)
+    with pytest.raises(dlm.DlmError):
+        dlm.debug_qint_linear_plan(1, 8, 8, 0, 0)
+    assert dlm.lib().dlm_debug_qint_linear_plan(1, 8, 8, 0, 256, None) == E
+
+
+# ----------------------------------------------------------------------- models
+def _cfg(**kw):
+    c = dict(n_layers=2, d_model=256, n_q_heads=4, n_kv_heads=2, head_dim=64, d_ffn=688, vocab=2048,
+             mask_id=2047, rms_eps=1e-5, rope_theta=1e4, inv_tau=10.0, dtype=dlm.DLM_BF16)
+    c.update(kw)
+    return dlm.DlmConfig(**c)
+
+
+def _weights(**kw):
+    shapes = dict(w_qkv=(512, 256), w_o=(256, 256), w_gate_up=(1376, 256), w_down=(256, 688))
+    shapes.update(kw)
+    mk = lambda name: _q(*shapes[name])
+    arr = (dlm.DlmLayerQint * 2)(*[dlm.DlmLayerQint(FAKE, mk("w_qkv"), mk("w_o"), FAKE, mk("w_gate_up"),
+                                                    mk("w_down")) for _ in range(2)])
+    w = dlm.DlmWeightsQint(FAKE, FAKE, FAKE, arr)
+    w._keep = arr
+    return w
+
+
+def test_load_model():
+    m = dlm.load_weights_qint(_cfg(), _weights())
+    assert dlm.workspace_bytes(m, 64, 2) > 0
+    assert dlm.kv_cache_alloc_mx(m, 2, 64)[1] > 0 and dlm.kv_cache_alloc(m, 2, 64)[1] > 0
+    dlm.model_destroy(m)
+
+
+@pytest.mark.parametrize("name,shape", [("w_qkv", (511, 256)), ("w_o", (256, 255)), ("w_gate_up", (688, 256)),
+                                        ("w_down", (256, 704)), ("w_o", (0, 256))])
+def test_load_refuses_other_shapes(name, shape):
+    with pytest.raises(dlm.DlmError) as e:
+        dlm.load_weights_qint(_cfg(), _weights(**{name: shape}))
+    assert e.value.status == E and name in str(e.value)
+
+
+def test_load_refuses_what_is_missing_or_unsupported():
+    for field in ("codes", "scales"):
+        w = _weights()
+        setattr(w.layers[1].w_o, field, None)
+        with pytest.raises(dlm.DlmError) as e:
+            dlm.load_weights_qint(_cfg(), w)
+        assert "layer 1: w_o" in str(e.value)
+    w = _weights()
+    w.layers[0].ffn_norm = None
+    with pytest.raises(dlm.DlmError):
+        dlm.load_weights_qint(_cfg(), w)
+    with pytest.raises(dlm.DlmError):
+        dlm.load_weights_qint(_cfg(rms_eps=0.0), _weights())
+    big = dict(w_gate_up=(2 * 131072, 256), w_down=(256, 131072))
+    with pytest.raises(dlm.DlmError) as e:
+        dlm.load_weights_qint(_cfg(d_ffn=131072), _weights(**big))
+    assert e.value.status == BIG and "w_down" in str(e.value)
+    assert dlm.lib().dlm_load_weights_qint(None, None, None) == E
+
+
+def test_engine_refuses_both_kinds():
+    from paper_2606_29094_amd import engine
+    with pytest.raises(ValueError):
+        engine.DeviceModel(engine.ModelShape(1, 64, 1, 1, 64, 64, 64, "bf16"), {}, 1.0, packed=True, int8=True)
