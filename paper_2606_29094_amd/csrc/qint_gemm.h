@@ -23,22 +23,6 @@ __device__ __forceinline__ i32x4 mfma16_i8(const u32x4& a, const u32x4& b, const
                                                c, 0, 0, 0);
 }
 
-// acc sx sw in fp32, off by at most three roundings: the token's scale first, except where that
-// could leave fp32's range on the way (|acc| < 2^31) though the result does not. Scales that
-// packing writes are 2^-126 at least, so nothing falls below the normal numbers on the way. FAST:
-// the rows' scales are known to be kQintWide at most.
-constexpr float kQintWide = 0x1p96f;
-template <bool FAST = false>
-__device__ __forceinline__ float qint_value(int acc, float sx, float sw) {
-  if constexpr (FAST) return (float)acc * sx * sw;
-  const bool wide = sx > kQintWide;
-  return (float)acc * (wide ? sw : sx) * (wide ? sx : sw);
-}
-// (rounded by itself whatever the kernel: no fused multiply-add)
-__device__ __forceinline__ float qint_add(float res, float p) {
-#pragma clang fp contract(off)
-  return res + p;
-}
 // (the reciprocal by the hardware's instruction, within 1 ulp)
 __device__ __forceinline__ float qint_silu_mul(float g, float u) {
   return g * __builtin_amdgcn_rcpf(1.f + __expf(-g)) * u;
@@ -457,6 +441,7 @@ hipError_t qint_matmul(const QintPlan& plan, const QintView& x, const QintView& 
   const bool vec = n_out % 4 == 0 && o.ldy % 4 == 0 && reinterpret_cast<uintptr_t>(o.y) % (4 * es) == 0 &&
                    (o.mode != DLM_QINT_ADD || (o.ldr % 4 == 0 && reinterpret_cast<uintptr_t>(o.res) % 16 == 0));
   auto join = [&](const int32_t* slices) {
+    if (!plan.join) return hipSuccess;
     const int rows = std::min(o.m, 65535);
     if (vec)
       DLM_LAUNCH((qint_join_kernel<4>), dim3(ceil_div(n_out, 1024), rows), dim3(256), 0, st, slices, plan.slices, o);
@@ -477,7 +462,7 @@ hipError_t qint_matmul(const QintPlan& plan, const QintView& x, const QintView& 
       if (swiglu) return launch(EpiQintSwiGLU{}, ceil_div(o.n, 32) * 32);
       return o.mode == DLM_QINT_ADD ? launch(EpiQint<true>{}, o.n) : launch(EpiQint<false>{}, o.n);
     }
-    const LaunchSpan span(true);
+    const LaunchSpan span(plan.join);
     EpiQintSlices e{};
     e.o = o, e.slices = reinterpret_cast<int32_t*>(scratch);
     const hipError_t err = gemm_dl_launch<EpiQintSlices>(g.cfg, a, units, b, units, o.m, o.n, units, g.splits,
@@ -486,7 +471,7 @@ hipError_t qint_matmul(const QintPlan& plan, const QintView& x, const QintView& 
     span.last();
     return join(e.slices);
   }
-  const LaunchSpan span(plan.slices > 1);
+  const LaunchSpan span(plan.slices > 1 && plan.join);
   int32_t* const slices = plan.slices > 1 ? reinterpret_cast<int32_t*>(scratch) : nullptr;
   const int per_slice = ceil_div(ceil_div(row_bytes, kQintWalk), plan.slices) * kQintWalk;
   const dim3 grid(ceil_div(n_out, 16), ceil_div(o.m, 16), plan.slices);

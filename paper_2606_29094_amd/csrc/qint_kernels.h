@@ -18,8 +18,26 @@ hipError_t qint_pack(const T* x, long ldx, const QintView& o, hipStream_t st);
 template <typename T>
 hipError_t qint_unpack(const QintView& x, T* out, long ldo, hipStream_t st);
 
+// acc sx sw in fp32, off by at most three roundings: the token's scale first, except where that
+// could leave fp32's range on the way (|acc| < 2^31) though the result does not. Scales that
+// packing writes are 2^-126 at least, so nothing falls below the normal numbers on the way. FAST:
+// the rows' scales are known to be kQintWide at most.
+constexpr float kQintWide = 0x1p96f;
+template <bool FAST = false>
+__device__ __forceinline__ float qint_value(int acc, float sx, float sw) {
+  if constexpr (FAST) return (float)acc * sx * sw;
+  const bool wide = sx > kQintWide;
+  return (float)acc * (wide ? sw : sx) * (wide ? sx : sw);
+}
+// (rounded by itself whatever the kernel: no fused multiply-add)
+__device__ __forceinline__ float qint_add(float res, float p) {
+#pragma clang fp contract(off)
+  return res + p;
+}
+
 // Rows of fp32 [o.n, o.k]: h + slices 0, 1, .. (T, `splits` of them, stride elements apart, rows
-// lda) goes to h_out (may be h or null), its norm times g in 8 bits to o.
+// lda) goes to h_out (may be h or null), its norm times g in 8 bits to o. T = int32_t: the K slices
+// that a product left unjoined, h + qint_value(their sum, sx, sw) (sx may be o's scales).
 template <typename T>
 struct QintNorm {
   const float* h;
@@ -31,6 +49,8 @@ struct QintNorm {
   long stride, lda;
   const float* g;
   float eps;
+  const float* sx = nullptr;
+  const float* sw = nullptr;
 };
 template <typename T>
 hipError_t qint_norm(const QintNorm<T>& a, const QintView& o, hipStream_t st);
@@ -49,9 +69,10 @@ struct QintOut {
   bool wide;
 };
 // A product's way: (gemm) the GEMM tiles, or blocks of 16 rows and columns straight from memory.
-// slices > 1: as many K slices go to scratch and are added by a second kernel.
+// slices > 1: as many K slices [slices, rows, n] go to scratch and are added by a second kernel, or,
+// without join, left there.
 struct QintPlan {
-  bool gemm = false;
+  bool gemm = false, join = true;
   GemmPlan g{};
   int slices = 1;
   size_t scratch = 0;

@@ -5,6 +5,7 @@
 #include <float.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "qint_kernels.h"
 
@@ -42,7 +43,7 @@ __device__ __forceinline__ double wave_max64(double v) {
   return v;
 }
 
-template <typename T> struct Vec16 { typedef T type __attribute__((ext_vector_type(16 / sizeof(T)))); };
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 
 // elements [at, at + V) of a row of k, zeros behind it. VEC: whole vectors of V elements.
 template <int V, bool VEC, typename T>
@@ -172,7 +173,31 @@ __global__ __launch_bounds__(1024) void qint_norm_kernel(QintNorm<T> a, QintView
     auto load = [&](int at0) {
 #pragma unroll
       for (int c = 0; c < C; ++c) load_row<4, VEC>(src, at_of(at0, c), k, v[c]);
-      if constexpr (S > 0) {
+      if constexpr (std::is_same<T, int32_t>::value) {
+        i32x4 sum[C];
+        float w[C][4];
+#pragma unroll
+        for (int c = 0; c < C; ++c) sum[c] = i32x4{0, 0, 0, 0}, load_row<4, VEC>(a.sw, at_of(at0, c), k, w[c]);
+#pragma unroll 2
+        for (int s = 0; s < a.splits; ++s)
+#pragma unroll
+          for (int c = 0; c < C; ++c) {
+            const int at = at_of(at0, c);
+            const int32_t* const p = part + s * a.stride + at;
+            if constexpr (VEC) {
+              if (at < k) sum[c] += *reinterpret_cast<const i32x4*>(p);
+            } else {
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (at + i < k) sum[c][i] += p[i];
+            }
+          }
+        const float x = a.sx[row];
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[c][i] = qint_add(v[c][i], qint_value(sum[c][i], x, w[c][i]));
+      } else if constexpr (S > 0) {
         float p[S][C][4];
 #pragma unroll
         for (int s = 0; s < S; ++s)
@@ -243,6 +268,7 @@ __global__ __launch_bounds__(1024) void qint_norm_kernel(QintNorm<T> a, QintView
     const float scale = (float)fmax(tmax * inv / 127.0, kQintMinScale);
     bad = !(scale <= FLT_MAX) || !(ss <= DBL_MAX);
     const double r = fmin(127.0 / tmax, inv / kQintMinScale);
+    // (a.sx may be these scales: every lane has read its row's by the exchange above)
     if (threadIdx.x == 0) o.scales[row] = bad ? __uint_as_float(0x7fc00000u) : scale;
     int8_t* const codes = o.codes + row * row_bytes;
     for (int at0 = 0; at0 < (LOOP ? row_bytes : 1); at0 += step) {
@@ -317,7 +343,8 @@ hipError_t qint_norm(const QintNorm<T>& a, const QintView& o, hipStream_t st) {
   const int quads = qint_row(o.k) / 4, blocks = std::min(o.n, kQintBlocks);
   const bool vec = vector_rows(a.h, a.ldh, o.k, 4) && vector_rows(a.g, 4, o.k, 4) &&
                    (!a.h_out || vector_rows(a.h_out, a.ldo, o.k, 4)) &&
-                   (a.splits == 0 || (vector_rows(a.add, a.lda, o.k, 4) && a.stride % 4 == 0));
+                   (a.splits == 0 || (vector_rows(a.add, a.lda, o.k, 4) && a.stride % 4 == 0)) &&
+                   (!a.sw || vector_rows(a.sw, 4, o.k, 4));
 #define NORM(S_, VEC_, C_, LOOP_)                                                                  \
   DLM_LAUNCH((qint_norm_kernel<T, S_, VEC_, C_, LOOP_>), dim3(blocks), dim3(qint_threads(quads, C_)), 0, \
              st, a, o)
@@ -332,10 +359,14 @@ hipError_t qint_norm(const QintNorm<T>& a, const QintView& o, hipStream_t st) {
   if (!vec) {
     if (quads > 4096) NORM(-1, false, 4, true);
     else NORM(-1, false, 4, false);
-  } else if (a.splits == 0) NORM_C(0);
-  else if (a.splits == 1) NORM_C(1);
-  else if (a.splits == 2) NORM_C(2);
-  else NORM_C(-1);
+  } else if constexpr (std::is_same<T, int32_t>::value) {
+    NORM_C(-1);
+  } else {
+    if (a.splits == 0) NORM_C(0);
+    else if (a.splits == 1) NORM_C(1);
+    else if (a.splits == 2) NORM_C(2);
+    else NORM_C(-1);
+  }
 #undef NORM_C
 #undef NORM
   return hipGetLastError();
@@ -348,5 +379,6 @@ hipError_t qint_norm(const QintNorm<T>& a, const QintView& o, hipStream_t st) {
 INST(bf16)
 INST(float)
 #undef INST
+template hipError_t qint_norm<int32_t>(const QintNorm<int32_t>&, const QintView&, hipStream_t);
 
 }  // namespace dlm

@@ -226,7 +226,8 @@ Layout layout(const dlm_model* m, int n, int n_req) {
     L.i_o = qint_plan(n, c.d_model, qd, false, m->num_cu);
     L.i_gu = qint_plan(n, 2 * c.d_ffn, c.d_model, true, m->num_cu);
     L.i_down = qint_plan(n, c.d_model, c.d_ffn, false, m->num_cu);
-    L.s_qkv = 1;                                  // (products join their own K slices)
+    // (the norm behind a residual projection adds its K slices; the other products join theirs)
+    L.s_qkv = 1;
   } else if (m->mx.empty()) {
     L.g_qkv = projection_plan(es_i, n, qkv_dim, c.d_model, m->num_cu);
     L.g_o = projection_plan(es_i, n, c.d_model, qd, m->num_cu);
@@ -261,7 +262,9 @@ Layout layout(const dlm_model* m, int n, int n_req) {
   L.cs = take((size_t)n * (c.head_dim / 2) * 8);
   L.q = take((size_t)n * qd * es);
   L.ao = take((size_t)n * qd * es);
-  L.part = take((size_t)std::max(L.s_o, L.s_down) * n * c.d_model * 4);
+  // (8-bit projections: scratch of their products)
+  L.part = take(std::max({(size_t)std::max(L.s_o, L.s_down) * n * c.d_model * 4, L.i_qkv.scratch, L.i_o.scratch,
+                          L.i_gu.scratch, L.i_down.scratch}));
   L.act = take((size_t)n * c.d_ffn * es);
   L.lm_rows = take((size_t)std::max(L.m_max, 1) * 4);
   L.lm_count = take(4);
@@ -273,8 +276,7 @@ Layout layout(const dlm_model* m, int n, int n_req) {
   L.pi = take((size_t)L.tiles * std::max(L.m_max, 1) * 4);
   L.conf = take((size_t)std::max(L.m_max, 1) * 4);
   L.tok = take((size_t)std::max(L.m_max, 1) * 4);
-  L.mx = take(std::max({L.q_qkv.scratch, L.q_o.scratch, L.q_gu.scratch, L.q_down.scratch, L.i_qkv.scratch,
-                        L.i_o.scratch, L.i_gu.scratch, L.i_down.scratch}));
+  L.mx = take(std::max({L.q_qkv.scratch, L.q_o.scratch, L.q_gu.scratch, L.q_down.scratch}));
   if (!m->qint.empty()) {    // the packed inputs of one projection at a time
     L.codes = take((size_t)n * qint_row(std::max({c.d_model, qd, c.d_ffn})));
     L.scales = take((size_t)n * sizeof(float));
@@ -444,7 +446,21 @@ dlm_status run_forward(dlm_model* m, dlm_cache* c, const dlm_batch* b, const Ste
     QintOut o{};
     o.y = y, o.ldy = ldy, o.res = mode == DLM_QINT_ADD ? reinterpret_cast<float*>(y) : nullptr, o.ldr = ldy;
     o.mode = mode, o.wide = wide;
-    return qint_matmul(plan, packed(w.k), QintView{w.codes, w.scales, w.n, w.k}, o, mxs, st);
+    return qint_matmul(plan, packed(w.k), QintView{w.codes, w.scales, w.n, w.k}, o, part, st);
+  };
+  // a projection into the residual stream, then the norm that follows (none: the step's last)
+  const auto residual8 = [&](const char* name, QintPlan plan, const dlm_qint& w, const float* gain) -> dlm_status {
+    plan.join = plan.slices == 1 || !gain;
+    LAUNCH(m, st, name, product8(plan, w, DLM_QINT_ADD, h, d, true));
+    if (!gain) return DLM_OK;
+    if (plan.join) {
+      LAUNCH(m, st, "rmsnorm", norm8(gain));
+    } else {
+      const QintNorm<int32_t> a{h, d, h, d, reinterpret_cast<const int32_t*>(part), plan.slices, (long)n * d, d, gain,
+                                cf.rms_eps, packed(d).scales, w.scales};
+      LAUNCH(m, st, "residual_rmsnorm", qint_norm<int32_t>(a, packed(d), st));
+    }
+    return DLM_OK;
   };
 
   LAUNCH(m, st, "embed_norm", embed_norm_rows<T>(p, reinterpret_cast<const T*>(m->embed), d, cf.vocab,
@@ -459,7 +475,7 @@ dlm_status run_forward(dlm_model* m, dlm_cache* c, const dlm_batch* b, const Ste
     T* kc = c->mx ? nullptr : reinterpret_cast<T*>(c->k_layer(l));
     T* vc = c->mx ? nullptr : reinterpret_cast<T*>(c->v_layer(l));
     const dlm_trace* t = tr && tr->layer == l ? tr : nullptr;
-    if (w8) LAUNCH(m, st, "rmsnorm", norm8(w.attn_norm));
+    if (w8 && l == 0) LAUNCH(m, st, "rmsnorm", norm8(w.attn_norm));
     if (t) {
       if (w8 && t->a_attn) HIPCHECK(qint_unpack<T>(packed(d), a, d, st));
       TRACE_COPY(t->h_in, h, (size_t)n * d * 4);
@@ -493,8 +509,8 @@ dlm_status run_forward(dlm_model* m, dlm_cache* c, const dlm_batch* b, const Ste
     // O projection; its residual update is fused into the FFN norm when K is split
     if (w8) {
       LAUNCH(m, st, "pack_attention", qint_pack<T>(ao, qd, packed(qd), st));
-      LAUNCH(m, st, "gemm_o", product8(L.i_o, w8l->w_o, DLM_QINT_ADD, h, d, true));
-      LAUNCH(m, st, "rmsnorm", norm8(w.ffn_norm));
+      const dlm_status s = residual8("gemm_o", L.i_o, w8l->w_o, w.ffn_norm);
+      if (s != DLM_OK) return s;
     } else if (L.s_o == 1) {
       if (w4)
         LAUNCH(m, st, "gemm_o", mx_matmul<T>(L.q_o, ao, qd, n, mx_view(w4l->w_o), qd, DLM_MX_ADD, h, d,
@@ -533,7 +549,8 @@ dlm_status run_forward(dlm_model* m, dlm_cache* c, const dlm_batch* b, const Ste
     T* next_a = l + 1 < cf.n_layers ? a : nullptr;
     if (w8) {
       LAUNCH(m, st, "pack_act", qint_pack<T>(act, cf.d_ffn, packed(cf.d_ffn), st));
-      LAUNCH(m, st, "gemm_down", product8(L.i_down, w8l->w_down, DLM_QINT_ADD, h, d, true));
+      const dlm_status s = residual8("gemm_down", L.i_down, w8l->w_down, next_norm);
+      if (s != DLM_OK) return s;
     } else if (L.s_down == 1) {
       if (w4)
         LAUNCH(m, st, "gemm_down", mx_matmul<T>(L.q_down, act, cf.d_ffn, n, mx_view(w4l->w_down), cf.d_ffn,

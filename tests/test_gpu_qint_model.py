@@ -126,6 +126,40 @@ def test_steps_of_many_rows(gpu):
     eng.close()
 
 
+def test_gains_and_scales_at_any_address(gpu):
+    """Gains and channel scales that start at no multiple of 16 bytes: the same steps."""
+    cfg = dataclasses.replace(GQA_SMALL, d_ffn=4096)
+    first = _model(cfg)
+
+    def moved(t):
+        big = torch.empty(t.numel() + 1, device=t.device)
+        big[1:].copy_(t)
+        return big[1:]
+
+    def moved_scales(q):
+        codes, scales = q._keep
+        q2 = dlm.DlmQint(codes.data_ptr(), 0, q.n, q.k)
+        q2._keep = (codes, moved(scales))
+        q2.scales = q2._keep[1].data_ptr()
+        return q2
+
+    layers = []
+    for l in first.tensors["layers"]:
+        l = {k: moved_scales(v) if isinstance(v, dlm.DlmQint) else v for k, v in l.items()}
+        layers.append(dict(l, ffn_norm=moved(l["ffn_norm"])))
+    second = engine.DeviceModel(first.shape, dict(first.tensors, layers=layers), 10.0, int8=True)
+    assert dlm.debug_qint_linear_plan(96, cfg.d_model, cfg.d_ffn)[1] > 1      # (slices for the norm)
+    outs = []
+    for model in (first, second):
+        eng, reqs = _start(cfg, model, "dual")
+        for _ in range(3):
+            eng.step(reqs)
+        outs.append(eng.read_outputs(3))
+        eng.close()
+    for k in ("n", "block_conf", "block_tok"):
+        assert np.array_equal(outs[0][k], outs[1][k]), k
+
+
 @pytest.mark.parametrize("packed_kv", [False, True])
 def test_generation_runs_and_repeats(gpu, packed_kv):
     """Whole generations: every position is unmasked, and a second run gives the same tokens."""
@@ -176,7 +210,9 @@ def test_step_profile(gpu, name):
         eng.step([r for r in reqs if not r.done])
     dlm.profile_enable(model.handle, False)
     prof = dlm.profile_read(model.handle)
-    for kind, each in (("rmsnorm", 2), ("gemm_qkv", 1), ("rope_kv_write", 1), ("attention", 1),
+    norms = [prof.get(kind, (0, 0, 0))[0] for kind in ("rmsnorm", "residual_rmsnorm")]
+    assert sum(norms) == 2 * 2 * cfg.n_layers          # (the second adds a product's K slices)
+    for kind, each in (("gemm_qkv", 1), ("rope_kv_write", 1), ("attention", 1),
                        ("pack_attention", 1), ("gemm_o", 1), ("gemm_gate_up_swiglu", 1), ("pack_act", 1),
                        ("gemm_down", 1)):
         calls, ms, seen = prof[kind]
