@@ -481,8 +481,9 @@ dlm_status dlm_qint_norm(const float* h, int64_t ldh, float* h_out, int64_t ldo,
  *   DLM_QINT_SWIGLU  y [x.n, w.n / 2] = silu(p[:, f]) * p[:, w.n / 2 + f] (rows [0, n / 2) of w are
  *                  the gate weights; n even)
  * y's rows are ldy elements apart; y must not overlap x or w. residual is not used by the others.
- * w holds 2^33 bytes of codes at most. Workspace: as in dlm_mx_linear, for the same m_rows (x.n),
- * w and epilogue. A row's result depends on that row alone, bit for bit. */
+ * w holds less than 2^33 bytes of codes (DLM_EUNSUPPORTED; w.n counted in whole 32 rows), x any
+ * number of up to DLM_MAX_REQ * DLM_MAX_SEQ rows. Workspace: as in dlm_mx_linear, for the same
+ * m_rows (x.n), w and epilogue. A row's result depends on that row and w alone, bit for bit. */
 typedef enum { DLM_QINT_STORE = 0, DLM_QINT_ADD = 1, DLM_QINT_SWIGLU = 2 } dlm_qint_epilogue;
 dlm_status dlm_qint_linear_workspace(int32_t m_rows, const dlm_qint* w, int32_t epilogue,
                                    size_t* out_bytes);

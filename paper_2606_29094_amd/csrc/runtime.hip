@@ -723,8 +723,9 @@ QintView qint_view(const dlm_qint& q) { return {q.codes, q.scales, q.n, q.k}; }
 dlm_status check_qint_linear(int32_t m_rows, const dlm_qint* w, int32_t epilogue) {
   dlm_status s = check_qint(w, -1, false, "w");
   if (s != DLM_OK) return s;
-  if ((size_t)w->n * qint_row(w->k) > (size_t)1 << 33)
-    return fail(DLM_EUNSUPPORTED, "w: 8-bit matrix of %d x %d: more than 2^33 bytes", w->n, w->k);
+  // (the tiles address w by 32-bit offsets of 2-byte units, gate/up columns in blocks of 32)
+  if (align_up(w->n, 32) * qint_row(w->k) >= (size_t)1 << 33)
+    return fail(DLM_EUNSUPPORTED, "w: 8-bit matrix of %d x %d: 2^33 bytes or more", w->n, w->k);
   if (m_rows < 0 || m_rows > DLM_MAX_REQ * DLM_MAX_SEQ)
     return fail(DLM_EINVAL, "%d rows outside [0, %d]", m_rows, DLM_MAX_REQ * DLM_MAX_SEQ);
   if (epilogue < DLM_QINT_STORE || epilogue > DLM_QINT_SWIGLU) return fail(DLM_EINVAL, "epilogue %d", epilogue);

@@ -78,7 +78,8 @@ class DlmWeightsMx(ctypes.Structure):
 
 
 class DlmQint(ctypes.Structure):
-    _keep = ()              # the tensors of make_qint
+    _keep = ()              # the tensors of make_qint, and the device they are on
+    _device = None
     _fields_ = [("codes", c_void_p), ("scales", c_void_p), ("n", c_int32), ("k", c_int32)]
 
 
@@ -410,14 +411,17 @@ def debug_gemm(cfg: int, epilogue: int, a, b, c, sub: int = 0, n_tail: int = 0,
 
 
 # ------------------------------------------------- 4-bit operands
+_dtype_ids = {}
+
+
 def _dtype_id(dtype) -> int:
     """dlm_dtype of a torch floating type."""
-    import torch
-    if dtype == torch.bfloat16:
-        return DLM_BF16
-    if dtype == torch.float32:
-        return DLM_F32
-    raise ValueError(f"{dtype}: bfloat16 or float32 expected")
+    if not _dtype_ids:
+        import torch
+        _dtype_ids.update({torch.bfloat16: DLM_BF16, torch.float32: DLM_F32})
+    if dtype not in _dtype_ids:
+        raise ValueError(f"{dtype}: bfloat16 or float32 expected")
+    return _dtype_ids[dtype]
 
 
 def _rows_of(name, t, shape, dtype=None):
@@ -442,17 +446,28 @@ def _flat(name, t, shape, dtype):
         raise ValueError(f"{name} is not contiguous")
 
 
-def _on(stream, *tensors, cache=None):
-    """The stream argument of a call on these tensors (and on a cache in a tensor's memory),
-    which have to be on the current device: the given one, or that device's current stream."""
-    import torch
-    dev = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else -2
+_current = None      # (device, stream) lookups of the initialised runtime
+
+
+def _on(stream, *tensors, cache=None, matrices=()):
+    """The stream argument of a call on these tensors (on a cache in a tensor's memory, on 8-bit
+    matrices), which have to be on the current device: the given one, or that device's current
+    stream."""
+    global _current
+    if _current is None:
+        import torch
+        if torch.cuda.is_initialized():
+            _current = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+    dev = _current[0]() if _current is not None else -2
     for t in tensors:
         if t.get_device() != dev:
             raise ValueError(f"a tensor is on {t.device}, not on the current GPU")
+    for q in matrices:
+        if q._device != dev:
+            raise ValueError(f"an 8-bit matrix is on cuda:{q._device}, not on the current GPU")
     if cache is not None and cache.device not in (None, dev):
         raise ValueError(f"the cache is on cuda:{cache.device}, not on the current GPU")
-    return stream if stream is not None else torch._C._cuda_getCurrentRawStream(dev)
+    return stream if stream is not None else _current[1](dev)
 
 
 def _scratch(workspace):
@@ -644,7 +659,7 @@ def make_qint(codes, scales, n: int, k: int) -> DlmQint:
     if codes.device != scales.device:
         raise ValueError(f"codes on {codes.device}, scales on {scales.device}")
     q = DlmQint(codes.data_ptr(), scales.data_ptr(), n, k)
-    q._keep = (codes, scales)
+    q._keep, q._device = (codes, scales), codes.get_device()
     return q
 
 
@@ -652,14 +667,14 @@ def qint_pack(x, q: DlmQint, stream=None):
     """Pack the rows of x [n, k] (bf16 or fp32, contiguous rows) into q's buffers."""
     ld = _rows_of("x", x, (q.n, q.k))
     check(lib().dlm_qint_pack(_dtype_id(x.dtype), x.data_ptr(), ld, ctypes.byref(q),
-                            _on(stream, x, *q._keep)))
+                              _on(stream, x, matrices=(q,))))
 
 
 def qint_unpack(q: DlmQint, out, stream=None):
     """The values of q, in out's dtype."""
     ld = _rows_of("out", out, (q.n, q.k))
     check(lib().dlm_qint_unpack(ctypes.byref(q), _dtype_id(out.dtype), out.data_ptr(), ld,
-                              _on(stream, out, *q._keep)))
+                                _on(stream, out, matrices=(q,))))
 
 
 def qint_norm(h, gain, eps: float, q: DlmQint, add=None, h_out=None, stream=None):
@@ -690,7 +705,7 @@ def qint_norm(h, gain, eps: float, q: DlmQint, add=None, h_out=None, stream=None
         ldo, out = (ldh if h_out is h else _rows_of("h_out", h_out, shape, f32)), h_out.data_ptr()
         tensors.append(h_out)
     check(lib().dlm_qint_norm(h.data_ptr(), ldh, out, ldo, dt, part, splits, stride, ldadd,
-                              gain.data_ptr(), eps, ctypes.byref(q), _on(stream, *tensors, *q._keep)))
+                              gain.data_ptr(), eps, ctypes.byref(q), _on(stream, *tensors, matrices=(q,))))
 
 
 def qint_linear_workspace(m_rows: int, w: DlmQint, epilogue: int = DLM_QINT_STORE) -> int:
@@ -704,7 +719,7 @@ def qint_linear(x: DlmQint, w: DlmQint, y, epilogue: int = DLM_QINT_STORE, works
     """y = x @ w.T (in y's dtype), residual + x @ w.T (fp32; residual may be y), or silu(gate) *
     up in y's dtype; workspace: at least qint_linear_workspace bytes, or None where that is 0."""
     n_out = w.n // 2 if epilogue == DLM_QINT_SWIGLU else w.n
-    ldy, tensors = _rows_of("y", y, (x.n, n_out)), [y, *x._keep, *w._keep]
+    ldy, tensors = _rows_of("y", y, (x.n, n_out)), [y]
     r, ldr, ws, size = None, 0, None, 0
     if epilogue == DLM_QINT_ADD:
         if residual is None:
@@ -717,7 +732,8 @@ def qint_linear(x: DlmQint, w: DlmQint, y, epilogue: int = DLM_QINT_STORE, works
         ws, size = _scratch(workspace)
         tensors.append(workspace)
     check(lib().dlm_qint_linear(ctypes.byref(x), ctypes.byref(w), epilogue, r, ldr,
-                              _dtype_id(y.dtype), y.data_ptr(), ldy, ws, size, _on(stream, *tensors)))
+                              _dtype_id(y.dtype), y.data_ptr(), ldy, ws, size,
+                              _on(stream, *tensors, matrices=(x, w))))
 
 
 def load_weights_qint(cfg: DlmConfig, weights: DlmWeightsQint) -> c_void_p:

@@ -139,7 +139,7 @@ def test_gains_and_scales_at_any_address(gpu):
     def moved_scales(q):
         codes, scales = q._keep
         q2 = dlm.DlmQint(codes.data_ptr(), 0, q.n, q.k)
-        q2._keep = (codes, moved(scales))
+        q2._keep, q2._device = (codes, moved(scales)), q._device
         q2.scales = q2._keep[1].data_ptr()
         return q2
 

@@ -88,6 +88,9 @@ def _linear(L, x=None, w=None, epilogue=0, res=FAKE, ldr=64, dtype=0, y=FAKE, ld
     (lambda L: _linear(L, dtype=7), E), (lambda L: _linear(L, y=None), E), (lambda L: _linear(L, ldy=63), E),
     (lambda L: _linear(L, x=_q(4, codes=FAKE + 1)), E), (lambda L: _linear(L, w=_q(codes=None)), E),
     (lambda L: _linear(L, x=_q(4, 131000), w=_q(70000, 131000), ldy=70000), BIG),
+    (lambda L: _linear(L, x=_q(4, 131000), w=_q(65505, 131000), ldy=70000), BIG),      # 65536 in whole 32s
+    (lambda L: L.dlm_qint_linear_workspace(4, _q(65505, 131000), 0, None), BIG),
+    (lambda L: L.dlm_qint_linear_workspace(4, _q(65504, 131000), 0, None), E),         # (no place for the size)
     (lambda L: _linear(L, x=_q(4, 1 << 20), w=_q(64, 1 << 20)), BIG),
 ])
 def test_calls_refused(call, status):
