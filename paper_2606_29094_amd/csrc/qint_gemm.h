@@ -144,9 +144,10 @@ struct EpiQintBase {
     return !__any(wide);
   }
   // A wave's accumulators go through LDS, kRows rows at a time, so that a lane finishes four adjacent
-  // columns of a row and a row's stores are whole lines. The rows of a time are finished in
-  // rounds of PER quads a lane, body(round, r0, r, q): row r0 + r of the wave's, quad q of QUADS, at buf + r
-  // stride. Only the writes to LDS name accumulators, so only they are unrolled over them.
+  // columns of a row and a row's stores are whole lines. Those rows are finished in rounds of PER
+  // quads a lane, body(round, r0, place): place(t, r, q) gives the lane's t-th one, row r0 + r of
+  // the wave's, quad q of QUADS, at buf + r kStride. Only the writes to LDS name accumulators, so
+  // only they are unrolled over them.
   template <int FN> static constexpr int kStride = FN * 16 + 4;
   template <int FM> static constexpr int kRows = FM % 2 == 0 ? 32 : 16;
   template <int QUADS, int PER, int FM, int FN, class Body>

@@ -68,9 +68,10 @@ def silu_mul(g, u):
 def swiglu(p, bound):
     """(y, bound) of gate and up halves: the products' bounds through silu(g) u (|silu'| <= 1.1,
     |silu(g)| <= |g|), and of the fp32 steps: the exponential's argument |g| u, itself and the sum,
-    the quotient and the product 8 u. It overflows below -88, where silu is less than 2^-120."""
+    the quotient and the product 8 u. Below -87.3 the quotient is a subnormal number or the
+    exponential overflows, and silu may become zero: it is less than 2^-119 there."""
     g, u = p.chunk(2, 1)
     tg, tu = bound.chunk(2, 1)
     y = silu_mul(g, u)
     return y, (1.1 * tg * (u.abs() + tu) + g.abs() * tu + (g.abs() + 8) * U * y.abs() +
-               2.0 ** -120 * (u.abs() + tu))
+               2.0 ** -119 * (u.abs() + tu))
