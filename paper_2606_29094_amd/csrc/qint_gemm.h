@@ -398,11 +398,12 @@ QintPlan qint_plan(int rows, int n, int k, bool swiglu, int num_cu) {
     const GemmPlan g = gemm_plan(2, rows, n, units, true, num_cu, false, true, true, kFewRows, false, true, &us);
     if (g.splits > 1 && us < best) best = us, p.g = g;
   }
-  // Several row tiles: in groups of 8, so that an XCD's blocks share weight columns as well as rows
-  // (37888 x 3584 SwiGLU at 2048 rows 270 -> 249 us, at 4096 512 -> 496; 3584 x 18944 at 4096 240 ->
-  // 229; smaller matrices by less than 2 %).
-  int bm, bn, threads;
-  if (gemm_dl_tile(p.g.cfg, &bm, &bn, &threads) && p.g.splits == 1 && ceil_div(rows, bm) >= 4) p.g.group_m = 8;
+  // Weights that fill half of the 256 MB last-level cache, or many rows: row tiles in groups of 8, so
+  // that an XCD's blocks share weight columns as well as rows. Plain order / groups, us: 37888 x 3584
+  // SwiGLU at 1500 rows 205 / 188, 4096 503 / 477, 10240 1243 / 1183; 4096 x 12288 at 10240 494 / 474;
+  // 3584 x 18944 at 4096 237 / 236, 10240 648 / 639. Fewer rows of smaller ones: 24576 x 4096 at 4096
+  // 340 / 342, 12288 x 4096 174 / 180, 4096 x 4096 at 1000 rows 23 / 27.
+  if (((double)n * units > 64e6 || rows >= 8192) && p.g.splits == 1) p.g.group_m = 8;
   p.slices = p.g.splits;
   if (rows <= kQintFewRows) {
     const int blocks = ceil_div(swiglu ? n / 2 : n, 16), walks = ceil_div(units * 2, kQintWalk);

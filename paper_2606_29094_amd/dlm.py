@@ -680,10 +680,9 @@ def qint_unpack(q: DlmQint, out, stream=None):
 def qint_norm(h, gain, eps: float, q: DlmQint, add=None, h_out=None, stream=None):
     """h' = h + add (fp32 [n, k]; add [n, k] or slices [splits, n, k], bf16 or fp32), stored to
     h_out or, where there is an add and no h_out, to h; its RMS norm times gain, packed into q."""
-    f32 = gain.dtype
-    if str(f32) != "torch.float32":
+    shape, f32 = (q.n, q.k), gain.dtype
+    if _dtype_id(f32) != DLM_F32:
         raise ValueError(f"gain is {f32}, expected torch.float32")
-    shape = (q.n, q.k)
     ldh = _rows_of("h", h, shape, f32)
     _flat("gain", gain, (q.k,), f32)
     splits, stride, ldadd, dt, part = 0, 0, 0, DLM_F32, None

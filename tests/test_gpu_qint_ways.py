@@ -75,6 +75,14 @@ def test_way(gpu, m, n, k, epilogue, way):
             _check_linear(gpu, m, n, k, name, dtype, pad=pad, seed=m)
 
 
+@pytest.mark.parametrize("m,n,k", [(8200, 520, 300), (8193, 1030, 140), (12345, 94, 257)])
+@pytest.mark.parametrize("epilogue", ["store", "add", "swiglu"])
+def test_tiles_in_groups(gpu, m, n, k, epilogue):
+    """Row tiles in groups of eight, the last group smaller, whole tiles and sub-tiles."""
+    assert dlm.debug_qint_linear_plan(m, n, k, dlm.QINT_EPILOGUES[epilogue])[3] == 8
+    _check_linear(gpu, m, n, k, epilogue, F32, seed=m)
+
+
 def test_ways_are_all_there():
     """Every configuration that the planner takes over a wide range of sizes is tested above."""
     import random
