@@ -426,6 +426,8 @@ def _dtype_id(dtype) -> int:
 
 def _rows_of(name, t, shape, dtype=None):
     """Row stride of a 2-d device tensor of the given shape (and dtype) with contiguous rows."""
+    if t.shape == shape and (dtype is None or t.dtype == dtype) and t.is_contiguous():
+        return shape[1]
     if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     if dtype is not None and t.dtype != dtype:
@@ -440,6 +442,8 @@ def _rows_of(name, t, shape, dtype=None):
 
 
 def _flat(name, t, shape, dtype):
+    if t.shape == shape and t.dtype == dtype and t.is_contiguous():
+        return
     if t.shape != shape or t.dtype != dtype:
         raise ValueError(f"{name} is {t.dtype} {tuple(t.shape)}, expected {dtype} {tuple(shape)}")
     if not t.is_contiguous():
@@ -686,10 +690,8 @@ def qint_norm(h, gain, eps: float, q: DlmQint, add=None, h_out=None, stream=None
     ldh = _rows_of("h", h, shape, f32)
     _flat("gain", gain, (q.k,), f32)
     splits, stride, ldadd, dt, part = 0, 0, 0, DLM_F32, None
-    if add is None:
-        tensors = [h, gain]
-    else:
-        dt, tensors = _dtype_id(add.dtype), [h, gain, add]
+    if add is not None:
+        dt = _dtype_id(add.dtype)
         if add.dim() == 2:
             splits, ldadd = 1, _rows_of("add", add, shape)
         elif add.shape[0]:
@@ -702,9 +704,9 @@ def qint_norm(h, gain, eps: float, q: DlmQint, add=None, h_out=None, stream=None
     ldo, out = 0, None
     if h_out is not None:
         ldo, out = (ldh if h_out is h else _rows_of("h_out", h_out, shape, f32)), h_out.data_ptr()
-        tensors.append(h_out)
+    st = _on(stream, h, gain, h if add is None else add, h if h_out is None else h_out, matrices=(q,))
     check(lib().dlm_qint_norm(h.data_ptr(), ldh, out, ldo, dt, part, splits, stride, ldadd,
-                              gain.data_ptr(), eps, ctypes.byref(q), _on(stream, *tensors, matrices=(q,))))
+                              gain.data_ptr(), eps, ctypes.byref(q), st))
 
 
 def qint_linear_workspace(m_rows: int, w: DlmQint, epilogue: int = DLM_QINT_STORE) -> int:
