@@ -53,7 +53,7 @@ __device__ __forceinline__ void dl_tile(char* smem, const bf16* __restrict__ A, 
                                         int rot, const Epi& epi) {
   typedef typename MulOf<Epi>::type Mul;
   static_assert(RB == 64 || RB == 128, "k-tile row bytes");
-  static_assert(SA >= 2 && SA <= 4 && SB >= SA && SB <= 4, "A and B stages");
+  static_assert(SA >= 2 && SA <= 8 && SB >= SA && SB <= 8, "A and B stages");
   static_assert(MF == 16 || MF == 32, "MFMA tile");
   constexpr int DA = SA - 1, DB = SB - 1;  // prefetch distances (k-tiles ahead)
   constexpr int NW = WAVES_M * WAVES_N;
@@ -89,9 +89,9 @@ __device__ __forceinline__ void dl_tile(char* smem, const bf16* __restrict__ A, 
   // (column tile mod k-tiles), so that the blocks in flight read different
   // column offsets of their weight rows at any moment and spread over the HBM
   // channels (MHA vocab head with 32 rows: 4.5 -> 5.9 TB/s); the others walk K
-  // from the start. Only the four-stage tiles take rot: deciding it at run
+  // from the start. Only tiles of four stages and more take rot: deciding it at run
   // time costs the large launches of the other tiles 1-2 %.
-  const int krot = (Epi::kRotateK || (SA == 4 && rot)) && nkt > 0 ? tn % nkt : 0;
+  const int krot = (Epi::kRotateK || (SA >= 4 && rot)) && nkt > 0 ? tn % nkt : 0;
   auto ktile = [&](int kt) { const int k = kt + krot; return k >= nkt ? k - nkt : k; };
 
   // LDS chunk slot of global chunk c in row r: c ^ swz(r). With 16x16x32
@@ -716,7 +716,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void gemm_dl_head_kernel(
 // 24576x4096 51.0 -> 35.3 us (5.7 TB/s), QKV 22.9 -> 20.0, down 4096x12288
 // 22.5 -> 20.1; at 136 rows gate/up 37888x3584 72.6 -> 57.3 us, down
 // 3584x18944 45.9 -> 39.0; at 384 rows gate/up 24576x4096 79.2 -> 65.9 us
-// (192x192 split-phase).
+// (192x192 split-phase). 94, with seven k-tiles ahead, is planned for 8-bit integers alone.
 #define DL_CONFIGS(X)                      \
   X(1, 128, 128, 2, 2, 2, 2, 128, 16, 0)   \
   X(6, 256, 256, 2, 4, 2, 3, 128, 16, 1)   \
@@ -741,7 +741,8 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void gemm_dl_head_kernel(
   X(89, 160, 128, 2, 4, 4, 4, 128, 16, 0)  \
   X(90, 160, 160, 2, 5, 4, 4, 128, 16, 0)  \
   X(92, 192, 128, 4, 2, 3, 3, 128, 16, 1)  \
-  X(93, 192, 192, 4, 2, 3, 3, 128, 16, 1)
+  X(93, 192, 192, 4, 2, 3, 3, 128, 16, 1)  \
+  X(94, 32, 32, 2, 2, 8, 8, 128, 16, 0)
 
 // The configurations lm_head_plan chooses from (16x16 MFMA, an even number of column
 // fragments, many rounds); the head's and the logits' epilogues exist for these only.

@@ -5,6 +5,7 @@
 #pragma once
 
 #include <algorithm>
+#include <cmath>
 
 #include "../../include/dlm.h"
 #include "qint_kernels.h"
@@ -377,11 +378,11 @@ __global__ __launch_bounds__(256) void qint_join_kernel(const int32_t* __restric
 // Way of a product. The GEMM tiles' times are those of bf16 operands of as many bytes (gemm_plan;
 // the matrix cores take the same time over them), K slices by a join of their own. Up to 16 rows
 // also blocks that read memory directly (qint_few_kernel), us on MI355X with the weights from HBM:
-// 3.4 + the weights at 5.6 TB/s (less while blocks leave CUs idle) + x, once for each column tile, at
+// 3.4 + the weights at 5.6 TB/s (less where CUs have unequal shares) + x, once for each column tile, at
 // 11 TB/s out of the L2s, and for K slices 2 + 0.8 a MB of them. Direct / tiles: one row of 4096 x
 // 4096 6.4 / 8.3, 3584 x 18944 15.5 / 18.1, 24576 x 4096 SwiGLU 21.6 / 21.3; 16 rows 8.0 / 8.9, 22.4 /
 // 18.6, 26.0 / 21.6.
-constexpr int kQintFewRows = 16;
+constexpr int kQintFewRows = 16, kQintSmallTile = 94;
 
 // Rows that the tiles can address (32-bit offsets of 2-byte units); more are taken in turn.
 static int qint_near_rows(int units) { return (int)std::min<long>(((1L << 32) / units - 1) & ~255L, 1 << 30); }
@@ -404,13 +405,27 @@ QintPlan qint_plan(int rows, int n, int k, bool swiglu, int num_cu) {
   // 3584 x 18944 at 4096 237 / 236, 10240 648 / 639. Fewer rows of smaller ones: 24576 x 4096 at 4096
   // 340 / 342, 12288 x 4096 174 / 180, 4096 x 4096 at 1000 rows 23 / 27.
   if (((double)n * units > 64e6 || rows >= 8192) && p.g.splits == 1) p.g.group_m = 8;
+  // Small products: tiles of 32 x 32 with eight stages, 3.45 + 0.1875 for each k-tile where every CU
+  // has a block, 15 % more where it has two, beside the stream. The other tiles / these, us: 2048 x
+  // 2048 at 64 rows 8.7 / 6.3, 3584 x 3584 10.9 / 8.8, 4608 x 3584 11.3 / 9.6, 4096 x 4096 at 128 rows
+  // 12.7 / 10.8, 689 x 1031 6.7 / 5.4, 256 x 688 5.0 / 4.0; long walks and many tiles are the others':
+  // 4096 x 12288 at 64 rows 17.4 / 22.4, 12288 x 4096 15.9 / 22.6, 4608 x 3584 at 128 rows 12.4 / 15.9. (The
+  // models of both are off by up to a tenth, which the others keep.)
+  if (!swiglu) {
+    const long tiles = (long)ceil_div(rows, 32) * ceil_div(n, 32), full = tiles / (2 * num_cu), rem = tiles - full * 2 * num_cu;
+    const double rounds = 1.15 * full + (rem > num_cu ? 1.15 : rem ? 1.0 : 0.0);
+    const double walk = units / 64 * 0.1875 * rounds, stream = (double)n * units * 2e-6 / 7.1;
+    const double t = 3.45 + (double)rows * n * 4e-6 / 6.46 + std::sqrt(walk * walk + stream * stream);
+    if (t < 0.9 * best) best = t, p.g = GemmPlan{kQintSmallTile, 1, 0};
+  }
   p.slices = p.g.splits;
   if (rows <= kQintFewRows) {
     const int blocks = ceil_div(swiglu ? n / 2 : n, 16), walks = ceil_div(units * 2, kQintWalk);
     const double mb = (double)n * units * 2e-6, x_mb = (double)rows * units * 2e-6 * blocks;
     for (int s = 1; s <= 16 && s <= walks; s *= 2) {
       if (ceil_div(walks, ceil_div(walks, s)) != s) continue;     // (none of them empty)
-      double t = 3.4 + mb * std::max(1.0, 0.875 * num_cu / ((double)blocks * s)) / 5.6 + x_mb / 11;
+      const double shares = (double)blocks * s / num_cu;
+      double t = 3.4 + mb * std::max(1.0, 0.875 * std::ceil(shares) / shares) / 5.6 + x_mb / 11;
       if (s > 1) t += 2 + 0.8 * s * rows * (double)n * 4e-6;
       if (t < best) best = t, p.gemm = false, p.slices = s;
     }

@@ -23,37 +23,38 @@ WAYS = [
     (227, 34644, 1, STORE, (21, 1, 0)), (604, 14650, 1, ADD, (21, 1, 0)), (985, 16782, 2, ADD, (21, 1, 2)),
     (4102, 146, 4620, STORE, (21, 4, 2)), (2060, 162, 8934, ADD, (21, 8, 2)),
     (4677, 168, 4029, SWIGLU, (21, 4, 2)), (1025, 2, 1, STORE, (22, 1, 0)), (1031, 2, 1, ADD, (22, 1, 0)),
-    (1063, 2, 1, SWIGLU, (22, 1, 0)), (645, 2, 1, SWIGLU, (29, 1, 4)), (647, 2, 1, ADD, (29, 1, 4)),
-    (651, 2, 1, STORE, (29, 1, 4)), (837, 2140, 1, SWIGLU, (29, 1, 2)), (197, 22092, 1, STORE, (29, 1, 0)),
-    (646, 2, 2123, SWIGLU, (29, 2, 4)), (682, 2, 2071, ADD, (29, 2, 4)), (702, 4, 1963, STORE, (29, 2, 4)),
+    (1063, 2, 1, SWIGLU, (22, 1, 0)), (645, 2, 1, SWIGLU, (29, 1, 4)), (582, 2578, 1, STORE, (29, 1, 4)),
+    (835, 1832, 1, ADD, (29, 1, 4)), (837, 2140, 1, SWIGLU, (29, 1, 2)),
+    (197, 22092, 1, STORE, (29, 1, 0)), (646, 2, 2123, SWIGLU, (29, 2, 4)),
+    (656, 2, 4193, ADD, (29, 4, 4)), (681, 2, 3983, STORE, (29, 4, 4)),
     (4255, 2, 4000, SWIGLU, (29, 4, 2)), (4142, 4, 8090, ADD, (29, 8, 0)),
     (2727, 644, 1922, SWIGLU, (42, 1, 2)), (1197, 1644, 1938, ADD, (42, 1, 2)),
-    (1289, 1574, 1922, STORE, (42, 1, 2)), (2056, 136, 4091, ADD, (42, 4, 2)),
-    (2154, 148, 4644, STORE, (42, 4, 2)), (1242, 154, 8644, SWIGLU, (42, 8, 2)),
+    (1289, 1574, 1922, STORE, (42, 1, 2)), (1218, 148, 8221, ADD, (42, 8, 2)),
+    (1164, 156, 8492, STORE, (42, 8, 2)), (1242, 154, 8644, SWIGLU, (42, 8, 2)),
     (591, 16488, 1, ADD, (70, 1, 0)), (417, 24662, 1, STORE, (70, 1, 0)),
-    (4340, 216, 18224, ADD, (70, 8, 0)), (17, 2, 1, STORE, (80, 1, 0)), (17, 2, 1, ADD, (80, 1, 0)),
-    (17, 2, 1, SWIGLU, (80, 1, 0)), (17, 2, 2436, ADD, (80, 2, 0)), (17, 2, 2469, SWIGLU, (80, 2, 0)),
-    (19, 2, 2634, STORE, (80, 2, 0)), (132, 5474, 1, SWIGLU, (81, 1, 0)), (200, 4202, 1, ADD, (81, 1, 0)),
-    (259, 3426, 1, STORE, (81, 1, 0)), (76, 2092, 4051, ADD, (81, 4, 0)),
-    (132, 1540, 4091, SWIGLU, (81, 4, 0)), (270, 930, 4297, STORE, (81, 4, 0)),
-    (17, 33958, 1, SWIGLU, (83, 1, 0)), (44, 32782, 2, STORE, (83, 1, 0)), (26, 33274, 6, ADD, (83, 1, 0)),
-    (14, 8368, 7794, ADD, (83, 4, 0)), (12, 4368, 20078, STORE, (83, 8, 0)),
-    (26, 8246, 8666, SWIGLU, (83, 4, 0)), (322, 4274, 1, STORE, (84, 1, 0)),
-    (326, 4206, 1, SWIGLU, (84, 1, 0)), (400, 3462, 1, ADD, (84, 1, 0)),
-    (395, 416, 8165, SWIGLU, (84, 8, 0)), (356, 1042, 4162, STORE, (84, 4, 0)),
-    (138, 2766, 4397, ADD, (84, 4, 0)), (24, 27394, 1, STORE, (85, 1, 0)),
+    (4340, 216, 18224, ADD, (70, 8, 0)), (17, 2, 1, SWIGLU, (80, 1, 0)),
+    (165, 4266, 135, STORE, (80, 1, 0)), (141, 5274, 144, ADD, (80, 1, 0)),
+    (17, 2, 2469, SWIGLU, (80, 2, 0)), (17, 2, 3071, STORE, (80, 2, 0)), (18, 2, 3206, ADD, (80, 2, 0)),
+    (132, 5474, 1, SWIGLU, (81, 1, 0)), (260, 4646, 1, ADD, (81, 1, 0)), (300, 4298, 1, STORE, (81, 1, 0)),
+    (76, 2092, 4051, ADD, (81, 4, 0)), (132, 1540, 4091, SWIGLU, (81, 4, 0)),
+    (11, 4098, 5119, STORE, (81, 4, 0)), (17, 33958, 1, SWIGLU, (83, 1, 0)),
+    (44, 32782, 2, STORE, (83, 1, 0)), (44, 33040, 76, ADD, (83, 1, 0)), (2, 8250, 6122, ADD, (83, 4, 0)),
+    (5, 8686, 7125, SWIGLU, (83, 4, 0)), (7, 9902, 7036, STORE, (83, 4, 0)),
+    (326, 4206, 1, SWIGLU, (84, 1, 0)), (390, 3988, 1, STORE, (84, 1, 0)), (429, 3708, 1, ADD, (84, 1, 0)),
+    (395, 416, 8165, SWIGLU, (84, 8, 0)), (409, 394, 9439, STORE, (84, 8, 0)),
+    (138, 2766, 4397, ADD, (84, 4, 0)), (100, 14248, 1, STORE, (85, 1, 0)),
     (104, 13454, 1, SWIGLU, (85, 1, 0)), (97, 14806, 1, ADD, (85, 1, 0)),
-    (203, 2188, 4232, SWIGLU, (85, 4, 0)), (209, 2192, 4137, STORE, (85, 4, 0)),
-    (205, 2402, 4232, ADD, (85, 4, 0)), (133, 18086, 1, SWIGLU, (86, 1, 0)),
+    (203, 2188, 4232, SWIGLU, (85, 4, 0)), (205, 2402, 4232, ADD, (85, 4, 0)),
+    (208, 2462, 4254, STORE, (85, 4, 0)), (133, 18086, 1, SWIGLU, (86, 1, 0)),
     (129, 19130, 1, ADD, (86, 1, 0)), (77, 33530, 1, STORE, (86, 1, 0)),
     (129, 4598, 9627, STORE, (86, 4, 0)), (527, 1580, 1, SWIGLU, (87, 1, 2)),
-    (551, 1556, 1, ADD, (87, 1, 2)), (429, 2142, 1, STORE, (87, 1, 2)), (514, 3268, 1, STORE, (87, 1, 0)),
+    (514, 3268, 1, STORE, (87, 1, 0)), (518, 3752, 1, ADD, (87, 1, 0)),
     (528, 4, 18065, STORE, (87, 16, 2)), (539, 8, 17446, ADD, (87, 16, 2)),
     (637, 2, 19324, SWIGLU, (87, 16, 2)), (623, 782, 4057, SWIGLU, (87, 4, 0)),
-    (321, 2, 1, SWIGLU, (88, 1, 4)), (325, 2, 1, STORE, (88, 1, 4)), (329, 2, 1, ADD, (88, 1, 4)),
-    (520, 2778, 1, SWIGLU, (88, 1, 2)), (516, 5410, 1, ADD, (88, 1, 0)),
-    (325, 2, 2166, SWIGLU, (88, 2, 4)), (325, 2, 2198, STORE, (88, 2, 4)), (356, 2, 1973, ADD, (88, 2, 4)),
-    (529, 650, 4042, STORE, (88, 4, 2)), (536, 664, 11237, ADD, (88, 8, 0)),
+    (321, 2, 1, SWIGLU, (88, 1, 4)), (520, 2778, 1, SWIGLU, (88, 1, 2)), (554, 2852, 1, STORE, (88, 1, 2)),
+    (618, 3048, 1, ADD, (88, 1, 2)), (516, 5410, 1, ADD, (88, 1, 0)), (325, 2, 2166, SWIGLU, (88, 2, 4)),
+    (334, 2, 4028, ADD, (88, 4, 4)), (339, 2, 4206, STORE, (88, 4, 4)),
+    (523, 684, 5037, STORE, (88, 4, 2)), (536, 664, 11237, ADD, (88, 8, 0)),
     (781, 4136, 1, SWIGLU, (89, 1, 0)), (794, 4198, 1, ADD, (89, 1, 0)), (386, 9550, 1, STORE, (89, 1, 0)),
     (546, 1624, 4227, STORE, (89, 4, 0)), (642, 1370, 4863, SWIGLU, (89, 4, 0)),
     (751, 1466, 4507, ADD, (89, 4, 0)), (257, 16510, 1, SWIGLU, (90, 1, 0)),
@@ -63,7 +64,9 @@ WAYS = [
     (662, 774, 8271, STORE, (92, 8, 0)), (858, 580, 8505, SWIGLU, (92, 8, 0)),
     (818, 582, 8957, ADD, (92, 8, 0)), (332, 18022, 1, STORE, (93, 1, 0)),
     (245, 24290, 1, ADD, (93, 1, 0)), (277, 22242, 1, SWIGLU, (93, 1, 0)),
-    (789, 1064, 12201, SWIGLU, (93, 8, 0))]
+    (789, 1064, 12201, SWIGLU, (93, 8, 0)), (17, 2, 1, STORE, (94, 1, 0)), (17, 2, 1, ADD, (94, 1, 0)),
+    (64, 2048, 2048, STORE, (94, 1, 0)), (128, 4096, 1100, ADD, (94, 1, 0)),
+    (70, 689, 1031, STORE, (94, 1, 0)), (33, 4600, 3000, ADD, (94, 1, 0))]
 
 
 @pytest.mark.parametrize("m,n,k,epilogue,way", WAYS)
