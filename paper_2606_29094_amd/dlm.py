@@ -720,21 +720,20 @@ def qint_linear(x: DlmQint, w: DlmQint, y, epilogue: int = DLM_QINT_STORE, works
     """y = x @ w.T (in y's dtype), residual + x @ w.T (fp32; residual may be y), or silu(gate) *
     up in y's dtype; workspace: at least qint_linear_workspace bytes, or None where that is 0."""
     n_out = w.n // 2 if epilogue == DLM_QINT_SWIGLU else w.n
-    ldy, tensors = _rows_of("y", y, (x.n, n_out)), [y]
+    shape = (x.n, n_out)
+    ldy = _rows_of("y", y, shape)
     r, ldr, ws, size = None, 0, None, 0
     if epilogue == DLM_QINT_ADD:
         if residual is None:
             raise ValueError("the add epilogue takes a residual")
-        r, ldr = residual.data_ptr(), _rows_of("residual", residual, (x.n, n_out))
+        r, ldr = residual.data_ptr(), _rows_of("residual", residual, shape)
         if _dtype_id(residual.dtype) != DLM_F32:
             raise ValueError(f"residual is {residual.dtype}, expected torch.float32")
-        tensors.append(residual)
     if workspace is not None:
         ws, size = _scratch(workspace)
-        tensors.append(workspace)
+    st = _on(stream, y, y if r is None else residual, y if workspace is None else workspace, matrices=(x, w))
     check(lib().dlm_qint_linear(ctypes.byref(x), ctypes.byref(w), epilogue, r, ldr,
-                              _dtype_id(y.dtype), y.data_ptr(), ldy, ws, size,
-                              _on(stream, *tensors, matrices=(x, w))))
+                                _dtype_id(y.dtype), y.data_ptr(), ldy, ws, size, st))
 
 
 def load_weights_qint(cfg: DlmConfig, weights: DlmWeightsQint) -> c_void_p:
