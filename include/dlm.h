@@ -434,9 +434,10 @@ dlm_status dlm_mx_kv_attention(const dlm_cache* c, int32_t layer, int32_t n_req,
  * Format. A matrix [n, k] holds a signed byte (its code) for every value and one fp32
  * scale for every row (a token of an activation, an output channel of a weight matrix): the value
  * is code * scale. Packing takes A = the row's largest magnitude, the scale max(A / 127, 2^-126)
- * rounded to fp32, and for each x the integer nearest to x min(127 / A, 2^126) (ties to the even
- * one; decided in 64 bits, so either neighbour where x lies within 2^-40 of a step of the middle).
- * A row that holds an infinity or a NaN gets the scale NaN and zero codes.
+ * rounded to fp32, and for each x the integer nearest to x min(127 / A, 2^126), ties to the even
+ * one: that of the exact quotient. (Of the norm below, whose values have more than 24 bits, either
+ * neighbour where the quotient lies within 2^-40 of the middle of two; exact middles go to the even
+ * one.) A row that holds an infinity or a NaN gets the scale NaN and zero codes.
  * Products of two such matrices are sums of whole numbers in 32 bits, exact and independent of
  * their order: k is DLM_QINT_MAX_K at most (DLM_EUNSUPPORTED beyond, in every call). */
 enum { DLM_QINT_ROW = 128, DLM_QINT_MAX_K = 131071 };
