@@ -384,17 +384,19 @@ __global__ __launch_bounds__(256) void qint_join_kernel(const int32_t* __restric
 // 18.6, 26.0 / 21.6.
 constexpr int kQintFewRows = 16, kQintSmallTile = 94;
 
-// Rows that the tiles can address (32-bit offsets of 2-byte units); more are taken in turn.
+// Rows that the tiles can address (32-bit offsets of 2-byte units); more are taken in turn, all by
+// one plan: whole tiles over whole K, whose last round has no sub-tiles (their number is that of one
+// launch's tiles; 65280 rows and more are many rounds).
 static int qint_near_rows(int units) { return (int)std::min<long>(((1L << 32) / units - 1) & ~255L, 1 << 30); }
 
 QintPlan qint_plan(int rows, int n, int k, bool swiglu, int num_cu) {
   QintPlan p;
   if (rows <= 0) return p;
   const int units = qint_row(k) / 2, cols = swiglu ? ceil_div(n, 32) * 32 : n;   // 2-byte units of a row
-  const bool split = !swiglu && rows <= qint_near_rows(units);
+  const bool near = rows <= qint_near_rows(units), split = !swiglu && near;
   double us, best;
   p.gemm = true;
-  p.g = gemm_plan(2, rows, cols, units, split, num_cu, false, true, !swiglu, kFewRows, false, split, &best);
+  p.g = gemm_plan(2, rows, cols, units, split, num_cu, false, near, !swiglu, kFewRows, false, split, &best);
   if (swiglu && (long)rows * cols < 64 * 64 * (long)num_cu) {     // (the smallest tiles leave CUs idle)
     const GemmPlan g = gemm_plan(2, rows, n, units, true, num_cu, false, true, true, kFewRows, false, true, &us);
     if (g.splits > 1 && us < best) best = us, p.g = g;
