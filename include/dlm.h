@@ -550,6 +550,10 @@ dlm_status dlm_debug_gemm(int32_t cfg, int32_t epilogue, int32_t sub, int32_t n_
 dlm_status dlm_debug_gemm_plan(int32_t elem_bytes, int32_t M, int32_t N, int32_t K, int32_t kind,
                                int32_t num_cu, int32_t out[4]);
 
+/* Test hook (host only): bytes of scratch that the attention of a step of rows recomputed rows of
+ * n_req requests has for the partial results of key splits. */
+dlm_status dlm_debug_attention_scratch(const dlm_model* m, int32_t rows, int32_t n_req, size_t* out_bytes);
+
 /* Test hook for the attention dispatch (host only): the kernel (0 shared tiles,
  * 1 shared tiles in blocks of four waves, 2 to 4 one query head per block with 32
  * query rows and four key groups, 64 and two, 32 and two) and the number of key

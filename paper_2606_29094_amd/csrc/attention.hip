@@ -827,6 +827,14 @@ static hipError_t attention_dh(const StepPlan& p, const bf16* q, const bf16* kc,
 //    four key groups where the 256-key turns are full (32 heads, 256 rows over 256
 //    8.1 / 9.1; 200 over 200 10.9 / 10.8), else 64 rows and two (512 rows 14.7,
 //    shared 17.6); then shared tiles (600 rows 21.7 / 32.5, 1024 34.3 / 44.7).
+// (a request's blocks are rounded up, so fewest of them where all rows are one request's)
+size_t attention_scratch_most(int rows, int hq, int hkv, int dh, size_t elem, int num_cu) {
+  if (elem != 2 || hkv < 1 || hq % hkv != 0 || rows < 1) return 0;
+  const long blocks = (long)hkv * shared_blocks(rows, hq / hkv, kSharedWaves);
+  const long s = std::min((long)kMaxSplits, (num_cu + num_cu / 8) / blocks);
+  return s > 1 ? (size_t)s * rows * hq * (dh * sizeof(float) + sizeof(float2)) : 0;
+}
+
 AttnPlan attention_plan(const StepPlan& p, int hq, int hkv, int dh, size_t elem,
                         size_t scratch_bytes, int num_cu) {
   if (elem != 2 || hkv < 1 || hq % hkv != 0 || p.n_rows < 1) return AttnPlan{};

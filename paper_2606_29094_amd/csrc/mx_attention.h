@@ -563,6 +563,15 @@ size_t mx_attention_scratch(int rows, int hq, int dh, int splits) {
   return (size_t)splits * rows * hq * (dh * sizeof(float) + sizeof(float2));
 }
 
+size_t mx_attention_scratch_most(int rows, int hq, int hkv, int dh, size_t elem, int num_cu) {
+  if (hkv < 1 || hq % hkv != 0 || rows < 1) return 0;
+  // (the blocks of the largest kind, all rows one request's: the fewest there may be)
+  const long items = elem == 2 ? 128 : 16, blocks = hkv * (((long)rows * (hq / hkv) + items - 1) / items);
+  int s = 1;
+  while (s < kMxSplits && blocks * s * 2 <= num_cu) s *= 2;
+  return mx_attention_scratch(rows, hq, dh, s);
+}
+
 // Kernel and key splits. Times in us on MI355X (256 CUs), head_dim 128: 6.5, and for each
 // 64-key tile that a block walks 0.555, 1.3 or 2.03 (32 items whose four waves split the
 // keys, 64 and 128 items that share them) while every CU has one block, or 0.48, 1.04 or

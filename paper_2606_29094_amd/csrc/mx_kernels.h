@@ -91,6 +91,9 @@ struct MxAttnPlan { int kind = kMxAttnFew; int splits = 1; };
 MxAttnPlan mx_attention_plan(const StepPlan& p, int hq, int hkv, int dh, size_t elem,
                              size_t scratch_bytes, int num_cu);
 size_t mx_attention_scratch(int rows, int hq, int dh, int splits);
+// the same of any plan for so many rows, at most; and of the attention over other caches (attention.hip)
+size_t mx_attention_scratch_most(int rows, int hq, int hkv, int dh, size_t elem, int num_cu);
+size_t attention_scratch_most(int rows, int hq, int hkv, int dh, size_t elem, int num_cu);
 template <typename T>
 hipError_t mx_attention(const StepPlan& p, const T* q, const MxKv& kv, int hq, int hkv, int dh,
                         T* out, MxAttnPlan plan, float* scratch, hipStream_t st);

@@ -262,9 +262,16 @@ Layout layout(const dlm_model* m, int n, int n_req) {
   L.cs = take((size_t)n * (c.head_dim / 2) * 8);
   L.q = take((size_t)n * qd * es);
   L.ao = take((size_t)n * qd * es);
-  // (8-bit projections: scratch of their products)
+  // (8-bit projections: scratch of their products, and with the activations, which come later,
+  // room for every key split that their attention may plan: the other models' slices leave it)
+  size_t splits = 0;
+  if (!m->qint.empty()) {
+    splits = std::max(attention_scratch_most(n, c.n_q_heads, c.n_kv_heads, c.head_dim, es, m->num_cu),
+                      mx_attention_scratch_most(n, c.n_q_heads, c.n_kv_heads, c.head_dim, es, m->num_cu));
+    splits -= std::min(splits, (size_t)n * c.d_ffn * es);
+  }
   L.part = take(std::max({(size_t)std::max(L.s_o, L.s_down) * n * c.d_model * 4, L.i_qkv.scratch, L.i_o.scratch,
-                          L.i_gu.scratch, L.i_down.scratch}));
+                          L.i_gu.scratch, L.i_down.scratch, splits}));
   L.act = take((size_t)n * c.d_ffn * es);
   L.lm_rows = take((size_t)std::max(L.m_max, 1) * 4);
   L.lm_count = take(4);
@@ -1160,6 +1167,15 @@ dlm_status dlm_debug_gemm_plan(int32_t elem_bytes, int32_t M, int32_t N, int32_t
   out[1] = p.splits;
   out[2] = p.sub;
   out[3] = p.n_tail;
+  return DLM_OK;
+}
+
+dlm_status dlm_debug_attention_scratch(const dlm_model* m, int32_t rows, int32_t n_req, size_t* out_bytes) {
+  g_err.clear();
+  if (!m || !out_bytes) return fail(DLM_EINVAL, "NULL argument");
+  if (rows < 1 || n_req < 1 || n_req > kMaxReq) return fail(DLM_EINVAL, "%d rows, %d requests", rows, n_req);
+  const Layout L = layout(m, rows, n_req);
+  *out_bytes = L.lm_rows - L.part;
   return DLM_OK;
 }
 

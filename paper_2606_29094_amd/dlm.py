@@ -33,7 +33,7 @@ EXPORTS = ["dlm_load_weights", "dlm_model_destroy", "dlm_workspace_bytes",
            "dlm_kv_cache_alloc", "dlm_cache_destroy", "dlm_cache_invalidate",
            "dlm_denoise_step", "dlm_denoise_step_noalloc", "dlm_cache_refresh",
            "dlm_debug_logits", "dlm_debug_trace", "dlm_debug_gemm_info", "dlm_debug_gemm",
-           "dlm_debug_gemm_plan", "dlm_debug_attention_plan",
+           "dlm_debug_gemm_plan", "dlm_debug_attention_plan", "dlm_debug_attention_scratch",
            "dlm_head_confidence", "dlm_profile_enable", "dlm_profile_read",
            "dlm_profile_sample", "dlm_ceiling_mfma", "dlm_ceiling_copy", "dlm_last_error",
            "dlm_mx_bytes", "dlm_mx_pack", "dlm_mx_unpack", "dlm_mx_linear_workspace",
@@ -175,6 +175,7 @@ def lib():
                                      c_void_p]
         L.dlm_debug_gemm_plan.argtypes = [c_int32, c_int32, c_int32, c_int32, c_int32, c_int32,
                                           POINTER(c_int32)]
+        L.dlm_debug_attention_scratch.argtypes = [c_void_p, c_int32, c_int32, POINTER(c_size_t)]
         L.dlm_debug_attention_plan.argtypes = [c_int32, c_int32, c_int32, c_int32,
                                                POINTER(c_int32), POINTER(c_int32), c_size_t,
                                                c_int32, POINTER(c_int32), POINTER(c_int32)]
@@ -226,7 +227,7 @@ def lib():
                      "dlm_cache_refresh",
                      "dlm_debug_logits", "dlm_debug_trace", "dlm_head_confidence",
                      "dlm_debug_gemm_info", "dlm_debug_gemm", "dlm_debug_gemm_plan",
-                     "dlm_debug_attention_plan", "dlm_profile_enable",
+                     "dlm_debug_attention_plan", "dlm_debug_attention_scratch", "dlm_profile_enable",
                      "dlm_profile_read", "dlm_profile_sample", "dlm_mx_bytes", "dlm_mx_pack",
                      "dlm_mx_unpack", "dlm_mx_linear_workspace", "dlm_mx_linear",
                      "dlm_load_weights_mx", "dlm_kv_cache_alloc_mx", "dlm_mx_kv_append",
@@ -389,6 +390,13 @@ def debug_attention_plan(hq: int, hkv: int, dh: int, rows, lens, scratch_bytes: 
                                          scratch_bytes, num_cu, ctypes.byref(kernel),
                                          ctypes.byref(splits)))
     return kernel.value, splits.value
+
+
+def debug_attention_scratch(model, rows: int, n_req: int = 1) -> int:
+    """Bytes that a step's attention has for key splits (dlm_debug_attention_scratch)."""
+    out = c_size_t()
+    check(lib().dlm_debug_attention_scratch(model, rows, n_req, ctypes.byref(out)))
+    return out.value
 
 
 def debug_gemm(cfg: int, epilogue: int, a, b, c, sub: int = 0, n_tail: int = 0,
