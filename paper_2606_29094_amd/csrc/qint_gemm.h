@@ -16,6 +16,7 @@ namespace {
 
 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 typedef int32_t i32x16 __attribute__((ext_vector_type(16)));
+typedef f32x4 f32x4u __attribute__((aligned(4)));      // at a float's alignment
 
 // 16x16x64 int8: lane l supplies A[row = l%16][k = 16*(l/16) .. +15] and B[col = l%16] of the same
 // k; D[row = 4*(l/16) + i][col = l%16] = acc[i].
@@ -212,16 +213,20 @@ struct EpiQint : EpiQintBase {
                                          const float* sw, int32_t* buf, int lane) const {
     constexpr int Q = FN * 4, LAST = FM * 16 * Q / 64 / FN - 1;      // quads of a row; the last round
     f32x4 res[FN], next[FN];
-    auto load = [&](f32x4 (&v)[FN], int round) {       // (rounds go over the wave's rows in order)
+    // (Rounds go over the wave's rows in order. A place beyond the matrix reads the channels' scales,
+    // which nobody writes, instead of a value that another wave may be storing where the residual is
+    // in place: by a choice of the address, since branches here spill the accumulators, 4096 x
+    // 4096 at 4096 rows 83 -> 182 us.)
+    auto load = [&](f32x4 (&v)[FN], int round) {
 #pragma unroll
       for (int t = 0; t < FN; ++t) {
-        const int at = (round * FN + t) * 64 + lane, n = n0 + at % Q * 4;
-        const float* const r = o.res + (long)min(m0 + at / Q, o.m - 1) * o.ldr;
+        const int at = (round * FN + t) * 64 + lane, m = m0 + at / Q, n = n0 + at % Q * 4;
+        const float* const r = o.res + (long)m * o.ldr + n;
         if (vec) {
-          v[t] = *reinterpret_cast<const f32x4*>(r + min(n, o.n - 4));
+          v[t] = *reinterpret_cast<const f32x4u*>(m < o.m && n < o.n ? r : o.sw);
         } else {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) v[t][i] = r[min(n + i, o.n - 1)];
+          for (int i = 0; i < 4; ++i) v[t][i] = *(m < o.m && n + i < o.n ? r + i : o.sw);
         }
       }
     };
