@@ -410,8 +410,12 @@ QintPlan qint_plan(int rows, int n, int k, bool swiglu, int num_cu) {
   // that an XCD's blocks share weight columns as well as rows. Plain order / groups, us: 37888 x 3584
   // SwiGLU at 1500 rows 205 / 188, 4096 503 / 477, 10240 1243 / 1183; 4096 x 12288 at 10240 494 / 474;
   // 3584 x 18944 at 4096 237 / 236, 10240 648 / 639. Fewer rows of smaller ones: 24576 x 4096 at 4096
-  // 340 / 342, 12288 x 4096 174 / 180, 4096 x 4096 at 1000 rows 23 / 27.
-  if (((double)n * units > 64e6 || rows >= 8192) && p.g.splits == 1) p.g.group_m = 8;
+  // 340 / 342, 12288 x 4096 174 / 180, 4096 x 4096 at 1000 rows 23 / 27. One row tile has no rows to
+  // share and keeps the plain order: 37888 x 3584 SwiGLU at 32 rows 26.8 / 27.0, 128 31.5 / 31.8, 256
+  // 44.4 / 44.8 (28672 x 8192 at 32 rows 45.1 / 44.3, 192 63.0 / 63.6).
+  int bm, bn, th;
+  if (((double)n * units > 64e6 || rows >= 8192) && p.g.splits == 1 && gemm_dl_tile(p.g.cfg, &bm, &bn, &th) && rows > bm)
+    p.g.group_m = 8;
   // Small products: tiles of 32 x 32 with eight stages, 3.45 + 0.1875 for each k-tile where every CU
   // has a block, 15 % more where it has two, beside the stream. The other tiles / these, us: 2048 x
   // 2048 at 64 rows 8.7 / 6.3, 3584 x 3584 10.9 / 8.8, 4608 x 3584 11.3 / 9.6, 4096 x 4096 at 128 rows
