@@ -166,7 +166,8 @@ __device__ __forceinline__ float4 load4(const bf16* p, bool vec) {
 // of the rotary table:
 //   h[n] = E[mask ? mask_id : token] (fp32 residual; token ids outside
 //     [0, vocab) are read as [MASK]),
-//   out[n] = rmsnorm(h[n]) * g of the first layer (same sums as rmsnorm_kernel),
+//   out[n] = rmsnorm(h[n]) * g of the first layer (same sums as rmsnorm_kernel; out null: no
+//     norm, for models whose own norm packs what it makes),
 //   cs[n][i] = (cos, sin) of pos(n) * theta^(-2i/head_dim), angle and trig in fp64.
 // Bound by its launch at few rows and by the scattered table rows at many:
 // separate embedding (one value per load and store), table and norm kernels
@@ -203,7 +204,7 @@ __global__ __launch_bounds__(256) void embed_norm_kernel(
   const int id = (mask[ti] || tk < 0 || tk >= vocab) ? mask_id : tk;
   const T* src = E + (long)id * d;
   float* x = h + (long)n * d;
-  T* o = out + (long)n * d;
+  T* o = out ? out + (long)n * d : nullptr;
   float ss = 0.f, inv;
   if (d <= 4096) {                          // the row stays in registers
     float4 v[4];
@@ -220,6 +221,7 @@ __global__ __launch_bounds__(256) void embed_norm_kernel(
         ss += v[c].x * v[c].x + v[c].y * v[c].y + v[c].z * v[c].z + v[c].w * v[c].w;
       }
     }
+    if (!o) return;
     inv = 1.0f / sqrtf(block_sum_256(ss, red) / (float)d + eps);
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
@@ -236,6 +238,7 @@ __global__ __launch_bounds__(256) void embed_norm_kernel(
       *reinterpret_cast<float4*>(x + j) = v;
       ss += v.x * v.x + v.y * v.y + v.z * v.z + v.w * v.w;
     }
+    if (!o) return;
     inv = 1.0f / sqrtf(block_sum_256(ss, red) / (float)d + eps);
     for (int j = threadIdx.x * 4; j < d; j += 1024) {
       const float4 v = load4(src + j, vec);

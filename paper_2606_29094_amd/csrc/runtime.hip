@@ -472,7 +472,7 @@ dlm_status run_forward(dlm_model* m, dlm_cache* c, const dlm_batch* b, const Ste
 
   LAUNCH(m, st, "embed_norm", embed_norm_rows<T>(p, reinterpret_cast<const T*>(m->embed), d, cf.vocab,
                          cf.mask_id, b->tokens, b->mask, m->layers[0].attn_norm, cf.rms_eps, dh,
-                         cf.rope_theta, h, a, cs, st));
+                         cf.rope_theta, h, w8 ? (T*)nullptr : a, cs, st));
   const size_t es = sizeof(T);
   for (int l = 0; l < cf.n_layers; ++l) {
     const dlm_layer_weights& w = m->layers[l];
