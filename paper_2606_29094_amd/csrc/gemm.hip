@@ -409,7 +409,7 @@ int last_round_subs(int subs, long rem, long slots) {
 
 GemmPlan gemm_plan(int es, int M, int N, int K, bool splittable, int num_cu, bool allow_mf32,
                    bool allow_tail, bool allow_odd, int few_rows, bool allow_small, bool join,
-                   double* us) {
+                   double* int8_us) {
   GemmPlan best{-1, 1, 0};
   // (a join takes slices of any number of k-tiles, so every power of two will do)
   const int max_s = join ? 32 : 8;
@@ -450,7 +450,7 @@ GemmPlan gemm_plan(int es, int M, int N, int K, bool splittable, int num_cu, boo
     const FewRowDims* const tiles = few_row_dims();
     for (int i = 0; i < kFewRowCount; ++i) {
       const FewRowDims& c = tiles[i];
-      if (!allow_odd && c.odd) continue;
+      if ((!allow_odd && c.odd) || (int8_us && !gemm_dl_int8(c.cfg))) continue;
       const int n_m = ceil_div(M, c.bm);
       if (c.bm < 192 && n_m > 5) continue;   // (the weights once per row tile)
       const double f = pow2 && !(n_m == 1 && c.stages == 4) ? 1.0 + 0.054 / n_m : 1.0;
@@ -485,7 +485,7 @@ GemmPlan gemm_plan(int es, int M, int N, int K, bool splittable, int num_cu, boo
   }
   for (const RoundTable& c : kRoundTables) {
     if (M <= few_rows) break;
-    if (M > c.max_m) continue;
+    if (M > c.max_m || (int8_us && !gemm_dl_int8(c.cfg))) continue;
     if (!allow_mf32 && gemm_dl_mfma(c.cfg) == 32) continue;
     if (!allow_odd && gemm_dl_odd(c.cfg)) continue;
     int bm, bn, th;
@@ -513,7 +513,7 @@ GemmPlan gemm_plan(int es, int M, int N, int K, bool splittable, int num_cu, boo
       }
     }
   }
-  if (us) *us = best_t;
+  if (int8_us) *int8_us = best_t;
   // weights larger than the last-level cache (256 MB Infinity Cache) stream
   // from HBM once per row tile in plain order: use the grouped XCD order
   int bm, bn, th;

@@ -28,7 +28,8 @@
 namespace dlm {
 
 // The matrix instruction of a tile: a fragment of 16 bytes a lane each, accumulators of 16x16
-// (and 32x32) tiles. An epilogue for other operands than bf16 names its own as Epi::Mul.
+// tiles, and of 32x32 ones where there are such tiles. An epilogue for other operands than bf16
+// names its own as Epi::Mul.
 struct MulBf16 {
   typedef f32x4 Acc16;
   typedef f32x16 Acc32;
@@ -41,6 +42,8 @@ struct MulBf16 {
 };
 template <class Epi, class = void> struct MulOf { typedef MulBf16 type; };
 template <class Epi> struct MulOf<Epi, std::void_t<typename Epi::Mul>> { typedef typename Epi::Mul type; };
+template <class Mul, int MF> struct AccOf { typedef typename Mul::Acc16 type; };
+template <class Mul> struct AccOf<Mul, 32> { typedef typename Mul::Acc32 type; };
 
 // One BM x BN output tile at rows m0.., columns n0.., K range [kbeg, kend),
 // with the block's LDS at smem. tn and tz (column tile, K slice) are passed
@@ -147,7 +150,7 @@ __device__ __forceinline__ void dl_tile(char* smem, const bf16* __restrict__ A, 
   };
 
   // accumulators: 16x16 tiles (4 values per lane) or 32x32 tiles (16 per lane)
-  typedef typename std::conditional<MF == 32, typename Mul::Acc32, typename Mul::Acc16>::type Acc;
+  typedef typename AccOf<Mul, MF>::type Acc;
   Acc acc[FM][FN];
 #pragma unroll
   for (int a = 0; a < FM; ++a)
@@ -716,7 +719,8 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void gemm_dl_head_kernel(
 // 24576x4096 51.0 -> 35.3 us (5.7 TB/s), QKV 22.9 -> 20.0, down 4096x12288
 // 22.5 -> 20.1; at 136 rows gate/up 37888x3584 72.6 -> 57.3 us, down
 // 3584x18944 45.9 -> 39.0; at 384 rows gate/up 24576x4096 79.2 -> 65.9 us
-// (192x192 split-phase). 94, with seven k-tiles ahead, is planned for 8-bit integers alone.
+// (192x192 split-phase). 94, with seven k-tiles ahead, is planned for 8-bit integers alone
+// (in bf16 its plain and residual stores run in the configurations' tests).
 #define DL_CONFIGS(X)                      \
   X(1, 128, 128, 2, 2, 2, 2, 128, 16, 0)   \
   X(6, 256, 256, 2, 4, 2, 3, 128, 16, 1)   \
@@ -751,9 +755,12 @@ constexpr bool head_tile(int cfg) {
          cfg == 42;
 }
 
-// The configurations that are planned with for 8-bit integers (16x16 MFMA; 10 and 11 are the
-// head's alone).
-constexpr bool int8_tile(int cfg) { return cfg != 10 && cfg != 11 && cfg != 62 && cfg != 65; }
+// The configurations that are planned with for 8-bit integers: 16x16 MFMA, not the head's own (1,
+// 10, 11), and not 82, which is never the fastest by the model (none of 1.6 million random plans).
+constexpr bool int8_tile(int cfg) {
+  return cfg != 1 && cfg != 10 && cfg != 11 && cfg != 62 && cfg != 65 && cfg != 82;
+}
+int gemm_dl_int8(int cfg) { return int8_tile(cfg); }
 
 int gemm_dl_tile(int cfg, int* bm, int* bn, int* threads) {
   switch (cfg) {
@@ -854,7 +861,9 @@ hipError_t gemm_dl_launch(int cfg, const bf16* A, int lda, const bf16* B, int ld
         DLM_LAUNCH((gemm_dl_kernel<BM_, BN_, WM_, WN_, SA_, S_, RB_, MF_, SP_, false, Epi>),   \
                    dim3(n_n, n_m, splits), dim3(WM_ * WN_ * 64), 0, st, A, lda, B, ldb, M, \
                    N, K, kps, n_n, n_m, group_m, 0, 0, rot, e);                               \
-      } else if constexpr (Epi::kTailSplit) {                                            \
+      } else if constexpr (Epi::kTailSplit &&                                            \
+                           (SubTiles<BM_, BN_, WM_, WN_, RB_, MF_>::kHalf ||             \
+                            SubTiles<BM_, BN_, WM_, WN_, RB_, MF_>::kQuarter)) {         \
         DLM_LAUNCH((gemm_dl_kernel<BM_, BN_, WM_, WN_, SA_, S_, RB_, MF_, SP_, true, Epi>),    \
                    dim3((unsigned)blocks), dim3(WM_ * WN_ * 64), 0, st, A, lda, B, ldb, M, \
                    N, K, kps, n_n, n_m, group_m, n_tail, sub, rot, e);                        \

@@ -96,6 +96,7 @@ int gemm_dl_tile(int cfg, int* bm, int* bn, int* threads);
 int gemm_dl_mfma(int cfg);
 int gemm_dl_subs(int cfg);
 int gemm_dl_odd(int cfg);
+int gemm_dl_int8(int cfg);
 int gemm_dl_stages(int cfg);
 // one launch of configuration cfg with epilogue 0 (fp32 store of `splits` K
 // slices), 1 (SwiGLU to bf16, N = 2 F) or 2 (fp32 add), A [M, K], B [N, K],
@@ -111,13 +112,13 @@ constexpr int kFewRows = 1024;
 // allow_small: fp32 launches whose 128-wide tiles would not fill the CUs may use
 // the 16x32-tile kernel (plan cfg kSmallF32; every epilogue that needs only its
 // own wave)
-// join: K slices are added by a kernel of their own (and may differ by a k-tile); us: the
-// modelled time of a bf16 plan
+// join: K slices are added by a kernel of their own (and may differ by a k-tile); int8_us: the
+// plan is for 8-bit integers as half as many 2-byte elements (gemm_dl_int8 tiles), its modelled time
 constexpr int kSmallF32 = -2;
 GemmPlan gemm_plan(int elem_bytes, int M, int N, int K, bool splittable, int num_cu,
                    bool allow_mf32 = true, bool allow_tail = true, bool allow_odd = true,
                    int few_rows = kFewRows, bool allow_small = true, bool join = false,
-                   double* us = nullptr);
+                   double* int8_us = nullptr);
 // plan of the LM-head GEMM (M rows x V vocab entries)
 GemmPlan lm_head_plan(int elem_bytes, int M, int V, int K, int num_cu);
 template <typename T>

@@ -15,7 +15,6 @@ namespace dlm {
 namespace {
 
 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
-typedef int32_t i32x16 __attribute__((ext_vector_type(16)));
 typedef f32x4 f32x4u __attribute__((aligned(4)));      // at a float's alignment
 
 // 16x16x64 int8: lane l supplies A[row = l%16][k = 16*(l/16) .. +15] and B[col = l%16] of the same
@@ -108,13 +107,8 @@ __global__ __launch_bounds__(kQintWaves * 64) void qint_few_kernel(const int8_t*
 // ------------------------------------------------- the tiles of gemm_dl.hip --
 struct MulI8 {
   typedef i32x4 Acc16;
-  typedef i32x16 Acc32;
   __device__ __forceinline__ static Acc16 mma16(const u32x4& a, const u32x4& b, const Acc16& c) {
     return mfma16_i8(a, b, c);
-  }
-  __device__ __forceinline__ static Acc32 mma32(const u32x4& a, const u32x4& b, const Acc32& c) {
-    return __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b),
-                                                 c, 0, 0, 0);
   }
 };
 
@@ -130,8 +124,6 @@ struct EpiQintBase {
   bool vec;         // rows of y (and of the residual) are whole vectors of four
   __host__ __device__ void set_mfma(int) {}
   __device__ bool skip_tile(int) const { return false; }
-  template <int FM, int FN>
-  __device__ void op32(i32x16 (&)[FM][FN], int, int, int, int) const {}
 
   // The block's scales, in LDS (free by now): tokens m0 .. of bm rows, channels row(n0) .. of bn
   // columns. (Loaded by every lane for itself, fragment by fragment, each waits for memory: 37888 x

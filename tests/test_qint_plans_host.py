@@ -1,5 +1,5 @@
-"""Plans of products of 8-bit matrices (host only): row tiles go in groups where there are
-several."""
+"""Plans of products of 8-bit matrices (host only): tiles that exist for them, row tiles in groups
+where there are several."""
 import os
 import random
 
@@ -24,3 +24,13 @@ def test_groups_take_several_row_tiles():
         else:
             several += group > 0
     assert alone > 500 and several > 500
+
+
+def test_tiles_exist_for_8_bit_operands():
+    """Those of the vocabulary head alone, of 32 x 32 matrix instructions and 82 do not."""
+    rng = random.Random(6)
+    size = lambda lo, hi: int(lo * (hi / lo) ** rng.random())
+    for _ in range(10000):
+        n, k = 2 * size(1, 30000), size(1, 131071)
+        cfg = dlm.debug_qint_linear_plan(size(1, 20000), n, k, rng.randrange(3), rng.choice([8, 80, 256, 304]))[0]
+        assert cfg not in (1, 10, 11, 62, 65, 82)
